@@ -345,6 +345,80 @@ gpusq_status gpusq_gemm_int8_dense(const int8_t* Xq, const int8_t* Wq, const flo
                                    const float* bias, void* Y, gpusq_dtype out_dt, const float* out_scale,
                                    int64_t M, int64_t N, int64_t K, int epilogue, void* stream);
 
+/* ---- the operators of a decoder that reads what the encoder's layers above have made: products with 4-bit weights for a few tokens,
+ * the norm and rotation of queries and keys, attention over a 4-bit cache of the decoder's own tokens, attention to the encoder's states.
+ * They serve: none has a gradient.  head_dim is a multiple of 8 up to 256 (GPUSQ_ERR_UNSUPPORTED), heads a multiple of kv_heads
+ * (GPUSQ_ERR_SHAPE): query head h reads key head h / (heads / kv_heads).  Outputs must not overlap inputs.
+ *
+ * Linear layers on 4-bit weights with a scale for each `group` (32, 64 or 128; GPUSQ_ERR_UNSUPPORTED) consecutive weights of a row,
+ * K % group == 0:  W[n][k] = codes[n][k] * scales[n][k / group].
+ *   gpusq_quantize_groups_int4: fp32 W to codes (int8, -7..7) and scales (fp16): s = max|w| / 7 of the group rounded to fp16 (at most
+ *     65504; 1 where that is 0), code = clamp(rint(w / s), -7, 7) with that s, IEEE division, half to even, NaN 0.
+ *   gpusq_pack_int4_groups: codes (of -8..7) and scales (any fp16) to what the product reads: tiles of 16 rows, steps of 128 k;
+ *     [N / 16][K / 128][64 lanes][4 words]: word j of lane 16 g + r holds row r's k = 32 j + 8 g + 0..7 as code + 8, k + 2 i in bits
+ *     4 i .. + 3 and k + 2 i + 1 in bits 16 + 4 i .. + 3; then the scales [N / 16][K / 128 * (128 / group)][16 rows].  Rows and columns
+ *     beyond the matrix hold zeros.  gpusq_int4_groups_packed_bytes bytes (0 for invalid sizes).
+ *   gpusq_linear_int4: Y [M][N] (out_dt GPUSQ_F16 or GPUSQ_F32) = act(X [M][K] fp16 W^T + bias), products exact, sums in fp32, each
+ *     group's sum times its scale in fp32; GELU in its exact erf form.  N % 4 == 0 (GPUSQ_ERR_UNSUPPORTED).  Any M; made for up to 64
+ *     rows, beyond which the weights are read once for every 64. */
+size_t gpusq_int4_groups_packed_bytes(int64_t N, int64_t K, int group);
+gpusq_status gpusq_quantize_groups_int4(const float* W, int group, int8_t* codes, void* scales, int64_t N, int64_t K, void* stream);
+gpusq_status gpusq_pack_int4_groups(const int8_t* codes, const void* scales, int group, void* packed, int64_t N, int64_t K, void* stream);
+gpusq_status gpusq_linear_int4(const void* X, const void* Wpacked, int group, const float* bias, void* Y, gpusq_dtype out_dt, int64_t M,
+                               int64_t N, int64_t K, int epilogue, void* stream);
+
+/* The 4-bit cache: pages of 64 tokens, [num_pages][kv_heads][72 * DP bytes], DP = head_dim padded to 64, 128 or 256
+ * (gpusq_kv4_page_bytes(kv_heads, head_dim) bytes a page, 0 for invalid sizes).  Groups of 32 channels of a token and head share a scale,
+ * s = max|x| / 7 rounded to 7 significant bits (half to even; at most 896; 1 where fp16 has it as 0), code = clamp(rint(x / s), -7, 7):
+ * code * s is an fp16 number.  Inside a head's page, codes as code + 8:
+ *   key codes     [64 tokens][4 g][DP / 32 j] words: channels c = 32 j + 8 g + 0..7, c + 2 i in bits 4 i .. + 3, c + 2 i + 1 in 16 + 4 i .. + 3
+ *   key scales    [64 tokens][DP / 32] fp16
+ *   value codes   [16 quads of tokens][16 n][2 pairs][DP / 64 i][2 tokens] 16-bit places: channels DP / 16 * n + 4 i + 0..3, lowest first
+ *   value scales  [DP / 32][64 tokens] fp16
+ * Slot 64 p + t is token t of page p.  A slot is written whole by gpusq_qk_norm_rope; two tokens of one call must not share one. */
+size_t gpusq_kv4_page_bytes(int64_t kv_heads, int64_t head_dim);
+
+/* Norms of queries and keys for each head and the rotation by position, from a projection's output [tokens][heads + 2 kv_heads][head_dim]
+ * (queries, keys, values; dt GPUSQ_F16 or GPUSQ_F32; row_stride values from token to token, a multiple of 8), in one pass.
+ *   norm != 0: x * (1 / sqrt(mean(x^2) + eps)) * weight for every head's vector of queries (q_weight [head_dim], NULL: ones) and keys; eps >= 0.
+ *   rot_dim (0: no rotation; a multiple of 8): the first rot_dim channels turn: pairs (i, i + rot_dim / 2), or with interleaved != 0
+ *     (2 i, 2 i + 1), become (a c - b s, a s + b c) with c, s = cos, sin [table_rows][rot_dim / 2] at [positions[token]][i].  A position
+ *     outside the table takes the nearest row of it.
+ *   q_out [tokens][heads][head_dim] fp16.  Statistics and everything up to this rounding are in fp32.
+ *   cache NULL: k_out [tokens][kv_heads][head_dim] fp16, v_out NULL.
+ *   else the keys, and the values as they are, go to slots[token] of the cache (a slot outside it: that token is not kept); k_out and
+ *     v_out, where given, receive what the cache then stands for, code * scale. */
+gpusq_status gpusq_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_stride, int64_t tokens, int64_t heads, int64_t kv_heads,
+                                int64_t head_dim, int norm, const float* q_weight, const float* k_weight, float eps, const float* cos,
+                                const float* sin, const int32_t* positions, int64_t table_rows, int64_t rot_dim, int interleaved,
+                                void* q_out, void* k_out, void* v_out, void* cache, const int32_t* slots, int64_t num_pages, void* stream);
+
+/* Causal attention over the cache.  Sequence b has kv_lens[b] tokens in the cache (cut to 64 * max_pages), token t of it in page
+ * block_table[b][t / 64] (a page number outside the cache: these tokens are not seen); its queries are tokens cu_q[b] .. cu_q[b + 1] - 1
+ * of q [tokens][heads][head_dim] fp16, its last ones: the last query sees all kv_lens[b] tokens, the one before it one less.  max_q: the most
+ * queries of a sequence (of one that has more, only so many are answered).  cu_q NULL: max_q queries each, tokens = batch * max_q.
+ *   scale (0: 1 / sqrt(head_dim)) > 0.  out [tokens][heads][head_dim] fp16; 0 for a query that sees nothing, unspecified for a token that
+ *   no sequence has.  Scores, softmax and sums in fp32; the weights of the values are rounded to fp16.
+ *   workspace: gpusq_attention_kv4_workspace_bytes, may be NULL where that is 0 (long histories, few sequences: the keys are cut into parts
+ *   that are joined by a second launch); what it held does not matter. */
+size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads,
+                                           int64_t head_dim);
+gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* kv_lens, const int32_t* cu_q,
+                                 void* out, void* workspace, int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages,
+                                 int64_t num_pages, int64_t heads, int64_t kv_heads, int64_t head_dim, float scale, void* stream);
+
+/* Attention of q_len queries to kv_len keys and values of another source, or of the same one, without a causal mask: q [batch][q_len][heads],
+ * k, v [batch][kv_len][kv_heads], vectors of head_dim fp16 values, each dimension with a stride of its own in values (a multiple of 8,
+ * GPUSQ_ERR_ALIGN; not negative), so that heads may lie in a packed projection or apart.
+ *   kv_lens (or NULL): keys of batch b beyond kv_lens[b] are not seen; key_mask (or NULL) [batch][kv_len] bytes: keys of a 0 are not seen.
+ *   What is not seen may hold anything, NaN included.  scale, out [batch][q_len][heads][head_dim] and workspace as above. */
+size_t gpusq_cross_attention_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads, int64_t head_dim);
+gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, const int32_t* kv_lens, const uint8_t* key_mask, void* out,
+                                   void* workspace, int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads,
+                                   int64_t head_dim, int64_t q_batch_stride, int64_t q_stride, int64_t q_head_stride,
+                                   int64_t k_batch_stride, int64_t k_stride, int64_t k_head_stride, int64_t v_batch_stride,
+                                   int64_t v_stride, int64_t v_head_stride, float scale, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -497,6 +497,38 @@ gpusq_status launch_pack(const void* values, const uint8_t* meta, void* packed, 
 gpusq_status launch_prepare_weights(const float* W, gpusq_dtype dt, float* Wp, void* Wlow, float* w_scale, void* values,
                                     uint8_t* meta, void* packed, int64_t N, int64_t K, hipStream_t s);
 
+// the decoder's operators (linear4.hip, qk_norm.hip, attend.hip)
+gpusq_status launch_quantize_groups_int4(const float* W, int group, int8_t* codes, void* scales, int64_t N, int64_t K, hipStream_t s);
+gpusq_status launch_pack_int4_groups(const int8_t* codes, const void* scales, int group, void* packed, int64_t N, int64_t K, hipStream_t s);
+gpusq_status launch_linear_int4(const void* X, const void* W, int group, const float* bias, void* Y, bool f32, int64_t M, int64_t N, int64_t K, int epilogue,
+                                hipStream_t s);
+gpusq_status launch_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_stride, int64_t T, int64_t heads, int64_t kv_heads, int64_t D, int norm,
+                                 const float* q_weight, const float* k_weight, float eps, const float* cos, const float* sin, const int32_t* positions,
+                                 int64_t table_rows, int64_t R, int interleaved, void* q_out, void* k_out, void* v_out, void* cache, const int32_t* slots,
+                                 int64_t num_pages, hipStream_t s);
+struct AttentionKv4 {
+  const void *q, *cache;
+  const int32_t *block_table, *kv_lens, *cu_q;
+  void *out, *workspace;
+  int64_t tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim;
+  float scale;
+};
+struct CrossAttention {
+  const void *q, *k, *v;
+  const int32_t* kv_lens;
+  const uint8_t* key_mask;
+  void *out, *workspace;
+  int64_t batch, q_len, kv_len, heads, kv_heads, head_dim, q_stride[3], k_stride[3], v_stride[3];  // of a batch, a token, a head
+  float scale;
+};
+// how the keys of an attention are cut: parts of so many tiles of 32 keys
+struct AttendParts {
+  int parts, tiles;
+};
+AttendParts attend_parts(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t most_keys);
+gpusq_status launch_attention_kv4(const AttentionKv4& x, hipStream_t s);
+gpusq_status launch_cross_attention(const CrossAttention& x, hipStream_t s);
+
 inline gpusq_status check_launch() {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) {

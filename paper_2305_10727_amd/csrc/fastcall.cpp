@@ -8,9 +8,11 @@
 //   p  tensor, integer address or None (NULL)
 //   t  tensor on the GPU and contiguous (else ValueError), or None
 //   i  integer (int, int64_t, an enum)
+//   f  float, up to two
 //   s  torch's current stream; takes no argument
-// All of them travel in integer registers or 8-byte stack slots, so a function of any such parameters can be called through
-// one function type (x86-64 System V: the callee reads its parameters, the caller cleans up).
+// All but the floats travel in integer registers or 8-byte stack slots, the floats in the first vector registers wherever they stand among the
+// others, so a function of any such parameters can be called through one function type with the floats last (x86-64 System V: the callee
+// reads its parameters, the caller cleans up).
 //
 // Tensors are read, and results allocated (empty()), through torch's C++ interface: data_ptr() by way of Python takes 60 ns a tensor, torch.empty
 // by way of its Python arguments 1.8 us, which for the calls that prepare a layer's weights was half of what the host did.
@@ -25,8 +27,9 @@
 
 namespace {
 
-constexpr int kMaxArgs = 24;
-typedef int (*fn_t)(long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long);
+constexpr int kMaxArgs = 24, kMaxFloats = 2;
+typedef int (*fn_t)(long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long, long,
+                    float, float);
 
 struct FastCall {
   PyObject_HEAD
@@ -109,24 +112,29 @@ PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyObject* k
   if (given != f->wanted || (kwnames && PyTuple_GET_SIZE(kwnames) != 0))
     return PyErr_Format(PyExc_TypeError, "%U takes %d positional arguments", f->name, f->wanted);
   long a[kMaxArgs] = {0};
-  int at = 0;
+  float x[kMaxFloats] = {0};
+  int at = 0, to = 0, floats = 0;
   for (int i = 0; i < f->n; ++i) {
     switch (f->sig[i]) {
       case 's':
-        if (!current_stream(&a[i])) return nullptr;
+        if (!current_stream(&a[to++])) return nullptr;
         break;
       case 'i':
-        a[i] = PyLong_AsLong(args[at++]);
-        if (a[i] == -1 && PyErr_Occurred()) return nullptr;
+        a[to] = PyLong_AsLong(args[at++]);
+        if (a[to++] == -1 && PyErr_Occurred()) return nullptr;
+        break;
+      case 'f':
+        x[floats] = (float)PyFloat_AsDouble(args[at++]);
+        if (x[floats++] == -1.0f && PyErr_Occurred()) return nullptr;
         break;
       default:
-        if (!address_of(args[at++], f->sig[i] == 't', &a[i])) return nullptr;
+        if (!address_of(args[at++], f->sig[i] == 't', &a[to++])) return nullptr;
     }
   }
   int status;
   Py_BEGIN_ALLOW_THREADS
   status = f->fn(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15], a[16], a[17], a[18], a[19], a[20],
-                 a[21], a[22], a[23]);
+                 a[21], a[22], a[23], x[0], x[1]);
   Py_END_ALLOW_THREADS
   if (f->raw) return PyLong_FromLong(status);
   if (status == 0) Py_RETURN_NONE;
@@ -151,8 +159,10 @@ PyObject* make(PyTypeObject* type, PyObject* args, PyObject*) {
   int raw = 0;
   if (!PyArg_ParseTuple(args, "UKs|p", &name, &address, &sig, &raw)) return nullptr;
   const size_t n = strlen(sig);
-  if (n > kMaxArgs || strspn(sig, "ptis") != n) {
-    PyErr_SetString(PyExc_ValueError, "signature: up to 24 of p, t, i, s");
+  int floats = 0;
+  for (size_t i = 0; i < n; ++i) floats += sig[i] == 'f';
+  if (n > kMaxArgs || floats > kMaxFloats || strspn(sig, "ptifs") != n) {
+    PyErr_SetString(PyExc_ValueError, "signature: up to 24 of p, t, i, f, s, two of them f");
     return nullptr;
   }
   FastCall* f = (FastCall*)type->tp_alloc(type, 0);

@@ -1,0 +1,227 @@
+// Linear layers on 4-bit weights with group scales, for a few activation rows: Y = act(X W^T + b), W[n][k] = code[n][k] scale[n][k / G].
+//
+// Such a layer is bound by the bytes of its weights, half a byte and 2 / G of one for each; every other choice follows from reading them
+// once, in whole lines, with much in flight:
+//   - the packed operand is in the order of the registers that multiply it: 16 channels x 128 k are 1 KB, one 16-byte vector a lane,
+//     four words of 8 codes for the four 16 x 16 x 32 products of a step;
+//   - the weights are the first operand, whose rows are channels, and X the second, whose 16 columns are activation rows: one to 16
+//     rows cost the same;
+//   - codes are turned into fp16 integers, exact, and the products of a group summed in 32 bits before its scale, in 32 bits too,
+//     multiplies the sum: nothing is rounded before the output, whatever the scales;
+//   - a workgroup's wavefronts share its channels and deal out the steps of K; their sums meet in LDS once, at the end.
+#include "epilogue.h"
+#include "kv4.h"
+
+namespace gpusq {
+
+namespace {
+
+// ---- codes and scales of fp32 weights: the largest magnitude of each group / 7, as fp16; codes against the scale as it is kept ------------
+// One lane has 8 values: a group of 32, 64 or 128 is 4, 8 or 16 lanes.
+template <int GROUP>
+__global__ void __launch_bounds__(256) quantize_groups_kernel(const float* __restrict__ W, int8_t* __restrict__ codes, _Float16* __restrict__ scales, int64_t vecs) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const bool in = i < vecs;  // (vecs % (GROUP / 8) == 0: a group is inside or outside as a whole)
+  float x[8];
+  float amax = 0.0f;
+  if (in) {
+    const f4 a = ((const f4*)W)[2 * i], b = ((const f4*)W)[2 * i + 1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] = a[j];
+      x[4 + j] = b[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(x[j]));  // (a NaN is left out)
+#pragma unroll
+  for (int d = 1; d < GROUP / 8; d *= 2) amax = fmaxf(amax, __shfl_xor(amax, d));
+  _Float16 s16 = (_Float16)fminf(__fdiv_rn(amax, 7.0f), 65504.0f);
+  if (s16 == (_Float16)0.0f) s16 = (_Float16)1.0f;
+  const float s = (float)s16;
+  int q[8];
+  quantize_codes<8>(x, s, scale_reciprocal(s), q, 7.0f);
+  if (!in) return;
+  u2 out;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    out[h] = low_bytes((unsigned)q[4 * h], (unsigned)q[4 * h + 1], (unsigned)q[4 * h + 2], (unsigned)q[4 * h + 3]);
+  ((u2*)codes)[i] = out;
+  if (i % (GROUP / 8) == 0) scales[i / (GROUP / 8)] = s16;
+}
+
+// ---- packing: a thread writes one word (8 codes), or one scale ------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) pack_int4_groups_kernel(const int8_t* __restrict__ codes, const _Float16* __restrict__ scales, uint8_t* __restrict__ packed,
+                                                                int N, int K, int group, int kt, int64_t words, int64_t scale_places) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < words) {
+    const int j = (int)(i & 3), lane = (int)(i >> 2) & 63;
+    const int64_t tile = i >> 8;
+    const int64_t n = tile / kt * 16 + (lane & 15);
+    const int k = (int)(tile % kt) * 128 + 32 * j + 8 * (lane >> 4);
+    unsigned w = 0x88888888u;  // zeros beyond the matrix
+    if (n < N && k < K) {
+      const u2 c = *(const u2*)(codes + n * K + k);
+      w = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const unsigned code = (c[e >> 2] >> (8 * (e & 3))) & 0xFFu;
+        w |= ((code + 8u) & 15u) << ((e & 1) * 16 + (e >> 1) * 4);
+      }
+    }
+    ((unsigned*)packed)[i] = w;
+  }
+  if (i < scale_places) {
+    const int per = kt * (128 / group);
+    const int64_t n = i / 16 / per * 16 + (i & 15);
+    const int g = (int)(i / 16 % per);
+    _Float16 s = (_Float16)0.0f;
+    if (n < N && g < K / group) s = scales[n * (K / group) + g];
+    ((_Float16*)(packed + words * 4))[i] = s;
+  }
+}
+
+__device__ __forceinline__ float gelu_exact(float x) { return 0.5f * x * erfcf(-0.70710678118654752f * x); }
+
+// ---- the product ----------------------------------------------------------------------------------------------------------------------
+struct Linear4Args {
+  const _Float16* X;
+  const uint8_t* W;
+  const float* bias;
+  void* Y;
+  int M, N, K, kt, epilogue;
+};
+
+// MT columns of 16 activation rows, NF tiles of 16 channels, NW wavefronts; GROUP channels of a scale
+template <int MT, int NF, int NW, int GROUP, bool F32>
+__global__ void __launch_bounds__(64 * NW) linear_int4_kernel(const Linear4Args a) {
+  constexpr int PER = 128 / GROUP, CH = GROUP / 32;  // groups of a step, products of a group
+  __shared__ f4 part[NW][NF * MT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+  const int nt = (a.N + 15) >> 4;
+  const int tile0 = blockIdx.x * NF, m0 = blockIdx.y * 16 * MT;
+  const u4* codes[NF];
+  const h4* scales[NF];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) {
+    const int64_t tile = tile0 + f < nt ? tile0 + f : nt - 1;  // (a tile beyond the last is computed again and not stored)
+    codes[f] = (const u4*)(a.W + tile * a.kt * 1024) + lane;
+    scales[f] = (const h4*)(a.W + (int64_t)nt * a.kt * 1024 + tile * a.kt * PER * 32) + g;
+  }
+  const _Float16* x[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int row = m0 + 16 * m + r < a.M ? m0 + 16 * m + r : a.M - 1;  // (columns beyond the last row repeat it and are not stored)
+    x[m] = a.X + (int64_t)row * a.K + 8 * g;
+  }
+  f4 acc[NF][MT] = {};
+  for (int step = wave; step < a.kt; step += NW) {
+    u4 w[NF];
+    h4 s[NF][PER];
+    h8 b[MT][4];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      w[f] = codes[f][(int64_t)step * 64];
+#pragma unroll
+      for (int p = 0; p < PER; ++p) s[f][p] = scales[f][(step * PER + p) * 4];
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[m][j] = 128 * step + 32 * j < a.K ? *(const h8*)(x[m] + 128 * step + 32 * j) : h8(0);
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int p = 0; p < PER; ++p) {
+        f4 sum[MT] = {};
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const int j = p * CH + c;
+          h2 v[4];
+          codes_to_halves(w[f][j], v);
+          const h8 wa = {v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
+#pragma unroll
+          for (int m = 0; m < MT; ++m) sum[m] = mfma16(wa, b[m][j], sum[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[f][m][e] = __builtin_fmaf(sum[m][e], (float)s[f][p][e], acc[f][m][e]);
+      }
+  }
+#pragma unroll
+  for (int f = 0; f < NF; ++f)
+#pragma unroll
+    for (int m = 0; m < MT; ++m) part[wave][f * MT + m][lane] = acc[f][m];
+  __syncthreads();
+  for (int i = threadIdx.x; i < NF * MT * 64; i += 64 * NW) {
+    const int fm = i >> 6, l = i & 63;
+    f4 y = part[0][fm][l];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) y += part[w][fm][l];
+    const int n = (tile0 + fm / MT) * 16 + 4 * (l >> 4), m = m0 + fm % MT * 16 + (l & 15);
+    if (n >= a.N || m >= a.M) continue;  // (N % 4 == 0: four channels are inside or outside together)
+    if (a.epilogue & GPUSQ_EPI_BIAS) y += *(const f4*)(a.bias + n);
+    if (a.epilogue & GPUSQ_EPI_GELU) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = gelu_exact(y[e]);
+    }
+    const int64_t at = (int64_t)m * a.N + n;
+    if constexpr (F32) {
+      *(f4*)((float*)a.Y + at) = y;
+    } else {
+      const h4 out = {(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
+      *(h4*)((_Float16*)a.Y + at) = out;
+    }
+  }
+}
+
+template <int MT, int NF, int NW>
+void launch_shape(const Linear4Args& a, int group, bool f32, hipStream_t s) {
+  const dim3 grid((unsigned)ceil_div(ceil_div(a.N, 16), NF), (unsigned)ceil_div(a.M, 16 * MT));
+#define GPUSQ_LINEAR4(G, F) linear_int4_kernel<MT, NF, NW, G, F><<<grid, 64 * NW, 0, s>>>(a)
+  if (group == 32)
+    f32 ? GPUSQ_LINEAR4(32, true) : GPUSQ_LINEAR4(32, false);
+  else if (group == 64)
+    f32 ? GPUSQ_LINEAR4(64, true) : GPUSQ_LINEAR4(64, false);
+  else
+    f32 ? GPUSQ_LINEAR4(128, true) : GPUSQ_LINEAR4(128, false);
+#undef GPUSQ_LINEAR4
+}
+
+}  // namespace
+
+gpusq_status launch_quantize_groups_int4(const float* W, int group, int8_t* codes, void* scales, int64_t N, int64_t K, hipStream_t s) {
+  const int64_t vecs = N * (K / 8);
+  const unsigned blocks = (unsigned)ceil_div(vecs, 256);
+  if (group == 32)
+    quantize_groups_kernel<32><<<blocks, 256, 0, s>>>(W, codes, (_Float16*)scales, vecs);
+  else if (group == 64)
+    quantize_groups_kernel<64><<<blocks, 256, 0, s>>>(W, codes, (_Float16*)scales, vecs);
+  else
+    quantize_groups_kernel<128><<<blocks, 256, 0, s>>>(W, codes, (_Float16*)scales, vecs);
+  return check_launch();
+}
+
+gpusq_status launch_pack_int4_groups(const int8_t* codes, const void* scales, int group, void* packed, int64_t N, int64_t K, hipStream_t s) {
+  const int64_t nt = ceil_div(N, 16), kt = ceil_div(K, 128), words = nt * kt * 256, places = nt * kt * (128 / group) * 16;
+  pack_int4_groups_kernel<<<(unsigned)ceil_div(words, 256), 256, 0, s>>>(codes, (const _Float16*)scales, (uint8_t*)packed, (int)N, (int)K, group, (int)kt, words, places);
+  return check_launch();
+}
+
+gpusq_status launch_linear_int4(const void* X, const void* W, int group, const float* bias, void* Y, bool f32, int64_t M, int64_t N, int64_t K, int epilogue,
+                                hipStream_t s) {
+  const Linear4Args a{(const _Float16*)X, (const uint8_t*)W, bias, Y, (int)M, (int)N, (int)K, (int)ceil_div(K, 128), epilogue};
+  if (M <= 16)
+    launch_shape<1, 1, 8>(a, group, f32, s);
+  else if (M <= 32)
+    launch_shape<2, 2, 8>(a, group, f32, s);
+  else
+    launch_shape<4, 2, 8>(a, group, f32, s);
+  return check_launch();
+}
+
+}  // namespace gpusq

@@ -32,6 +32,8 @@ EXPORTS = [
     "gpusq_int4_to_sparse_int8", "gpusq_prune_n_of_m", "gpusq_force_kernel",
     "gpusq_quantize_tensor_int8_noalloc", "gpusq_linear_int8", "gpusq_linear_int8_launches", "gpusq_linear_int8_quantiser",
     "gpusq_block_mlp_int8", "gpusq_block_mlp_int8_launches",
+    "gpusq_int4_groups_packed_bytes", "gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_kv4_page_bytes",
+    "gpusq_qk_norm_rope", "gpusq_attention_kv4_workspace_bytes", "gpusq_attention_kv4", "gpusq_cross_attention_workspace_bytes", "gpusq_cross_attention",
 ]
 
 
@@ -44,7 +46,7 @@ class GpusqError(RuntimeError):
         super().__init__("%s: %s" % (where, msg))
 
 
-# C parameters of the calls that launch kernels (fastcall.cpp: p pointer, t checked tensor, i integer, s the stream)
+# C parameters of the calls that launch kernels (fastcall.cpp: p pointer, t checked tensor, i integer, f float, s the stream)
 _SIGNATURES = {
     "gpusq_prune_2to4": "tttiiis", "gpusq_cast_f16": "ttis", "gpusq_quantize_int8": "tittiiiits",
     "gpusq_quantize_tensor_int8_noalloc": "tittiiis", "gpusq_compress": "ttttiiis", "gpusq_check_2to4": "titiis",
@@ -59,6 +61,8 @@ _SIGNATURES = {
     "gpusq_gemm_fp16_dense": "ttttiiiis", "gpusq_gemm_int8_dense": "ttttttitiiiis", "gpusq_prune_4to8_pairs": "tttiiis",
     "gpusq_quantize_rows_int4": "tittiiis", "gpusq_compress_int4": "ttttiis", "gpusq_decompress_int4": "tttiis",
     "gpusq_int4_to_sparse_int8": "tttttiis", "gpusq_prune_n_of_m": "ttiiiis",
+    "gpusq_quantize_groups_int4": "tittiis", "gpusq_pack_int4_groups": "ttitiis", "gpusq_linear_int4": "ttittiiiiis",
+    "gpusq_qk_norm_rope": "piiiiiiittftttiiitttttis", "gpusq_attention_kv4": "tttttttiiiiiiiifs", "gpusq_cross_attention": "pppttttiiiiiiiiiiiiiiifs",
 }
 
 
@@ -178,6 +182,21 @@ def lib():
         L.gpusq_quantize_rows_int4.argtypes = [vp, ci, vp, vp, ci, i64, i64, vp]
         L.gpusq_compress_int4.argtypes = [vp, vp, vp, vp, i64, i64, vp]
         L.gpusq_decompress_int4.argtypes = [vp, vp, vp, i64, i64, vp]
+        cf, sz = ctypes.c_float, ctypes.c_size_t
+        L.gpusq_int4_groups_packed_bytes.argtypes = [i64, i64, ci]
+        L.gpusq_quantize_groups_int4.argtypes = [vp, ci, vp, vp, i64, i64, vp]
+        L.gpusq_pack_int4_groups.argtypes = [vp, vp, ci, vp, i64, i64, vp]
+        L.gpusq_linear_int4.argtypes = [vp, vp, ci, vp, vp, ci, i64, i64, i64, ci, vp]
+        L.gpusq_kv4_page_bytes.argtypes = [i64, i64]
+        L.gpusq_qk_norm_rope.argtypes = [vp, ci] + [i64] * 5 + [ci, vp, vp, cf, vp, vp, vp, i64, i64, ci] + [vp] * 5 + [i64, vp]
+        L.gpusq_attention_kv4_workspace_bytes.argtypes = [i64] * 7
+        L.gpusq_attention_kv4.argtypes = [vp] * 7 + [i64] * 8 + [cf, vp]
+        L.gpusq_cross_attention_workspace_bytes.argtypes = [i64] * 6
+        L.gpusq_cross_attention.argtypes = [vp] * 7 + [i64] * 15 + [cf, vp]
+        for name in ("gpusq_int4_groups_packed_bytes", "gpusq_kv4_page_bytes", "gpusq_attention_kv4_workspace_bytes", "gpusq_cross_attention_workspace_bytes"):
+            getattr(L, name).restype = sz
+        for name in ("gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_qk_norm_rope", "gpusq_attention_kv4", "gpusq_cross_attention"):
+            getattr(L, name).restype = ci
         for name in ("gpusq_prune_2to4", "gpusq_cast_f16", "gpusq_quantize_int8", "gpusq_compress", "gpusq_check_2to4", "gpusq_decompress", "gpusq_pack",
                      "gpusq_spgemm_fp16", "gpusq_spgemm_int8", "gpusq_gemm_fp16_dense", "gpusq_gemm_int8_dense"):
             getattr(L, name).restype = ci
@@ -450,3 +469,128 @@ def gemm_int8_dense(Xq, Wq, act_scale=None, w_scale=None, bias=None, gelu=False,
     Y = _empty(Xq, out_dtype, M, N) if out is None else out
     calls.gpusq_gemm_int8_dense(Xq, Wq, act_scale, w_scale, bias, Y, _TORCH_DT[out_dtype], out_scale, M, N, K, _epi(bias, gelu))
     return Y
+
+
+# ---- the decoder's operators.  What a kernel would read with the wrong type or beyond its end is refused here (ValueError), what the
+# library refuses by itself is left to it.
+def _is(t, dtype, *shape):
+    """Whether t is on the GPU, of that type and shape (None: any size there)"""
+    return t.is_cuda and t.dtype == dtype and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape))
+
+
+def _want(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def quantize_groups_int4(W, group):
+    """gpusq_quantize_groups_int4: W [N,K] fp32 -> (codes [N,K] int8 of -7..7, scales [N,K/group] fp16)"""
+    _want(_is(W, torch.float32, None, None), "W: [N, K] float32 on the GPU")
+    N, K = W.shape
+    codes, scales = _empty(W, torch.int8, N, K), _empty(W, torch.float16, N, K // max(group, 1))
+    calls.gpusq_quantize_groups_int4(W, group, codes, scales, N, K)
+    return codes, scales
+
+
+def pack_int4_groups(codes, scales, group):
+    """gpusq_pack_int4_groups: codes [N,K] int8 of -8..7, scales [N,K/group] fp16 -> the operand of linear_int4 (uint8)"""
+    _want(_is(codes, torch.int8, None, None), "codes: [N, K] int8 on the GPU")
+    N, K = codes.shape
+    _want(_is(scales, torch.float16, N, K // max(group, 1)), "scales: [N, K / group] float16 on the GPU")
+    nbytes = lib().gpusq_int4_groups_packed_bytes(N, K, group)
+    packed = _empty(codes, torch.uint8, max(nbytes, 16))
+    calls.gpusq_pack_int4_groups(codes, scales, group, packed, N, K)
+    return packed
+
+
+def linear_int4(X, packed, N, group, bias=None, gelu=False, out_dtype=torch.float16, out=None):
+    """gpusq_linear_int4: X [M,K] fp16, packed from pack_int4_groups -> act(X W^T + bias) [M,N] fp16 or fp32"""
+    _want(_is(X, torch.float16, None, None), "X: [M, K] float16 on the GPU")
+    M, K = X.shape
+    _want(_is(packed, torch.uint8, lib().gpusq_int4_groups_packed_bytes(N, K, group) or None), "packed: of other sizes than N, K and group")
+    _want(bias is None or _is(bias, torch.float32, N), "bias: [N] float32 on the GPU")
+    Y = _empty(X, out_dtype, M, N) if out is None else out
+    _want(out is None or _is(out, out_dtype, M, N), "out: [M, N] of out_dtype on the GPU")
+    calls.gpusq_linear_int4(X, packed, group, bias, Y, _TORCH_DT[out_dtype], M, N, K, _epi(bias, gelu))
+    return Y
+
+
+def kv4_cache(num_pages, kv_heads, head_dim, device="cuda"):
+    """Pages of a 4-bit cache [num_pages, kv_heads, bytes] uint8 (64 tokens each, not initialised)"""
+    nbytes = lib().gpusq_kv4_page_bytes(kv_heads, head_dim)
+    if nbytes == 0:
+        raise GpusqError(ERR_SHAPE, "gpusq_kv4_page_bytes")
+    return torch.empty((num_pages, kv_heads, nbytes // kv_heads), dtype=torch.uint8, device=device)
+
+
+def _is_cache(cache, kv_heads, head_dim):
+    return _is(cache, torch.uint8, None, kv_heads, (lib().gpusq_kv4_page_bytes(kv_heads, head_dim) // max(kv_heads, 1)) or None)
+
+
+def qk_norm_rope(qkv, heads, kv_heads, head_dim, q_weight=None, k_weight=None, eps=1e-6, norm=True, cos=None, sin=None, positions=None, interleaved=False,
+                 cache=None, slots=None, want_cached=False, q_out=None):
+    """gpusq_qk_norm_rope: qkv [T, (heads + 2 kv_heads) * head_dim] fp16 or fp32, rows contiguous -> (q [T,heads,head_dim], k [T,kv_heads,head_dim])
+    fp16.  With a cache (kv4_cache) keys and values go to slots [T] int32 of it and the result is q, with want_cached (q, k, v): what the
+    cache stands for."""
+    _want(qkv.is_cuda and qkv.dtype in (torch.float32, torch.float16) and qkv.dim() == 2 and qkv.shape[1] >= (heads + 2 * kv_heads) * head_dim and qkv.stride(1) == 1,
+          "qkv: [T, (heads + 2 kv_heads) * head_dim] float16 or float32 on the GPU, rows contiguous")
+    T, R, rows = qkv.shape[0], 0, 0
+    _want(all(w is None or _is(w, torch.float32, head_dim) for w in (q_weight, k_weight)), "norm weights: [head_dim] float32 on the GPU")
+    if cos is not None:
+        rows, R = cos.shape[0], 2 * cos.shape[-1]
+        _want(_is(cos, torch.float32, rows, R // 2) and sin is not None and _is(sin, torch.float32, rows, R // 2), "cos, sin: [rows, rot_dim / 2] float32 on the GPU")
+        _want(positions is not None and _is(positions, torch.int32, T), "positions: [T] int32 on the GPU")
+    q = _empty(qkv, torch.float16, T, heads, head_dim) if q_out is None else q_out
+    _want(q_out is None or _is(q_out, torch.float16, T, heads, head_dim), "q_out: [T, heads, head_dim] float16 on the GPU")
+    k = v = None
+    if cache is None or want_cached:
+        k = _empty(qkv, torch.float16, T, kv_heads, head_dim)
+    if cache is not None:
+        _want(_is_cache(cache, kv_heads, head_dim), "cache: of other heads than kv_heads and head_dim")
+        _want(slots is not None and _is(slots, torch.int32, T), "slots: [T] int32 on the GPU")
+        v = _empty(qkv, torch.float16, T, kv_heads, head_dim) if want_cached else None
+    calls.gpusq_qk_norm_rope(qkv, _TORCH_DT[qkv.dtype], qkv.stride(0), T, heads, kv_heads, head_dim, int(norm), q_weight, k_weight, eps, cos, sin, positions, rows, R,
+                             int(interleaved), q, k, v, cache, slots, 0 if cache is None else cache.shape[0])
+    return (q, k) if cache is None else (q, k, v) if want_cached else q
+
+
+def _workspace(like, nbytes):
+    return _empty(like, torch.uint8, nbytes) if nbytes else None
+
+
+def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=1, scale=None, out=None, workspace=None):
+    """gpusq_attention_kv4: q [tokens,heads,head_dim] fp16, cache [pages,kv_heads,bytes], block_table [batch,max_pages] int32, kv_lens [batch] int32,
+    cu_q [batch + 1] int32 (None: max_q queries each) -> [tokens,heads,head_dim] fp16"""
+    _want(q.is_cuda and q.dtype == torch.float16 and q.dim() == 3, "q: [tokens, heads, head_dim] float16 on the GPU")
+    tokens, heads, D = q.shape
+    _want(cache.dim() == 3 and _is_cache(cache, cache.shape[1], D), "cache: of another head_dim than q")
+    _want(_is(block_table, torch.int32, None, None), "block_table: [batch, max_pages] int32 on the GPU")
+    batch, max_pages = block_table.shape
+    _want(_is(kv_lens, torch.int32, batch), "kv_lens: [batch] int32 on the GPU")
+    _want(cu_q is None or _is(cu_q, torch.int32, batch + 1), "cu_q: [batch + 1] int32 on the GPU")
+    o = torch.empty_like(q) if out is None else out
+    _want(out is None or _is(out, torch.float16, tokens, heads, D), "out: [tokens, heads, head_dim] float16 on the GPU")
+    nbytes = lib().gpusq_attention_kv4_workspace_bytes(tokens, batch, max_q, max_pages, heads, cache.shape[1], D)
+    _want(workspace is None or workspace.numel() * workspace.element_size() >= nbytes, "workspace: too small")
+    calls.gpusq_attention_kv4(q, cache, block_table, kv_lens, cu_q, o, _workspace(q, nbytes) if workspace is None else workspace, tokens, batch, max_q, max_pages,
+                              cache.shape[0], heads, cache.shape[1], D, 0.0 if scale is None else scale)
+    return o
+
+
+def cross_attention(q, k, v, kv_lens=None, key_mask=None, scale=None, out=None, workspace=None):
+    """gpusq_cross_attention: q [batch,q_len,heads,head_dim], k, v [batch,kv_len,kv_heads,head_dim] fp16 with any strides but a head's vector
+    contiguous; kv_lens [batch] int32, key_mask [batch,kv_len] uint8 or bool (0: not seen) -> [batch,q_len,heads,head_dim] fp16"""
+    _want(all(t.is_cuda and t.dtype == torch.float16 and t.dim() == 4 and t.stride(3) == 1 for t in (q, k, v)),
+          "q, k, v: four dimensions, float16, on the GPU, the last dimension contiguous")
+    B, Tq, H, D = q.shape
+    S, G = k.shape[1], k.shape[2]
+    _want(k.shape == v.shape and k.shape[0] == B and k.shape[3] == D, "k, v: [batch, kv_len, kv_heads, head_dim] of q's batch and head_dim")
+    _want(kv_lens is None or _is(kv_lens, torch.int32, B), "kv_lens: [batch] int32 on the GPU")
+    _want(key_mask is None or _is(key_mask, torch.uint8, B, S) or _is(key_mask, torch.bool, B, S), "key_mask: [batch, kv_len] uint8 or bool on the GPU")
+    o = _empty(q, torch.float16, B, Tq, H, D) if out is None else out
+    _want(out is None or _is(out, torch.float16, B, Tq, H, D), "out: [batch, q_len, heads, head_dim] float16 on the GPU")
+    nbytes = lib().gpusq_cross_attention_workspace_bytes(B, Tq, S, H, G, D)
+    _want(workspace is None or workspace.numel() * workspace.element_size() >= nbytes, "workspace: too small")
+    calls.gpusq_cross_attention(q, k, v, kv_lens, key_mask, o, _workspace(q, nbytes) if workspace is None else workspace, B, Tq, S, H, G, D,
+                                *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], 0.0 if scale is None else scale)
+    return o

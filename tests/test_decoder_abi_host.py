@@ -1,0 +1,133 @@
+"""Host-only checks of the decoder's operators: arguments that are refused before anything is launched, sizes of buffers, the places of the
+4-bit formats.  No kernel is launched here."""
+import ctypes
+
+import numpy as np
+import pytest
+
+import decoder_reference as ref
+from test_abi_host import lib  # noqa: F401
+
+OK, ERR_NULL, ERR_SHAPE, ERR_ALIGN, ERR_UNSUPPORTED = range(5)
+P, ODD = 0x10000, 0x10008  # never dereferenced: every call below fails validation first
+
+
+@pytest.fixture(scope="module")
+def g():
+    pytest.importorskip("torch")
+    from paper_2305_10727_amd import gpusq
+    gpusq.lib()
+    return gpusq
+
+
+def _refuses(g, name, good, changes):
+    """good: arguments by name, in order; changes: (status, {name: value})"""
+    fn = getattr(g.lib(), name)
+    for status, change in changes:
+        assert set(change) <= set(good)
+        assert fn(*{**good, **change}.values()) == status, (name, change)
+
+
+def test_linear_int4(g):
+    base = dict(W=P, group=64, codes=P, scales=P, N=64, K=128, stream=None)
+    _refuses(g, "gpusq_quantize_groups_int4", base, [
+        (ERR_NULL, dict(W=None)), (ERR_NULL, dict(codes=None)), (ERR_NULL, dict(scales=None)), (ERR_SHAPE, dict(N=0)), (ERR_SHAPE, dict(K=96)), (ERR_SHAPE, dict(K=-128)),
+        (ERR_SHAPE, dict(N=2**31)), (ERR_UNSUPPORTED, dict(group=16)), (ERR_UNSUPPORTED, dict(group=0)), (ERR_ALIGN, dict(W=ODD)), (ERR_ALIGN, dict(codes=ODD)), (ERR_ALIGN, dict(scales=ODD))])
+    base = dict(codes=P, scales=P, group=64, packed=P, N=64, K=128, stream=None)
+    _refuses(g, "gpusq_pack_int4_groups", base, [(ERR_NULL, dict(packed=None)), (ERR_SHAPE, dict(K=32)), (ERR_UNSUPPORTED, dict(group=256)), (ERR_ALIGN, dict(packed=ODD))])
+    base = dict(X=P, W=P, group=32, bias=P, Y=P, out_dt=g.F16, M=3, N=64, K=128, epilogue=g.EPI_BIAS, stream=None)
+    _refuses(g, "gpusq_linear_int4", base, [
+        (ERR_NULL, dict(X=None)), (ERR_NULL, dict(W=None)), (ERR_NULL, dict(Y=None)), (ERR_NULL, dict(bias=None)), (ERR_SHAPE, dict(M=0)), (ERR_SHAPE, dict(M=2**31)),
+        (ERR_SHAPE, dict(M=16 * 65535 + 1)), (ERR_SHAPE, dict(K=100)), (ERR_UNSUPPORTED, dict(N=62)), (ERR_UNSUPPORTED, dict(out_dt=g.I8)), (ERR_UNSUPPORTED, dict(epilogue=5)),
+        (ERR_UNSUPPORTED, dict(group=8)), (ERR_ALIGN, dict(X=ODD)), (ERR_ALIGN, dict(W=ODD)), (ERR_ALIGN, dict(Y=ODD)), (ERR_ALIGN, dict(bias=ODD))])
+    size = g.lib().gpusq_int4_groups_packed_bytes
+    assert size(64, 128, 32) == 4 * (1024 + 128) and size(65, 129 * 32, 32) == 5 * 33 * 1152 and size(16, 192, 64) == 2 * (1024 + 64) and size(16, 128, 128) == 1024 + 32
+    assert size(64, 100, 32) == 0 and size(64, 128, 48) == 0 and size(0, 128, 32) == 0
+
+
+def test_qk_norm_rope(g):
+    base = dict(qkv=P, dt=g.F16, row_stride=512, tokens=3, heads=4, kv_heads=2, head_dim=64, norm=1, qw=P, kw=P, eps=1e-6, cos=P, sin=P, positions=P, rows=9, rot=64, interleaved=0,
+                q=P, k=P, v=P, cache=P, slots=P, pages=4, stream=None)
+    _refuses(g, "gpusq_qk_norm_rope", base, [
+        (ERR_NULL, dict(qkv=None)), (ERR_NULL, dict(q=None)), (ERR_NULL, dict(slots=None)), (ERR_NULL, dict(cos=None)), (ERR_NULL, dict(sin=None)), (ERR_NULL, dict(positions=None)),
+        (ERR_NULL, dict(cache=None, k=None, v=None)), (ERR_UNSUPPORTED, dict(cache=None)), (ERR_SHAPE, dict(tokens=0)), (ERR_SHAPE, dict(heads=3)), (ERR_SHAPE, dict(kv_heads=0)),
+        (ERR_SHAPE, dict(row_stride=504)), (ERR_UNSUPPORTED, dict(row_stride=516)), (ERR_SHAPE, dict(rot=72)), (ERR_SHAPE, dict(rot=-8)), (ERR_UNSUPPORTED, dict(rot=20)),
+        (ERR_SHAPE, dict(rows=0)), (ERR_SHAPE, dict(pages=0)), (ERR_SHAPE, dict(pages=2**25)), (ERR_UNSUPPORTED, dict(dt=g.I8)), (ERR_UNSUPPORTED, dict(eps=-1.0)),
+        (ERR_UNSUPPORTED, dict(eps=float("nan"))), (ERR_UNSUPPORTED, dict(head_dim=60)), (ERR_UNSUPPORTED, dict(head_dim=264, row_stride=4096)), (ERR_ALIGN, dict(qkv=ODD)),
+        (ERR_ALIGN, dict(q=ODD)), (ERR_ALIGN, dict(k=ODD)), (ERR_ALIGN, dict(v=ODD)), (ERR_ALIGN, dict(cache=ODD)), (ERR_ALIGN, dict(qw=ODD)), (ERR_ALIGN, dict(kw=ODD)),
+        (ERR_ALIGN, dict(cos=ODD)), (ERR_ALIGN, dict(sin=ODD)), (ERR_ALIGN, dict(slots=P + 2)), (ERR_ALIGN, dict(positions=P + 1))])
+
+
+def test_attention_kv4(g):
+    base = dict(q=P, cache=P, table=P, lens=P, cu=P, out=P, ws=P, tokens=5, batch=2, max_q=3, max_pages=100, pages=300, heads=8, kv_heads=2, head_dim=128, scale=0.0, stream=None)
+    _refuses(g, "gpusq_attention_kv4", base, [
+        (ERR_NULL, dict(q=None)), (ERR_NULL, dict(cache=None)), (ERR_NULL, dict(table=None)), (ERR_NULL, dict(lens=None)), (ERR_NULL, dict(out=None)), (ERR_NULL, dict(ws=None)),
+        (ERR_SHAPE, dict(heads=7)), (ERR_SHAPE, dict(tokens=0)), (ERR_SHAPE, dict(batch=0)), (ERR_SHAPE, dict(max_q=6)), (ERR_SHAPE, dict(cu=None)), (ERR_SHAPE, dict(max_pages=0)),
+        (ERR_SHAPE, dict(max_pages=2**25)), (ERR_SHAPE, dict(pages=0)), (ERR_SHAPE, dict(tokens=2**29)), (ERR_UNSUPPORTED, dict(head_dim=12)), (ERR_UNSUPPORTED, dict(scale=-1.0)),
+        (ERR_UNSUPPORTED, dict(scale=float("nan"))), (ERR_UNSUPPORTED, dict(scale=float("inf"))), (ERR_ALIGN, dict(q=ODD)), (ERR_ALIGN, dict(cache=ODD)), (ERR_ALIGN, dict(out=ODD)),
+        (ERR_ALIGN, dict(ws=ODD)), (ERR_ALIGN, dict(table=P + 2)), (ERR_ALIGN, dict(lens=P + 2)), (ERR_ALIGN, dict(cu=P + 2))])
+    size = g.lib().gpusq_attention_kv4_workspace_bytes
+    assert size(1, 1, 1, 1, 8, 2, 128) == 0 and size(1, 1, 1, 2000, 8, 2, 128) % (8 * 130 * 4) == 0 < size(1, 1, 1, 2000, 8, 2, 128)
+    assert size(0, 1, 1, 1, 8, 2, 128) == 0 and size(1, 1, 1, 2000, 8, 3, 128) == 0
+    assert g.lib().gpusq_kv4_page_bytes(2, 128) == 2 * 9216 and g.lib().gpusq_kv4_page_bytes(1, 40) == 4608 and g.lib().gpusq_kv4_page_bytes(3, 136) == 3 * 18432
+    assert g.lib().gpusq_kv4_page_bytes(0, 128) == 0 and g.lib().gpusq_kv4_page_bytes(2, 260) == 0
+
+
+def test_cross_attention(g):
+    base = dict(q=P, k=P, v=P, lens=P, mask=P, out=P, ws=P, batch=1, q_len=1, kv_len=5000, heads=8, kv_heads=2, head_dim=64, qb=512, qt=512, qh=64, kb=640000, kt=128, kh=64, vb=640000,
+                vt=128, vh=64, scale=0.0, stream=None)
+    _refuses(g, "gpusq_cross_attention", base, [
+        (ERR_NULL, dict(q=None)), (ERR_NULL, dict(k=None)), (ERR_NULL, dict(v=None)), (ERR_NULL, dict(out=None)), (ERR_NULL, dict(ws=None)), (ERR_SHAPE, dict(heads=9)),
+        (ERR_SHAPE, dict(batch=0)), (ERR_SHAPE, dict(q_len=0)), (ERR_SHAPE, dict(kv_len=0)), (ERR_SHAPE, dict(kv_len=2**31 - 1)), (ERR_SHAPE, dict(batch=2**20, q_len=2**20)),
+        (ERR_SHAPE, dict(qt=-8)), (ERR_SHAPE, dict(vb=2**41)), (ERR_ALIGN, dict(kt=132)), (ERR_ALIGN, dict(vh=60)), (ERR_ALIGN, dict(qb=4)), (ERR_UNSUPPORTED, dict(head_dim=4)),
+        (ERR_UNSUPPORTED, dict(scale=-0.1)), (ERR_ALIGN, dict(q=ODD)), (ERR_ALIGN, dict(k=ODD)), (ERR_ALIGN, dict(v=ODD)), (ERR_ALIGN, dict(out=ODD)), (ERR_ALIGN, dict(lens=P + 1))])
+    size = g.lib().gpusq_cross_attention_workspace_bytes
+    assert size(64, 1, 577, 16, 16, 64) == 0 and size(1, 1, 5000, 8, 2, 64) > 0 and size(1, 1, 0, 8, 2, 64) == 0
+
+
+def test_floats_reach_their_parameters_among_the_others():
+    """The extension module passes floats in registers of their own: a C function of mixed parameters sees each where it stands"""
+    torch = pytest.importorskip("torch")
+    from paper_2305_10727_amd import _fastcall, gpusq
+    seen = []
+    proto = ctypes.CFUNCTYPE(ctypes.c_int, *([ctypes.c_long] * 3), ctypes.c_float, *([ctypes.c_long] * 6), ctypes.c_float, ctypes.c_long)
+    fn = proto(lambda *a: seen.append(a) or 0)
+    _fastcall.setup(lambda: 0, lambda d: 77, gpusq._raise)
+    try:
+        call = _fastcall.FastCall("mixed", ctypes.cast(fn, ctypes.c_void_p).value, "iiifiiiiiifs")
+        call(1, 2, 3, 0.5, 4, 5, 6, 7, 8, 9, -1.0)
+    finally:
+        _fastcall.setup(torch._C._cuda_getDevice, gpusq._stream_of, gpusq._raise)
+    assert seen == [(1, 2, 3, 0.5, 4, 5, 6, 7, 8, 9, -1.0, 77)]
+    with pytest.raises(TypeError):
+        call(1, 2, 3, "x", 4, 5, 6, 7, 8, 9, 1.0)
+    with pytest.raises(ValueError):
+        _fastcall.FastCall("three", 1, "fff")
+
+
+@pytest.mark.parametrize("D", [8, 64, 80, 128, 136, 256])
+def test_every_place_of_a_page_is_used_once(D):
+    """Of a page's nibbles and scales no two values share one, none is left over, and a token's key bytes and 16-bit value places are its own"""
+    p = ref.Places(D)
+    nibbles = np.concatenate([(p.k_byte * 2 + p.k_shift // 4).ravel(), (p.v_byte * 2 + p.v_shift // 4).ravel()])
+    scales = np.concatenate([p.k_scale.ravel(), p.v_scale.ravel()])
+    taken = np.concatenate([nibbles, *[scales * 4 + i for i in range(4)]])
+    assert np.array_equal(np.sort(taken), np.arange(2 * p.bytes))
+    for byte, unit in ((p.k_byte, 1), (p.v_byte, 2)):
+        owner = {}
+        for t in range(64):
+            for at in set((byte[t] // unit).tolist()):
+                assert owner.setdefault(at, t) == t
+
+
+def test_formats_read_back():
+    r = np.random.default_rng(0)
+    for D in (40, 128, 200):
+        x = r.standard_normal((2, 3, 64, D)).astype(np.float32)
+        c, s = ref.cache_codes(x)
+        assert abs(c).max() == 7
+        K, V = ref.read_pages(ref.write_pages(c, s, -c, s, D), D)
+        exp = c * s.astype(np.float64).repeat(32, -1)[..., :D]
+        assert np.array_equal(K, exp) and np.array_equal(V, -exp)
+        assert np.array_equal(exp.astype(np.float16).astype(np.float64), exp)  # fp16 numbers
+        assert (np.abs(exp - x) <= 0.56 * s.astype(np.float64).repeat(32, -1)[..., :D]).all()

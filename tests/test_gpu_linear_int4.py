@@ -1,0 +1,127 @@
+"""Linear layers on 4-bit weights with group scales against their definition in 64 bits."""
+import numpy as np
+import pytest
+
+import decoder_reference as ref
+from test_gpu_parity import dev, g, host  # noqa: F401
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _weights(N, K, group, seed):
+    r = np.random.default_rng(seed)
+    codes = r.integers(-8, 8, (N, K)).astype(np.int8)
+    scales = (r.uniform(0.5, 2, (N, K // group)) * 0.01).astype(np.float16)
+    return codes, scales
+
+
+def _gelu(x):
+    from scipy.special import ndtr
+    return x * ndtr(x)
+
+
+def _check(y, X, codes, scales, group, bias, gelu, K):
+    W = codes.astype(np.float64) * scales.astype(np.float64).repeat(group, 1)
+    X64 = X.astype(np.float64)
+    exp, size = X64 @ W.T, np.abs(X64) @ np.abs(W.T)
+    if bias is not None:
+        exp, size = exp + bias, size + np.abs(bias)
+    # sums of K products in 32 bits, each step off by 2^-24 of what it has; GELU's slope is at most 1.13, its own error a few 2^-24
+    off = (K + 16) * 2.0 ** -24 * size * (1.13 if gelu else 1)
+    if gelu:
+        exp = _gelu(exp)
+        off = off + 2.0 ** -20 * np.abs(exp) + 1e-30
+    if y.dtype == np.float16:
+        off = off + 2.0 ** -11 * (np.abs(exp) + off) + 2.0 ** -25
+    else:
+        off = off + 2.0 ** -24 * np.abs(exp)
+    assert (np.abs(y.astype(np.float64) - exp) <= off).all(), np.max(np.abs(y - exp) / off)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("N,K", [(4, 128), (37, 256), (130, 1152)])
+def test_quantise_and_pack(g, N, K, group):
+    r = np.random.default_rng(N + group)
+    W = (r.standard_normal((N, K)) * 0.02).astype(np.float32)
+    W[0, :group] = 0.0
+    W[1, 3], W[2, 5], W[2, group - 1] = np.inf, np.nan, -3.0
+    W[3, :group] = 1e-9  # a scale that is 0 in fp16
+    W[-1, -group:] *= np.float32(1e-4)  # a scale among fp16's subnormal numbers
+    codes, scales = g.quantize_groups_int4(dev(W), group)
+    exp_c, exp_s = ref.groups_int4(W, group)
+    assert np.array_equal(host(codes), exp_c) and np.array_equal(host(scales).view(np.uint16), exp_s.view(np.uint16))
+    codes[0, 1] = -8  # not a code of the quantiser, but one of 4 bits
+    exp_c[0, 1] = -8
+    packed = g.pack_int4_groups(codes, scales, group)
+    assert np.array_equal(host(packed), ref.pack_int4(exp_c, exp_s, group))
+
+
+# a row, one more and one less than a block of 16, several, and more than one pass over the weights; fewer channels than a tile, tiles that
+# are not full; K of one chunk of 32, of part of a step, of fewer and of more steps than wavefronts
+@pytest.mark.parametrize("M", [1, 2, 7, 15, 16, 17, 32, 33, 48, 64, 65, 150])
+@pytest.mark.parametrize("N,K,group", [(4, 32, 32), (20, 160, 32), (64, 192, 64), (1000, 1152, 128), (132, 1088, 64), (48, 2560, 128)])
+def test_product(g, M, N, K, group):
+    codes, scales = _weights(N, K, group, M + N)
+    r = np.random.default_rng(M)
+    X, bias = r.standard_normal((M, K)).astype(np.float16), r.standard_normal(N).astype(np.float32)
+    packed = g.pack_int4_groups(dev(codes), dev(scales), group)
+    for use_bias, gelu, dt in ((True, False, torch.float16), (False, False, torch.float32), (True, True, torch.float16), (True, True, torch.float32)):
+        y = g.linear_int4(dev(X), packed, N, group, bias=dev(bias) if use_bias else None, gelu=gelu, out_dtype=dt)
+        _check(host(y), X, codes, scales, group, bias if use_bias else None, gelu, K)
+
+
+def test_scales_of_every_size(g):
+    """subnormal, huge and zero scales: the sums of a group meet them in 32 bits"""
+    N, K, group = 32, 512, 32
+    codes, scales = _weights(N, K, group, 3)
+    scales[0], scales[1], scales[2, ::2], scales[3] = 6e-8, 5e-6, 0.0, 60000.0
+    X = np.random.default_rng(4).standard_normal((9, K)).astype(np.float16)
+    y = g.linear_int4(dev(X), g.pack_int4_groups(dev(codes), dev(scales), group), N, group, out_dtype=torch.float32)
+    _check(host(y), X, codes, scales, group, None, False, K)
+
+
+def test_a_row_without_a_value_keeps_to_itself(g):
+    N, K, group = 52, 416, 32
+    codes, scales = _weights(N, K, group, 5)
+    packed = g.pack_int4_groups(dev(codes), dev(scales), group)
+    X = np.random.default_rng(6).standard_normal((20, K)).astype(np.float16)
+    clean = host(g.linear_int4(dev(X), packed, N, group))
+    X[4, 7], X[18, 400] = np.nan, np.inf
+    y = host(g.linear_int4(dev(X), packed, N, group))
+    rest = [i for i in range(20) if i not in (4, 18)]
+    assert np.array_equal(y[rest], clean[rest]) and np.isnan(y[4]).all() and not np.isfinite(y[18]).any()
+
+
+def test_rows_of_a_larger_call_and_other_streams(g):
+    """Every row as in a call of its own size, on a stream that is not the default one, outputs given"""
+    N, K, group = 256, 1024, 64
+    codes, scales = _weights(N, K, group, 7)
+    packed = g.pack_int4_groups(dev(codes), dev(scales), group)
+    X16 = np.random.default_rng(8).standard_normal((16, K)).astype(np.float16)
+    X = dev(X16)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        out = torch.full((16, N), 7, dtype=torch.float16, device="cuda")
+        assert g.linear_int4(X, packed, N, group, out=out) is out
+        one = [g.linear_int4(X[i:i + 1], packed, N, group) for i in range(16)]
+        torch.cuda.current_stream().synchronize()
+    _check(host(out), X16, codes, scales, group, None, False, K)
+    _check(host(torch.cat(one)), X16, codes, scales, group, None, False, K)
+
+
+def test_refusals(g):
+    packed = torch.zeros(g.lib().gpusq_int4_groups_packed_bytes(64, 128, 32), dtype=torch.uint8, device="cuda")
+    X = torch.zeros((2, 128), dtype=torch.float16, device="cuda")
+    assert g.linear_int4(X, packed, 64, 32).shape == (2, 64)
+    for bad in (lambda: g.linear_int4(X.float(), packed, 64, 32), lambda: g.linear_int4(X, packed[:-16], 64, 32), lambda: g.linear_int4(X, packed, 68, 128),
+                lambda: g.linear_int4(X, packed, 64, 32, bias=torch.zeros(63, device="cuda")), lambda: g.linear_int4(X.cpu(), packed, 64, 32),
+                lambda: g.linear_int4(X[:, ::2], packed, 64, 32), lambda: g.linear_int4(X, packed, 64, 32, out=torch.zeros((2, 64), device="cuda")),
+                lambda: g.quantize_groups_int4(X, 32), lambda: g.pack_int4_groups(X.to(torch.int8), torch.zeros((2, 3), dtype=torch.float16, device="cuda"), 32)):
+        with pytest.raises(ValueError):
+            bad()
+    for group in (16, 0, 48):
+        with pytest.raises(g.GpusqError):
+            g.quantize_groups_int4(X.float(), group)
+    with pytest.raises(g.GpusqError):
+        g.quantize_groups_int4(torch.zeros((2, 100), device="cuda"), 32)
