@@ -218,7 +218,29 @@ PyObject* empty(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// is_tensor(t, dtype, *sizes): whether t is a tensor on the GPU of that type and those sizes (-1: any).  A tenth of what the same
+// questions take from Python.
+PyObject* is_tensor(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n < 2 || !THPDtype_Check(args[1])) {
+    PyErr_SetString(PyExc_TypeError, "is_tensor(t, dtype, *sizes): a dtype, sizes or -1");
+    return nullptr;
+  }
+  if (!THPVariable_Check(args[0])) Py_RETURN_FALSE;
+  const at::Tensor& t = THPVariable_Unpack(args[0]);
+  bool yes = t.is_cuda() && t.scalar_type() == ((THPDtype*)args[1])->scalar_type && t.dim() == n - 2;
+  for (Py_ssize_t i = 2; i < n && yes; ++i) {
+    const long size = PyLong_AsLong(args[i]);
+    if (size == -1 && PyErr_Occurred()) return nullptr;
+    yes = size == -1 || t.size(i - 2) == size;
+  }
+  if (yes) Py_RETURN_TRUE;
+  Py_RETURN_FALSE;
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef g_methods[] = {{"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, "empty(like, dtype, *sizes)"},
+                           {"is_tensor", (PyCFunction)(void (*)(void))is_tensor, METH_FASTCALL, "is_tensor(t, dtype, *sizes)"},
                            {"setup", setup, METH_VARARGS, "setup(get_device, get_stream, on_error)"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fastcall", "C functions as cheap Python callables", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

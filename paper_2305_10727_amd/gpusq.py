@@ -6,6 +6,7 @@ is the ctypes handle on the same library for everything else.
 There is no fallback: if the library has not been built, or no GPU tensor is passed, the calls raise.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -472,10 +473,13 @@ def gemm_int8_dense(Xq, Wq, act_scale=None, w_scale=None, bias=None, gelu=False,
 
 
 # ---- the decoder's operators.  What a kernel would read with the wrong type or beyond its end is refused here (ValueError), what the
-# library refuses by itself is left to it.
-def _is(t, dtype, *shape):
-    """Whether t is on the GPU, of that type and shape (None: any size there)"""
-    return t.is_cuda and t.dtype == dtype and t.dim() == len(shape) and all(n is None or n == m for n, m in zip(shape, t.shape))
+# library refuses by itself is left to it.  A token's calls are as long as a launch, so the questions are few and asked in the extension module.
+def _is(t, dtype, *sizes):
+    """Whether t is a tensor on the GPU, of that type and those sizes (-1: any); the extension module, loaded on first use, takes its place"""
+    global _is
+    from . import _fastcall
+    _is = _fastcall.is_tensor
+    return _is(t, dtype, *sizes)
 
 
 def _want(ok, what):
@@ -483,9 +487,15 @@ def _want(ok, what):
         raise ValueError(what)
 
 
+@functools.lru_cache(maxsize=1024)
+def _size(name, *sizes):
+    """What a size query of the library answers (-1 for 0: sizes that it does not take)"""
+    return getattr(lib(), name)(*sizes) or -1
+
+
 def quantize_groups_int4(W, group):
     """gpusq_quantize_groups_int4: W [N,K] fp32 -> (codes [N,K] int8 of -7..7, scales [N,K/group] fp16)"""
-    _want(_is(W, torch.float32, None, None), "W: [N, K] float32 on the GPU")
+    _want(_is(W, torch.float32, -1, -1), "W: [N, K] float32 on the GPU")
     N, K = W.shape
     codes, scales = _empty(W, torch.int8, N, K), _empty(W, torch.float16, N, K // max(group, 1))
     calls.gpusq_quantize_groups_int4(W, group, codes, scales, N, K)
@@ -494,25 +504,26 @@ def quantize_groups_int4(W, group):
 
 def pack_int4_groups(codes, scales, group):
     """gpusq_pack_int4_groups: codes [N,K] int8 of -8..7, scales [N,K/group] fp16 -> the operand of linear_int4 (uint8)"""
-    _want(_is(codes, torch.int8, None, None), "codes: [N, K] int8 on the GPU")
+    _want(_is(codes, torch.int8, -1, -1), "codes: [N, K] int8 on the GPU")
     N, K = codes.shape
     _want(_is(scales, torch.float16, N, K // max(group, 1)), "scales: [N, K / group] float16 on the GPU")
-    nbytes = lib().gpusq_int4_groups_packed_bytes(N, K, group)
-    packed = _empty(codes, torch.uint8, max(nbytes, 16))
+    packed = _empty(codes, torch.uint8, max(_size("gpusq_int4_groups_packed_bytes", N, K, group), 16))
     calls.gpusq_pack_int4_groups(codes, scales, group, packed, N, K)
     return packed
 
 
 def linear_int4(X, packed, N, group, bias=None, gelu=False, out_dtype=torch.float16, out=None):
     """gpusq_linear_int4: X [M,K] fp16, packed from pack_int4_groups -> act(X W^T + bias) [M,N] fp16 or fp32"""
-    _want(_is(X, torch.float16, None, None), "X: [M, K] float16 on the GPU")
+    _want(_is(X, torch.float16, -1, -1), "X: [M, K] float16 on the GPU")
     M, K = X.shape
-    _want(_is(packed, torch.uint8, lib().gpusq_int4_groups_packed_bytes(N, K, group) or None), "packed: of other sizes than N, K and group")
+    _want(_is(packed, torch.uint8, _size("gpusq_int4_groups_packed_bytes", N, K, group)), "packed: of other sizes than N, K and group")
     _want(bias is None or _is(bias, torch.float32, N), "bias: [N] float32 on the GPU")
-    Y = _empty(X, out_dtype, M, N) if out is None else out
-    _want(out is None or _is(out, out_dtype, M, N), "out: [M, N] of out_dtype on the GPU")
-    calls.gpusq_linear_int4(X, packed, group, bias, Y, _TORCH_DT[out_dtype], M, N, K, _epi(bias, gelu))
-    return Y
+    if out is None:
+        out = _empty(X, out_dtype, M, N)
+    else:
+        _want(_is(out, out_dtype, M, N), "out: [M, N] of out_dtype on the GPU")
+    calls.gpusq_linear_int4(X, packed, group, bias, out, _TORCH_DT[out_dtype], M, N, K, _epi(bias, gelu))
+    return out
 
 
 def kv4_cache(num_pages, kv_heads, head_dim, device="cuda"):
@@ -523,74 +534,84 @@ def kv4_cache(num_pages, kv_heads, head_dim, device="cuda"):
     return torch.empty((num_pages, kv_heads, nbytes // kv_heads), dtype=torch.uint8, device=device)
 
 
-def _is_cache(cache, kv_heads, head_dim):
-    return _is(cache, torch.uint8, None, kv_heads, (lib().gpusq_kv4_page_bytes(kv_heads, head_dim) // max(kv_heads, 1)) or None)
-
-
 def qk_norm_rope(qkv, heads, kv_heads, head_dim, q_weight=None, k_weight=None, eps=1e-6, norm=True, cos=None, sin=None, positions=None, interleaved=False,
                  cache=None, slots=None, want_cached=False, q_out=None):
     """gpusq_qk_norm_rope: qkv [T, (heads + 2 kv_heads) * head_dim] fp16 or fp32, rows contiguous -> (q [T,heads,head_dim], k [T,kv_heads,head_dim])
     fp16.  With a cache (kv4_cache) keys and values go to slots [T] int32 of it and the result is q, with want_cached (q, k, v): what the
     cache stands for."""
-    _want(qkv.is_cuda and qkv.dtype in (torch.float32, torch.float16) and qkv.dim() == 2 and qkv.shape[1] >= (heads + 2 * kv_heads) * head_dim and qkv.stride(1) == 1,
+    f32, f16 = torch.float32, torch.float16
+    _want((_is(qkv, f16, -1, -1) or _is(qkv, f32, -1, -1)) and qkv.shape[1] >= (heads + 2 * kv_heads) * head_dim and qkv.stride(1) == 1,
           "qkv: [T, (heads + 2 kv_heads) * head_dim] float16 or float32 on the GPU, rows contiguous")
     T, R, rows = qkv.shape[0], 0, 0
-    _want(all(w is None or _is(w, torch.float32, head_dim) for w in (q_weight, k_weight)), "norm weights: [head_dim] float32 on the GPU")
+    _want((q_weight is None or _is(q_weight, f32, head_dim)) and (k_weight is None or _is(k_weight, f32, head_dim)), "norm weights: [head_dim] float32 on the GPU")
     if cos is not None:
-        rows, R = cos.shape[0], 2 * cos.shape[-1]
-        _want(_is(cos, torch.float32, rows, R // 2) and sin is not None and _is(sin, torch.float32, rows, R // 2), "cos, sin: [rows, rot_dim / 2] float32 on the GPU")
-        _want(positions is not None and _is(positions, torch.int32, T), "positions: [T] int32 on the GPU")
-    q = _empty(qkv, torch.float16, T, heads, head_dim) if q_out is None else q_out
-    _want(q_out is None or _is(q_out, torch.float16, T, heads, head_dim), "q_out: [T, heads, head_dim] float16 on the GPU")
+        _want(_is(cos, f32, -1, -1), "cos: [rows, rot_dim / 2] float32 on the GPU")
+        rows, R = cos.shape
+        _want(_is(sin, f32, rows, R) and _is(positions, torch.int32, T), "sin: as cos; positions: [T] int32 on the GPU")
+    if q_out is None:
+        q_out = _empty(qkv, f16, T, heads, head_dim)
+    else:
+        _want(_is(q_out, f16, T, heads, head_dim), "q_out: [T, heads, head_dim] float16 on the GPU")
     k = v = None
+    pages = 0
     if cache is None or want_cached:
-        k = _empty(qkv, torch.float16, T, kv_heads, head_dim)
+        k = _empty(qkv, f16, T, kv_heads, head_dim)
     if cache is not None:
-        _want(_is_cache(cache, kv_heads, head_dim), "cache: of other heads than kv_heads and head_dim")
-        _want(slots is not None and _is(slots, torch.int32, T), "slots: [T] int32 on the GPU")
-        v = _empty(qkv, torch.float16, T, kv_heads, head_dim) if want_cached else None
-    calls.gpusq_qk_norm_rope(qkv, _TORCH_DT[qkv.dtype], qkv.stride(0), T, heads, kv_heads, head_dim, int(norm), q_weight, k_weight, eps, cos, sin, positions, rows, R,
-                             int(interleaved), q, k, v, cache, slots, 0 if cache is None else cache.shape[0])
-    return (q, k) if cache is None else (q, k, v) if want_cached else q
+        _want(_is(cache, torch.uint8, -1, kv_heads, _size("gpusq_kv4_page_bytes", 1, head_dim)), "cache: of other heads than kv_heads and head_dim")
+        _want(_is(slots, torch.int32, T), "slots: [T] int32 on the GPU")
+        pages = cache.shape[0]
+        if want_cached:
+            v = _empty(qkv, f16, T, kv_heads, head_dim)
+    calls.gpusq_qk_norm_rope(qkv, _TORCH_DT[qkv.dtype], qkv.stride(0), T, heads, kv_heads, head_dim, norm, q_weight, k_weight, eps, cos, sin, positions, rows, 2 * R,
+                             interleaved, q_out, k, v, cache, slots, pages)
+    return (q_out, k) if cache is None else (q_out, k, v) if want_cached else q_out
 
 
-def _workspace(like, nbytes):
-    return _empty(like, torch.uint8, nbytes) if nbytes else None
+def _workspace(like, given, nbytes):
+    if given is None:
+        return _empty(like, torch.uint8, nbytes) if nbytes > 0 else None
+    _want(given.numel() * given.element_size() >= nbytes, "workspace: too small")
+    return given
 
 
 def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=1, scale=None, out=None, workspace=None):
     """gpusq_attention_kv4: q [tokens,heads,head_dim] fp16, cache [pages,kv_heads,bytes], block_table [batch,max_pages] int32, kv_lens [batch] int32,
     cu_q [batch + 1] int32 (None: max_q queries each) -> [tokens,heads,head_dim] fp16"""
-    _want(q.is_cuda and q.dtype == torch.float16 and q.dim() == 3, "q: [tokens, heads, head_dim] float16 on the GPU")
+    _want(_is(q, torch.float16, -1, -1, -1), "q: [tokens, heads, head_dim] float16 on the GPU")
     tokens, heads, D = q.shape
-    _want(cache.dim() == 3 and _is_cache(cache, cache.shape[1], D), "cache: of another head_dim than q")
-    _want(_is(block_table, torch.int32, None, None), "block_table: [batch, max_pages] int32 on the GPU")
+    _want(_is(cache, torch.uint8, -1, -1, _size("gpusq_kv4_page_bytes", 1, D)), "cache: pages of kv4_cache of q's head_dim")
+    pages, kv_heads, _ = cache.shape
+    _want(_is(block_table, torch.int32, -1, -1), "block_table: [batch, max_pages] int32 on the GPU")
     batch, max_pages = block_table.shape
     _want(_is(kv_lens, torch.int32, batch), "kv_lens: [batch] int32 on the GPU")
     _want(cu_q is None or _is(cu_q, torch.int32, batch + 1), "cu_q: [batch + 1] int32 on the GPU")
-    o = torch.empty_like(q) if out is None else out
-    _want(out is None or _is(out, torch.float16, tokens, heads, D), "out: [tokens, heads, head_dim] float16 on the GPU")
-    nbytes = lib().gpusq_attention_kv4_workspace_bytes(tokens, batch, max_q, max_pages, heads, cache.shape[1], D)
-    _want(workspace is None or workspace.numel() * workspace.element_size() >= nbytes, "workspace: too small")
-    calls.gpusq_attention_kv4(q, cache, block_table, kv_lens, cu_q, o, _workspace(q, nbytes) if workspace is None else workspace, tokens, batch, max_q, max_pages,
-                              cache.shape[0], heads, cache.shape[1], D, 0.0 if scale is None else scale)
-    return o
+    if out is None:
+        out = _empty(q, torch.float16, tokens, heads, D)
+    else:
+        _want(_is(out, torch.float16, tokens, heads, D), "out: [tokens, heads, head_dim] float16 on the GPU")
+    workspace = _workspace(q, workspace, _size("gpusq_attention_kv4_workspace_bytes", tokens, batch, max_q, max_pages, heads, kv_heads, D))
+    calls.gpusq_attention_kv4(q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, pages, heads, kv_heads, D, 0.0 if scale is None else scale)
+    return out
 
 
 def cross_attention(q, k, v, kv_lens=None, key_mask=None, scale=None, out=None, workspace=None):
     """gpusq_cross_attention: q [batch,q_len,heads,head_dim], k, v [batch,kv_len,kv_heads,head_dim] fp16 with any strides but a head's vector
     contiguous; kv_lens [batch] int32, key_mask [batch,kv_len] uint8 or bool (0: not seen) -> [batch,q_len,heads,head_dim] fp16"""
-    _want(all(t.is_cuda and t.dtype == torch.float16 and t.dim() == 4 and t.stride(3) == 1 for t in (q, k, v)),
-          "q, k, v: four dimensions, float16, on the GPU, the last dimension contiguous")
+    f16 = torch.float16
+    _want(_is(q, f16, -1, -1, -1, -1), "q: [batch, q_len, heads, head_dim] float16 on the GPU")
     B, Tq, H, D = q.shape
-    S, G = k.shape[1], k.shape[2]
-    _want(k.shape == v.shape and k.shape[0] == B and k.shape[3] == D, "k, v: [batch, kv_len, kv_heads, head_dim] of q's batch and head_dim")
+    _want(_is(k, f16, B, -1, -1, D), "k: [batch, kv_len, kv_heads, head_dim] float16 on the GPU, of q's batch and head_dim")
+    _, S, G, _ = k.shape
+    _want(_is(v, f16, B, S, G, D), "v: as k")
+    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    _want(qs[3] == ks[3] == vs[3] == 1, "q, k, v: the last dimension contiguous")
     _want(kv_lens is None or _is(kv_lens, torch.int32, B), "kv_lens: [batch] int32 on the GPU")
     _want(key_mask is None or _is(key_mask, torch.uint8, B, S) or _is(key_mask, torch.bool, B, S), "key_mask: [batch, kv_len] uint8 or bool on the GPU")
-    o = _empty(q, torch.float16, B, Tq, H, D) if out is None else out
-    _want(out is None or _is(out, torch.float16, B, Tq, H, D), "out: [batch, q_len, heads, head_dim] float16 on the GPU")
-    nbytes = lib().gpusq_cross_attention_workspace_bytes(B, Tq, S, H, G, D)
-    _want(workspace is None or workspace.numel() * workspace.element_size() >= nbytes, "workspace: too small")
-    calls.gpusq_cross_attention(q, k, v, kv_lens, key_mask, o, _workspace(q, nbytes) if workspace is None else workspace, B, Tq, S, H, G, D,
-                                *q.stride()[:3], *k.stride()[:3], *v.stride()[:3], 0.0 if scale is None else scale)
-    return o
+    if out is None:
+        out = _empty(q, f16, B, Tq, H, D)
+    else:
+        _want(_is(out, f16, B, Tq, H, D), "out: [batch, q_len, heads, head_dim] float16 on the GPU")
+    workspace = _workspace(q, workspace, _size("gpusq_cross_attention_workspace_bytes", B, Tq, S, H, G, D))
+    calls.gpusq_cross_attention(q, k, v, kv_lens, key_mask, out, workspace, B, Tq, S, H, G, D, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                                0.0 if scale is None else scale)
+    return out
