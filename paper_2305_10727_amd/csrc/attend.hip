@@ -43,15 +43,6 @@ struct AttendArgs {
   float* part_ml;
 };
 
-template <int DP>
-struct Raw4 {  // 32 keys of the cache as they lie
-  static constexpr int J = DP / 32, CH = DP / 16;
-  unsigned kw[2][J];
-  h2 ks[2][J / 2];
-  unsigned vw[2][CH / 2];
-  h4 vs[2];
-};
-
 template <int N>
 __device__ __forceinline__ void load_words(const uint8_t* p, unsigned (&w)[N]) {
   if constexpr (N == 2) {
@@ -68,31 +59,50 @@ __device__ __forceinline__ void load_words(const uint8_t* p, unsigned (&w)[N]) {
   }
 }
 
+// 32 keys of the cache as they lie: codes and scales of keys, of values
 template <int DP>
-__device__ __forceinline__ void load_tile(const uint8_t* page, int half, int g, int r, Raw4<DP>& x) {
-  constexpr int J = DP / 32, CH = DP / 16;
+struct Keys4 {
+  static constexpr int J = DP / 32;
+  unsigned w[2][J];
+  h2 s[2][J / 2];
+  __device__ __forceinline__ void load(const uint8_t* page, int half, int g, int r) {
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int key = half * 32 + t * 16 + r, quad = half * 8 + t * 4 + g;
-    load_words<J>(page + key * (DP / 2) + g * J * 4, x.kw[t]);
-    unsigned s[J / 2];
-    if constexpr (J == 2) s[0] = *(const unsigned*)(page + key_scales_at(DP) + key * J * 2);
-    else load_words<J / 2>(page + key_scales_at(DP) + key * J * 2, s);
+    for (int t = 0; t < 2; ++t) {
+      const int key = half * 32 + t * 16 + r;
+      load_words<J>(page + key * (DP / 2) + g * J * 4, w[t]);
+      unsigned u[J / 2];
+      if constexpr (J == 2) u[0] = *(const unsigned*)(page + key_scales_at(DP) + key * J * 2);
+      else load_words<J / 2>(page + key_scales_at(DP) + key * J * 2, u);
 #pragma unroll
-    for (int i = 0; i < J / 2; ++i) x.ks[t][i] = __builtin_bit_cast(h2, s[i]);
-    load_words<CH / 2>(page + value_codes_at(DP) + (quad * 16 + r) * (2 * CH), x.vw[t]);
-    x.vs[t] = *(const h4*)(page + value_scales_at(DP) + (r * CH / 32 * kPageTokens + quad * 4) * 2);
+      for (int i = 0; i < J / 2; ++i) s[t][i] = __builtin_bit_cast(h2, u[i]);
+    }
   }
-}
+};
+template <int DP>
+struct Values4 {
+  static constexpr int CH = DP / 16;
+  unsigned w[2][CH / 2];
+  h4 s[2];
+  __device__ __forceinline__ void load(const uint8_t* page, int half, int g, int r) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int quad = half * 8 + t * 4 + g;
+      load_words<CH / 2>(page + value_codes_at(DP) + (quad * 16 + r) * (2 * CH), w[t]);
+      s[t] = *(const h4*)(page + value_scales_at(DP) + (r * CH / 32 * kPageTokens + quad * 4) * 2);
+    }
+  }
+};
 
 __device__ __forceinline__ h8 join(h2 a, h2 b, h2 c, h2 d) { return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}; }
+
+constexpr int waves_per_simd(bool kv4, int DP, int QT) { return DP > 128 ? 1 : QT == 1 ? (kv4 || DP == 64 ? 4 : 3) : QT == 2 ? 2 : 1; }
 
 // KV4: over the cache, else fp16 states.  QT: blocks of 16 columns of a wavefront.  WQ x WK wavefronts: WQ have columns of their own, WK
 // deal out the tiles of 32 keys and join their sums in LDS.
 template <bool KV4, int DP, int QT, int WQ, int WK, bool MASKED>
-__global__ void __launch_bounds__(64 * WQ * WK) attend_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(64 * WQ * WK, waves_per_simd(KV4, DP, QT)) attend_kernel(const AttendArgs a) {
   constexpr int J = DP / 32, CH = DP / 16;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
   const int wq = wave / WK, wk = wave % WK;
   // workgroups of one key head run on one XCD, whose L2 then reads its keys and values once
   const int units = a.batch * a.kv_heads, per_unit = a.col_blocks * a.parts;
@@ -210,43 +220,51 @@ __global__ void __launch_bounds__(64 * WQ * WK) attend_kernel(const AttendArgs a
   };
 
   if constexpr (KV4) {
+    // a wavefront takes whole pages: both halves of one, then the next of its own
     const int32_t* table = a.table + (int64_t)b * a.max_pages;
-    auto page_of = [&](int tile, bool& there) {
-      const int page = table[tile >> 1];
-      there = (unsigned)page < (unsigned)a.num_pages;  // (a page that is none: its tokens are not visible)
-      return a.cache + ((int64_t)(there ? page : 0) * a.kv_heads + kh) * page_bytes(DP);
-    };
-    Raw4<DP> next;
-    bool next_there = true;
-    int tile = begin + wk;
-    if (tile < end) load_tile<DP>(page_of(tile, next_there), tile & 1, g, r, next);
-    for (; tile < end; tile += WK) {
-      const Raw4<DP> x = next;
-      const bool there = next_there;
-      if (tile + WK < end) load_tile<DP>(page_of(tile + WK, next_there), (tile + WK) & 1, g, r, next);
+    auto page_at = [&](int number) { return a.cache + ((int64_t)number * a.kv_heads + kh) * page_bytes(DP); };
+    auto after = [&](int tile) { return tile & 1 ? tile + 2 * WK - 1 : tile + 1; };
+    auto page_of = [&](int tile, int otherwise) { return tile < end ? table[tile >> 1] : otherwise; };
+    Keys4<DP> k;
+    Values4<DP> v;
+    int tile = begin + 2 * wk;
+    // page numbers are read a tile ahead of the keys, keys a product ahead; a number that is no page is read as page 0 and not seen
+    int number = page_of(tile, 0), next = page_of(after(tile), 0);
+    bool there = (unsigned)number < (unsigned)a.num_pages;
+    const uint8_t* page = page_at(there ? number : 0);
+    if (tile < end) {
+      k.load(page, 0, g, r);
+      v.load(page, 0, g, r);
+    }
+    while (tile < end) {
       const int key0 = tile * 32;
       f4 s[QT][2] = {};
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-          const h2 sc = {x.ks[t][j / 2][j & 1], x.ks[t][j / 2][j & 1]};
-          h2 k[4];
-          codes_to_halves(x.kw[t][j], sc, sc * (_Float16)-72.0f, k);
-          const h8 ka = join(k[0], k[1], k[2], k[3]);
+          const h2 sc = {k.s[t][j / 2][j & 1], k.s[t][j / 2][j & 1]};
+          h2 c[4];
+          codes_to_halves(k.w[t][j], sc, sc * (_Float16)-72.0f, c);
+          const h8 ka = join(c[0], c[1], c[2], c[3]);
 #pragma unroll
           for (int i = 0; i < QT; ++i) s[i][t] = mfma16(ka, q[i][j], s[i][t]);
         }
-      h4 vs[2] = {x.vs[0], x.vs[1]};
+      const int ahead = after(tile);
+      const bool next_there = (unsigned)next < (unsigned)a.num_pages;
+      const uint8_t* next_page = page_at(next_there ? next : 0);
+      if (ahead < end) k.load(next_page, ahead & 1, g, r);
+      next = page_of(after(ahead), 0);
       const bool check = key0 + 32 > least || !there;
+      h8 p[QT];
+      softmax(s, key0, check, there ? 0xFFu : 0u, p);
+      h4 vs[2] = {v.s[0], v.s[1]};
       if (check) {  // places behind the last token may hold anything: a scale of theirs may be infinite or NaN
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) vs[t][e] = there && key0 + 16 * t + 4 * g + e < len ? vs[t][e] : (_Float16)0.0f;
       }
-      h8 p[QT];
-      softmax(s, key0, check, there ? 0xFFu : 0u, p);
       h2 sc[4], off[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -257,7 +275,7 @@ __global__ void __launch_bounds__(64 * WQ * WK) attend_kernel(const AttendArgs a
       for (int qd = 0; qd < CH / 4; ++qd) {
         h2 d[4][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) codes_to_halves(x.vw[i >> 1][(i & 1) * (CH / 4) + qd], sc[i], off[i], d[i]);
+        for (int i = 0; i < 4; ++i) codes_to_halves(v.w[i >> 1][(i & 1) * (CH / 4) + qd], sc[i], off[i], d[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const h8 va = join(d[0][e], d[1][e], d[2][e], d[3][e]);
@@ -265,6 +283,9 @@ __global__ void __launch_bounds__(64 * WQ * WK) attend_kernel(const AttendArgs a
           for (int i = 0; i < QT; ++i) o[i][4 * qd + e] = mfma16(va, p[i], o[i][4 * qd + e]);
         }
       }
+      if (ahead < end) v.load(next_page, ahead & 1, g, r);
+      tile = ahead;
+      there = next_there;
     }
   } else {
     const _Float16 *kp = a.k + b * a.k_batch + kh * a.k_head + 8 * g, *vp = a.v + b * a.v_batch + kh * a.v_head + CH * r;
@@ -416,26 +437,51 @@ __global__ void __launch_bounds__(64 * WQ * WK) attend_kernel(const AttendArgs a
   }
 }
 
-// Joins the parts of a row: a wavefront for each, its lanes the channels
+// Joins the parts of a row: a workgroup for each.  Its threads read the parts' maxima side by side, then take (channels, share of the
+// parts) each and add the shares up in LDS.
+constexpr int kMostParts = 256;
 __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml, _Float16* __restrict__ out, int rows, int D,
                                                           int parts) {
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (row >= rows) return;
-  float m = -__builtin_inff();
-  for (int p = 0; p < parts; ++p) m = fmaxf(m, part_ml[2 * ((int64_t)p * rows + row)]);
-  const float ref = m == -__builtin_inff() ? 0.0f : m;
-  float l = 0.0f;
-  f4 o = f4(0);
-  for (int p = 0; p < parts; ++p) {
-    const int64_t at = (int64_t)p * rows + row;
-    const float pm = part_ml[2 * at];
-    if (pm == -__builtin_inff()) continue;  // a part without a visible key; its sums may not be there
-    const float f = __builtin_amdgcn_exp2f(pm - ref);
-    l += part_ml[2 * at + 1] * f;
-    if (4 * lane < D) o += *(const f4*)(part_o + at * D + 4 * lane) * f;
+  __shared__ float weight[kMostParts], wave_max[4], wave_sum[4];
+  __shared__ f4 sums[256];
+  const int row = blockIdx.x, tid = threadIdx.x;
+  float m = -__builtin_inff(), l = 0.0f;
+  if (tid < parts) {
+    const float* p = part_ml + 2 * ((int64_t)tid * rows + row);
+    m = p[0];
+    l = p[1];
   }
-  const float f = l == 0.0f ? 0.0f : 1.0f / l;
-  if (4 * lane < D) *(h4*)(out + (int64_t)row * D + 4 * lane) = h4{(_Float16)(o[0] * f), (_Float16)(o[1] * f), (_Float16)(o[2] * f), (_Float16)(o[3] * f)};
+  float top = m;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  if ((tid & 63) == 0) wave_max[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
+  const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - top);  // a part without a visible key: its sums may not be there
+  weight[tid] = f;
+  l *= f;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+  if ((tid & 63) == 0) wave_sum[tid >> 6] = l;
+  __syncthreads();
+  l = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
+  const int quads = D / 4, shares = 256 / quads, share = tid / quads, quad = tid - share * quads;
+  f4 o = f4(0);
+  if (share < shares) {
+#pragma unroll 4
+    for (int p = share; p < parts; p += shares) {
+      const float w = weight[p];
+      const f4 v = *(const f4*)(part_o + ((int64_t)p * rows + row) * D + 4 * quad);
+      if (w != 0.0f) o += v * w;
+    }
+  }
+  sums[tid] = o;
+  __syncthreads();
+  if (tid < quads) {
+    for (int i = 1; i < shares; ++i) o += sums[i * quads + tid];
+    const float r = l == 0.0f ? 0.0f : 1.0f / l;
+    *(h4*)(out + (int64_t)row * D + 4 * tid) = h4{(_Float16)(o[0] * r), (_Float16)(o[1] * r), (_Float16)(o[2] * r), (_Float16)(o[3] * r)};
+  }
 }
 
 template <bool KV4, int DP, int QT, int WQ, int WK>
@@ -471,8 +517,9 @@ void launch_head(const AttendArgs& a, hipStream_t s) {
 AttendParts attend_parts(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t most_keys) {
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
   const int64_t groups = batch * kv_heads * ceil_div(cols, 64);
-  int64_t parts = ceil_div(1024, groups);
+  int64_t parts = ceil_div(256, groups);
   if (parts > ceil_div(tiles, 32)) parts = ceil_div(tiles, 32);
+  if (parts > kMostParts) parts = kMostParts;
   AttendParts p;
   p.tiles = (int)(ceil_div(ceil_div(tiles, parts), 2) * 2);
   p.parts = (int)ceil_div(tiles, p.tiles);
@@ -493,7 +540,7 @@ static gpusq_status run(AttendArgs a, bool kv4, const AttendParts& p, void* work
     DP == 64 ? launch_head<false, 64>(a, s) : DP == 128 ? launch_head<false, 128>(a, s) : launch_head<false, 256>(a, s);
   gpusq_status st = check_launch();
   if (st != GPUSQ_OK || p.parts == 1) return st;
-  join_parts_kernel<<<(unsigned)ceil_div(rows, 4), 256, 0, s>>>(a.part_o, a.part_ml, a.out, (int)rows, a.D, p.parts);
+  join_parts_kernel<<<(unsigned)rows, 256, 0, s>>>(a.part_o, a.part_ml, a.out, (int)rows, a.D, p.parts);
   return check_launch();
 }
 
