@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgpusq.so")
 SOURCES = ["api.hip", "prep.hip", "int4.hip", "spgemm.hip", "fewrows.hip", "wide.hip", "mlp.hip", "patches.hip", "tile1_i8.hip", "tile1_f16.hip",
-           "tile1_i8_ragged.hip", "tile1_f16_ragged.hip", "tile2.hip", "dense.hip", "api_decoder.hip", "linear4.hip", "qk_norm.hip", "attend.hip"]
+           "tile1_i8_ragged.hip", "tile1_f16_ragged.hip", "tile2.hip", "dense.hip", "api_decoder.hip", "linear4.hip", "qk_norm.hip", "attend.hip", "attend_tiles.hip"]
 # Python's side of the binding: a host-only extension module beside the library (no GPU code, so the host compiler)
 FASTCALL = os.path.join(HERE, "_fastcall" + sysconfig.get_config_var("EXT_SUFFIX"))
 FLAGS = [

@@ -1,0 +1,213 @@
+// What the kernels of attention share: their arguments, the running softmax, the columns and the output of a wavefront.
+//
+//   o[q] = sum_j exp(s_qj - m_q) v_j / sum_j exp(s_qj - m_q),  s_qj = scale q . k_j,  m_q the largest visible s_qj;  0 where none is visible
+//
+// One pass over the keys with the running maximum and sum of the softmax; scores never leave the registers.  A wavefront takes 32 keys
+// at a time.  The first product is turned over, scores^T = K Q^T, so that a lane of the result has one query (column lane % 16) and the
+// keys 4 g .. + 3 (g = lane / 16) of either 16: these are, as they lie, the second operand of output^T = V^T P^T, if V^T's k runs over
+// the same keys in the same order.  Nothing crosses lanes between the products.
+// Queries of the heads that share a key head are columns side by side: column = token * (heads per key head) + head.
+//
+// The maximum moves only when a score passes it by 2^8 (kSlack): p = 2^(s - m + 6) then lies in fp16 up to 2^14, and down to 2^-24,
+// that is to 2^-30 of the largest where it has not moved.  Most tiles need neither the maximum across lanes nor a rescaled sum.
+// P is rounded to fp16 for the matrix instruction (the one rounding between the scores and the output); its sum is that of the rounded
+// values, in 32 bits, one matrix instruction with a first operand of ones instead of 8 additions a lane.
+#pragma once
+#include "kv4.h"
+
+namespace gpusq {
+
+constexpr float kLog2e = 1.4426950408889634f, kShift = 6.0f, kSlack = 8.0f;
+
+struct AttendArgs {
+  const _Float16* q;
+  _Float16* out;
+  int64_t q_batch, q_token, q_head;  // in values
+  int64_t o_token;                   // out: [token][heads][D]
+  int heads, kv_heads, rep, D, batch, q_len;
+  float c;  // scale * log2(e)
+  // over the cache
+  const uint8_t* cache;
+  const int32_t *table, *cu_q;
+  int max_pages, num_pages, tokens;
+  // over fp16 states
+  const _Float16 *k, *v;
+  int64_t k_batch, k_token, k_head, v_batch, v_token, v_head;
+  const uint8_t* mask;
+  int kv_len;
+  const int32_t* lens;
+  // work: column blocks of a (batch, key head), parts of its keys
+  int col_blocks, parts, part_tiles;
+  float* part_o;   // [part][row][D] sums, [part][row][2] maximum and sum
+  float* part_ml;
+};
+
+__device__ __forceinline__ h8 join(h2 a, h2 b, h2 c, h2 d) { return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}; }
+
+// What a workgroup works on: part of the keys of a (batch, key head) and a block of its columns.  Blocks of the same keys run on one XCD, whose
+// L2 then reads these once: many keys are dealt out over the XCDs in turn (batches are of different lengths), few in equal shares.
+struct Work {
+  int b, kh, part, block;
+  __device__ __forceinline__ bool find(const AttendArgs& a) {
+    const int units = a.batch * a.kv_heads * a.parts, xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    int unit;
+    if (units >= kManyUnits) {
+      block = local % a.col_blocks;
+      unit = local / a.col_blocks * 8 + xcd;
+      if (unit >= units) return false;
+    } else {
+      const int total = units * a.col_blocks, per_xcd = (total + 7) >> 3, at = xcd * per_xcd + local;
+      if (local >= per_xcd || at >= total) return false;
+      block = at % a.col_blocks;
+      unit = at / a.col_blocks;
+    }
+    part = unit % a.parts;
+    b = unit / a.parts / a.kv_heads;
+    kh = unit / a.parts % a.kv_heads;
+    return true;
+  }
+  static constexpr int kManyUnits = 64;
+  static unsigned workgroups(const AttendArgs& a) {
+    const int64_t units = (int64_t)a.batch * a.kv_heads * a.parts;
+    return (unsigned)(units >= kManyUnits ? ceil_div(units, 8) * 8 * a.col_blocks : ceil_div(units * a.col_blocks, 8) * 8);
+  }
+};
+
+// The tokens of a batch's queries, the keys that it has
+template <bool KV4>
+struct Span {
+  int t0, nq, len;
+  int64_t q_base;
+  __device__ __forceinline__ Span(const AttendArgs& a, int b) : t0(b * a.q_len), nq(a.q_len) {
+    if constexpr (KV4) {
+      if (a.cu_q != nullptr) {
+        t0 = a.cu_q[b];
+        const int t1 = a.cu_q[b + 1];
+        nq = t0 >= 0 && t1 <= a.tokens && t1 > t0 ? (t1 - t0 < a.q_len ? t1 - t0 : a.q_len) : 0;
+      }
+      q_base = (int64_t)t0 * a.q_token;
+      const int most = a.max_pages * kPageTokens;
+      len = a.lens[b];
+      len = len < 0 ? 0 : len < most ? len : most;
+    } else {
+      q_base = b * a.q_batch;
+      len = a.kv_len;
+      if (a.lens != nullptr) {
+        const int l = a.lens[b];
+        len = l < 0 ? 0 : l < len ? l : len;
+      }
+    }
+  }
+  // keys that the query of token `tok` sees
+  __device__ __forceinline__ int sees(int tok) const {
+    const int limit = KV4 ? len - nq + tok + 1 : len;
+    return limit < len ? limit : len;
+  }
+};
+
+// QT blocks of 16 columns of a wavefront
+template <bool KV4, int DP, int QT>
+struct Columns {
+  static constexpr int J = DP / 32, CH = DP / 16;
+  h8 q[QT][J];
+  int limit[QT], row[QT];  // keys that this lane's column sees; its row of the output, or -1
+  f4 o[QT][CH], l[QT];
+  float m[QT];
+
+  // block i begins at column first(i)
+  template <class First>
+  __device__ __forceinline__ void load(const AttendArgs& a, const Span<KV4>& span, int kh, int g, int r, First first) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const int col = first(i) + r, tok = col / a.rep, head = kh * a.rep + (col - tok * a.rep);
+      const bool in = col < span.nq * a.rep;
+      row[i] = in ? (span.t0 + tok) * a.heads + head : -1;
+      limit[i] = span.sees(tok);
+      const _Float16* p = a.q + span.q_base + tok * a.q_token + head * a.q_head;
+#pragma unroll
+      for (int j = 0; j < J; ++j) q[i][j] = in && 32 * j + 8 * g < a.D ? *(const h8*)(p + 32 * j + 8 * g) : h8(0);
+      m[i] = -__builtin_inff();
+      l[i] = f4(0);
+#pragma unroll
+      for (int t = 0; t < CH; ++t) o[i][t] = f4(0);
+    }
+  }
+
+  // Scores^T of 32 keys to p^T.  hidden(i, t, e): whether block i's column of this lane does not see key 16 t + 4 g + e; asked if `check`.
+  template <class Hidden>
+  __device__ __forceinline__ void softmax(f4 (&s)[QT][2], float c, bool check, Hidden hidden, h8 (&p)[QT]) {
+    if (check) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i][t][e] = hidden(i, t, e) ? -__builtin_inff() : s[i][t][e];
+    }
+    float top[QT];
+    bool moves = false;
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])), fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) * c;
+      moves |= top[i] > m[i] + kSlack;
+    }
+    if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        float n = fmaxf(top[i], __shfl_xor(top[i], 16));
+        n = fmaxf(n, __shfl_xor(n, 32));
+        n = fmaxf(n, m[i]);
+        const float f = m[i] == n ? 1.0f : __builtin_amdgcn_exp2f(m[i] - n);  // (-inf by -inf: nothing there to scale)
+        m[i] = n;
+        l[i] *= f;
+#pragma unroll
+        for (int t = 0; t < CH; ++t) o[i][t] *= f;
+      }
+    }
+    const _Float16 u = (_Float16)1.0f;
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const float off = kShift - (m[i] == -__builtin_inff() ? 0.0f : m[i]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[i][4 * t + e] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i][t][e], c, off));
+      l[i] = mfma16(h8{u, u, u, u, u, u, u, u}, p[i], l[i]);
+    }
+  }
+
+  // Lane 16 g + r has channel(t, e) of its column in o[.][t][e]; four in a row over e (or over t, where they are apart over e).
+  template <class Channel>
+  __device__ __forceinline__ void store(const AttendArgs& a, int part, Channel channel, int g) const {
+    const bool over_e = channel(0, 1) == channel(0, 0) + 1;
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      if (row[i] < 0) continue;
+      const int64_t at = (int64_t)part * a.tokens * a.heads + row[i];
+      const float f = a.parts > 1 ? 1.0f : l[i][0] == 0.0f ? 0.0f : 1.0f / l[i][0];
+      if (a.parts > 1 && g == 0) {
+        a.part_ml[2 * at] = m[i];
+        a.part_ml[2 * at + 1] = l[i][0];
+      }
+#pragma unroll
+      for (int n = 0; n < CH; ++n) {
+        const int t = over_e ? n : n / 4 * 4, e = over_e ? 0 : n % 4, c = channel(t, e);
+        const f4 v = over_e ? o[i][t] : f4{o[i][t][e], o[i][t + 1][e], o[i][t + 2][e], o[i][t + 3][e]};
+        if (c >= a.D) continue;
+        if (a.parts > 1)
+          *(f4*)(a.part_o + at * a.D + c) = v;
+        else
+          *(h4*)(a.out + (int64_t)row[i] * a.D + c) = h4{(_Float16)(v[0] * f), (_Float16)(v[1] * f), (_Float16)(v[2] * f), (_Float16)(v[3] * f)};
+      }
+    }
+  }
+};
+
+// the kernel for many columns (attend_tiles.hip), and how many a workgroup takes
+constexpr int kFewColumns = 32;
+// (a tile of 64 tokens in 32-bit offsets)
+inline bool tiles_reach(bool kv4, const AttendArgs& a) { return kv4 || (a.k_token < (1 << 24) && a.v_token < (1 << 24)); }
+constexpr int tiles_columns(int DP) { return DP > 128 ? 64 : 128; }
+void launch_attend_tiles(bool kv4, AttendArgs a, hipStream_t s);
+
+}  // namespace gpusq

@@ -1,0 +1,263 @@
+// Attention of many queries (a prompt's chunk over the cache, an image's tokens to its own or another's states): the kernel whose bound is
+// arithmetic.  A workgroup's wavefronts have columns of their own and share the keys: keys and values go through LDS a tile at a time, in rows
+// as they lie in memory, with the 16-byte pieces of a row in places that differ from row to row (place()), so that neither the 16 rows of a
+// key operand nor the transposed reads of a value operand meet in a bank.  Two buffers: while one is multiplied the other is filled.
+//   fp16 states go from memory to LDS directly; the cache's codes become fp16 numbers on the way, once for all the workgroup's columns.
+#include "attend.h"
+#include "tile_common.h"
+
+namespace gpusq {
+
+namespace {
+
+// Where a row keeps its 16-byte piece c: rows that a wavefront reads together have the same piece in different banks.  (16 rows of 256 bytes
+// or 8 pairs of rows of 128.)
+template <int DP>
+__device__ __forceinline__ int place(int row, int c) {
+  return DP == 64 ? c ^ ((row >> 1) & 7) : c ^ (row & 15);
+}
+template <int DP>
+constexpr int kRow = 2 * DP;  // bytes
+
+// Four keys of a value operand: lane 16 g + r reads 8 bytes of row 4 g + r / 4 and gets channel r of the four rows
+__device__ __forceinline__ h4 read_transposed(const uint8_t* p) {
+  typedef __fp16 t4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) t4 lds_t4;
+  return __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_t4*)p));
+}
+
+// ---- fp16 states on their way: memory to LDS, 1 KB a wavefront and instruction -----------------------------------------------------------
+template <int DP, int KT, int NW>
+struct States {
+  static constexpr int PIECES = DP / 8, ROWS = 64 / PIECES;          // pieces of a row, rows of an instruction
+  static constexpr int COPIES = KT / (ROWS * NW);                    // instructions of a wavefront, for keys and for values
+  static_assert(COPIES * ROWS * NW == KT, "whole instructions");
+  const uint8_t *kp, *vp;
+  int64_t k_row, v_row;  // bytes
+  uint32_t lds;
+  int row[COPIES], piece[COPIES], len, D2;
+
+  __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles)
+      : kp((const uint8_t*)(a.k + w.b * a.k_batch + w.kh * a.k_head)), vp((const uint8_t*)(a.v + w.b * a.v_batch + w.kh * a.v_head)), k_row(2 * a.k_token), v_row(2 * a.v_token),
+        lds(lds_address(tiles) + wave * COPIES * 1024), len(len_), D2(2 * a.D) {
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+      row[i] = (wave * COPIES + i) * ROWS + lane / PIECES;
+      piece[i] = 16 * place<DP>(row[i], lane % PIECES);
+    }
+  }
+  // Rows from `len` on are its last row once more (finite where that is), pieces beyond the head are left out.
+  __device__ __forceinline__ void load(int buf, int key0) const {
+    const uint8_t *k = kp + key0 * k_row, *v = vp + key0 * v_row;
+    const int last = len - 1 - key0;
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) {
+      const unsigned r = row[i] < last ? row[i] : last;
+      const uint32_t at = lds + buf * (2 * KT * kRow<DP>) + i * 1024;
+      if (piece[i] < D2) {
+        copy16_to_lds(k, r * (unsigned)k_row + piece[i], at);
+        copy16_to_lds(v, r * (unsigned)v_row + piece[i], at + KT * kRow<DP>);
+      }
+    }
+  }
+};
+
+// ---- the cache's codes on their way -----------------------------------------------------------------------------------------------------
+// KT = 64: a page.  Wavefront w has keys 16 w .. + 15: lane 16 g + r pieces 4 j + g of key r, and channels CH r .. of the quad of values 4 w + g.
+template <int DP>
+struct Codes {
+  static constexpr int J = DP / 32, CH = DP / 16;
+  unsigned kw[J], vw[CH / 2], vs[2];
+  h2 ks[J / 2];
+  const uint8_t* cache;
+  const int32_t* table;
+  int len, num_pages, kv_heads, kh, wave, lane;
+  bool there;
+
+  __device__ __forceinline__ Codes(const AttendArgs& a, const Work& w, int len_, int wave_, int lane_)
+      : cache(a.cache), table(a.table + (int64_t)w.b * a.max_pages), len(len_), num_pages(a.num_pages), kv_heads(a.kv_heads), kh(w.kh), wave(wave_), lane(lane_), there(false) {}
+
+  __device__ __forceinline__ void load(int key0) {
+    const int number = table[key0 >> 6];
+    there = (unsigned)number < (unsigned)num_pages;  // (a number that is no page is read as page 0, and not seen)
+    const uint8_t* page = cache + ((int64_t)(there ? number : 0) * kv_heads + kh) * page_bytes(DP);
+    const int g = lane >> 4, r = lane & 15, key = wave * 16 + r, quad = wave * 4 + g;
+    load_words<J>(page + key * (DP / 2) + g * J * 4, kw);
+    unsigned u[J / 2];
+    if constexpr (J == 2) u[0] = *(const unsigned*)(page + key_scales_at(DP) + key * J * 2);
+    else load_words<J / 2>(page + key_scales_at(DP) + key * J * 2, u);
+#pragma unroll
+    for (int i = 0; i < J / 2; ++i) ks[i] = __builtin_bit_cast(h2, u[i]);
+    load_words<CH / 2>(page + value_codes_at(DP) + (quad * 16 + r) * (2 * CH), vw);
+    load_words<2>(page + value_scales_at(DP) + (r * CH / 32 * kPageTokens + quad * 4) * 2, vs);
+    if (!there || key0 + 64 > len) scales_in_front(vs, there ? len - (key0 + quad * 4) : 0);
+  }
+  __device__ __forceinline__ void write(uint8_t* keys, uint8_t* values) const {
+    const int g = lane >> 4, r = lane & 15;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const h2 sc = {ks[j / 2][j & 1], ks[j / 2][j & 1]};
+      h2 c[4];
+      codes_to_halves(kw[j], sc, sc * (_Float16)-72.0f, c);
+      *(h8*)(keys + (wave * 16 + r) * kRow<DP> + place<DP>(r, 4 * j + g) * 16) = join(c[0], c[1], c[2], c[3]);
+    }
+    const h2 s0 = __builtin_bit_cast(h2, vs[0]), s1 = __builtin_bit_cast(h2, vs[1]), off0 = s0 * (_Float16)-72.0f, off1 = s1 * (_Float16)-72.0f;
+#pragma unroll
+    for (int qd = 0; qd < CH / 4; ++qd) {
+      h2 c0[4], c1[4];
+      codes_to_halves(vw[qd], s0, off0, c0);
+      codes_to_halves(vw[CH / 4 + qd], s1, off1, c1);
+      const int piece = (CH * r + 4 * qd) >> 3, half = CH == 4 ? r & 1 : qd & 1;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const h2(&c)[4] = e < 2 ? c0 : c1;
+        const int token = 4 * g + e;
+        *(h4*)(values + (wave * 16 + token) * kRow<DP> + place<DP>(token, piece) * 16 + half * 8) = h4{c[0][e & 1], c[1][e & 1], c[2][e & 1], c[3][e & 1]};
+      }
+    }
+  }
+};
+
+constexpr int tile_waves_per_simd(int DP, int QT) { return DP > 128 ? 1 : DP / 64 * QT <= 4 ? 2 : 1; }
+
+template <bool KV4, int DP, int QT, int NW, int KT, bool MASKED>
+__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP, QT)) attend_tiles_kernel(const AttendArgs a) {
+  static_assert(!KV4 || (KT == 64 && NW == 4), "a page, 16 keys a wavefront");
+  constexpr int J = DP / 32, CH = DP / 16, NT = 64 * NW, kTile = KT * kRow<DP>;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * 2 * kTile];  // [buffer][keys, values]
+  __shared__ __attribute__((aligned(4))) uint8_t seen[MASKED ? KT : 4];
+  __shared__ int pages[2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
+  Work w;
+  if (!w.find(a)) return;
+  const Span<KV4> span(a, w.b);
+  // blocks of 16 columns, dealt out evenly over the workgroups that they need and then over the wavefronts
+  const int cols = span.nq * a.rep, col_tiles = (cols + 15) >> 4, groups = (col_tiles + NW * QT - 1) / (NW * QT);
+  if (w.block >= groups) return;
+  const int tile0 = w.block * col_tiles / groups, tile1 = (w.block + 1) * col_tiles / groups;
+  Columns<KV4, DP, QT> x;
+  // (block i of a wavefront beyond the workgroup's last: columns that are no columns)
+  x.load(a, span, w.kh, g, r, [&](int i) { return tile0 + wave + NW * i < tile1 ? 16 * (tile0 + wave + NW * i) : cols; });
+  const bool works = tile0 + wave < tile1;
+  const int least = span.sees(16 * (tile0 + wave) / a.rep);
+  const int last = 16 * tile1 < cols ? 16 * tile1 - 1 : cols - 1;
+  const int most = span.sees(last / a.rep);
+  const int first_key = w.part * a.part_tiles * 32, end_key = first_key + a.part_tiles * 32 < most ? first_key + a.part_tiles * 32 : most;
+
+  // this lane's key operands and value operands: pieces by their places
+  int key_at[J], value_at[CH];
+#pragma unroll
+  for (int j = 0; j < J; ++j) key_at[j] = r * kRow<DP> + place<DP>(r, 4 * j + g) * 16;
+#pragma unroll
+  for (int t = 0; t < CH; ++t) {
+    const int row = 4 * g + (r >> 2);
+    value_at[t] = kTile + row * kRow<DP> + place<DP>(row, 2 * t + (r >> 1 & 1)) * 16 + (r & 1) * 8;
+  }
+
+  auto multiply = [&](int buf, int key0, bool there) {
+    const uint8_t* tile = lds + buf * 2 * kTile;
+#pragma unroll
+    for (int half = 0; half < KT / 32; ++half) {
+      f4 s[QT][2] = {};
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+          const h8 k = *(const h8*)(tile + key_at[j] + (2 * half + t) * 16 * kRow<DP>);
+#pragma unroll
+          for (int i = 0; i < QT; ++i) s[i][t] = mfma16(k, x.q[i][j], s[i][t]);
+        }
+      h8 p[QT];
+      const int at = key0 + 32 * half + 4 * g;
+      unsigned shown[2] = {~0u, ~0u};
+      if constexpr (MASKED) {
+        shown[0] = *(const unsigned*)&seen[32 * half + 4 * g];
+        shown[1] = *(const unsigned*)&seen[32 * half + 16 + 4 * g];
+      }
+      x.softmax(s, a.c, MASKED || !there || key0 + 32 * half + 32 > least,
+                [&](int i, int t, int e) { return (shown[t] >> (8 * e) & 1) == 0 || at + 16 * t + e >= (there ? x.limit[i] : 0); }, p);
+#pragma unroll
+      for (int t = 0; t < CH; ++t) {
+        const h4 v0 = read_transposed(tile + value_at[t] + 32 * half * kRow<DP>), v1 = read_transposed(tile + value_at[t] + (32 * half + 16) * kRow<DP>);
+        const h8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) x.o[i][t] = mfma16(v, p[i], x.o[i][t]);
+      }
+    }
+  };
+
+  if constexpr (KV4) {
+    Codes<DP> stage(a, w, span.len, wave, lane);
+    auto put = [&](int buf) {
+      stage.write(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile);
+      if (threadIdx.x == 0) pages[buf] = stage.there;
+    };
+    if (first_key < end_key) {
+      stage.load(first_key);
+      put(0);
+      if (first_key + KT < end_key) stage.load(first_key + KT);
+    }
+    int buf = 0;
+    for (int key0 = first_key; key0 < end_key; key0 += KT) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (loads for registers stay in flight)
+      if (works) multiply(buf, key0, pages[buf] != 0);
+      if (key0 + KT < end_key) {
+        put(buf ^ 1);
+        if (key0 + 2 * KT < end_key) stage.load(key0 + 2 * KT);
+      }
+      buf ^= 1;
+    }
+  } else {
+    const States<DP, KT, NW> stage(a, w, span.len, wave, lane, lds);
+    if (a.D < DP) {  // the pieces beyond the head: zeros, once
+      for (int i = threadIdx.x; i < 4 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
+      __syncthreads();
+    }
+    if (first_key < end_key) stage.load(0, first_key);
+    int buf = 0;
+    for (int key0 = first_key; key0 < end_key; key0 += KT) {
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // this tile is there, and nobody reads the other buffer
+      if (key0 + KT < end_key) stage.load(buf ^ 1, key0 + KT);
+      if constexpr (MASKED) {
+        // what is not seen may hold anything: 0 times it would not be 0
+        uint8_t* values = lds + buf * 2 * kTile + kTile;
+        const uint8_t* mask = a.mask + (int64_t)w.b * a.kv_len;
+        for (int i = threadIdx.x; i < KT * DP / 8; i += NT) {
+          const int row = i / (DP / 8);
+          const bool see = key0 + row < span.len && mask[key0 + row] != 0;
+          if (!see) *(u4*)(values + i * 16) = u4(0);
+          if (i % (DP / 8) == 0) seen[row] = see;
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      }
+      if (works) multiply(buf, key0, true);
+      buf ^= 1;
+    }
+  }
+  if (works) x.store(a, w.part, [&](int t, int e) { return 16 * t + 4 * g + e; }, g);
+}
+
+template <bool KV4, int DP, int QT, int NW, int KT>
+void launch_shape(AttendArgs a, hipStream_t s) {
+  a.col_blocks = (int)ceil_div((int64_t)a.q_len * a.rep, 16 * QT * NW);
+  const unsigned blocks = Work::workgroups(a);
+  if constexpr (!KV4) {
+    if (a.mask != nullptr) {
+      attend_tiles_kernel<KV4, DP, QT, NW, KT, true><<<blocks, 64 * NW, 0, s>>>(a);
+      return;
+    }
+  }
+  attend_tiles_kernel<KV4, DP, QT, NW, KT, false><<<blocks, 64 * NW, 0, s>>>(a);
+}
+
+}  // namespace
+
+void launch_attend_tiles(bool kv4, AttendArgs a, hipStream_t s) {
+  const int DP = padded_head(a.D);
+  if (kv4)
+    DP == 64 ? launch_shape<true, 64, 2, 4, 64>(a, s) : DP == 128 ? launch_shape<true, 128, 2, 4, 64>(a, s) : launch_shape<true, 256, 1, 4, 64>(a, s);
+  else
+    DP == 64 ? launch_shape<false, 64, 2, 4, 64>(a, s) : DP == 128 ? launch_shape<false, 128, 2, 4, 64>(a, s) : launch_shape<false, 256, 1, 4, 64>(a, s);
+}
+
+}  // namespace gpusq

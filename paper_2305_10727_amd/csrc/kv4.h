@@ -59,6 +59,30 @@ __device__ __forceinline__ void codes_to_halves(unsigned w, h2 (&out)[4]) {
   out[3] = __builtin_bit_cast(h2, nibbles_at_4(w >> 8)) + m72;
 }
 
+// N words, in vectors of up to four
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, unsigned (&w)[N]) {
+  if constexpr (N == 2) {
+    const u2 v = *(const u2*)p;
+    w[0] = v[0];
+    w[1] = v[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const u4 v = *(const u4*)(p + 4 * i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[i + j] = v[j];
+    }
+  }
+}
+
+// Scales of four tokens as two pairs; those of tokens from `left` on are 0 (places behind the last token may hold anything: a scale of
+// theirs may be infinite or NaN, and 0 times it too).
+__device__ __forceinline__ void scales_in_front(unsigned (&s)[2], int left) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) s[i] &= left > 2 * i + 1 ? 0xFFFFFFFFu : left > 2 * i ? 0xFFFFu : 0u;
+}
+
 // v_mfma_f32_16x16x32_f16: lane 16 g + r has row (column) r and k = 8 g .. + 7 of the operands, column r and rows 4 g .. + 3 of the result
 __device__ __forceinline__ f4 mfma16(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
