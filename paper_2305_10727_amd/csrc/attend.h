@@ -51,7 +51,7 @@ struct Work {
   __device__ __forceinline__ bool find(const AttendArgs& a) {
     const int units = a.batch * a.kv_heads * a.parts, xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
     int unit;
-    if (units >= kManyUnits) {
+    if (in_turn(units)) {
       block = local % a.col_blocks;
       unit = local / a.col_blocks * 8 + xcd;
       if (unit >= units) return false;
@@ -66,10 +66,10 @@ struct Work {
     kh = unit / a.parts % a.kv_heads;
     return true;
   }
-  static constexpr int kManyUnits = 64;
+  static __host__ __device__ __forceinline__ bool in_turn(int64_t units) { return units >= 64 || units % 8 == 0; }
   static unsigned workgroups(const AttendArgs& a) {
     const int64_t units = (int64_t)a.batch * a.kv_heads * a.parts;
-    return (unsigned)(units >= kManyUnits ? ceil_div(units, 8) * 8 * a.col_blocks : ceil_div(units * a.col_blocks, 8) * 8);
+    return (unsigned)(in_turn(units) ? ceil_div(units, 8) * 8 * a.col_blocks : ceil_div(units * a.col_blocks, 8) * 8);
   }
 };
 
@@ -119,7 +119,7 @@ struct Columns {
   __device__ __forceinline__ void load(const AttendArgs& a, const Span<KV4>& span, int kh, int g, int r, First first) {
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-      const int col = first(i) + r, tok = col / a.rep, head = kh * a.rep + (col - tok * a.rep);
+      const int col = first(i) + r, tok = a.rep == 1 ? col : col / a.rep, head = kh * a.rep + (col - tok * a.rep);
       const bool in = col < span.nq * a.rep;
       row[i] = in ? (span.t0 + tok) * a.heads + head : -1;
       limit[i] = span.sees(tok);
@@ -133,17 +133,20 @@ struct Columns {
     }
   }
 
-  // Scores^T of 32 keys to p^T.  hidden(i, t, e): whether block i's column of this lane does not see key 16 t + 4 g + e; asked if `check`.
+  // Scores^T of 32 keys to p^T, in three steps.  hidden(i, t, e): whether block i's column of this lane does not see key 16 t + 4 g + e
   template <class Hidden>
-  __device__ __forceinline__ void softmax(f4 (&s)[QT][2], float c, bool check, Hidden hidden, h8 (&p)[QT]) {
-    if (check) {
+  __device__ __forceinline__ void hide(f4 (&s)[QT][2], Hidden hidden) const {
 #pragma unroll
-      for (int i = 0; i < QT; ++i)
+    for (int i = 0; i < QT; ++i)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[i][t][e] = hidden(i, t, e) ? -__builtin_inff() : s[i][t][e];
-    }
+        for (int e = 0; e < 4; ++e) s[i][t][e] = hidden(i, t, e) ? -__builtin_inff() : s[i][t][e];
+  }
+  // Moves the maxima if a score passes one by kSlack, and rescales the sums, and weights p that are not in them yet (they become 2^-8 of what
+  // they were, or less, so that their second rounding is of no weight).
+  template <bool PENDING>
+  __device__ __forceinline__ void follow(const f4 (&s)[QT][2], float c, h8 (&p)[QT]) {
     float top[QT];
     bool moves = false;
 #pragma unroll
@@ -151,7 +154,7 @@ struct Columns {
       top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])), fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) * c;
       moves |= top[i] > m[i] + kSlack;
     }
-    if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(moves) != 0, 0)) {
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
         float n = fmaxf(top[i], __shfl_xor(top[i], 16));
@@ -162,9 +165,14 @@ struct Columns {
         l[i] *= f;
 #pragma unroll
         for (int t = 0; t < CH; ++t) o[i][t] *= f;
+        if constexpr (PENDING) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[i][e] = (_Float16)((float)p[i][e] * f);
+        }
       }
     }
-    const _Float16 u = (_Float16)1.0f;
+  }
+  __device__ __forceinline__ void weights(const f4 (&s)[QT][2], float c, h8 (&p)[QT]) const {
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
       const float off = kShift - (m[i] == -__builtin_inff() ? 0.0f : m[i]);
@@ -172,8 +180,12 @@ struct Columns {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[i][4 * t + e] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i][t][e], c, off));
-      l[i] = mfma16(h8{u, u, u, u, u, u, u, u}, p[i], l[i]);
     }
+  }
+  __device__ __forceinline__ void sum(const h8 (&p)[QT]) {
+    const _Float16 u = (_Float16)1.0f;
+#pragma unroll
+    for (int i = 0; i < QT; ++i) l[i] = mfma16(h8{u, u, u, u, u, u, u, u}, p[i], l[i]);
   }
 
   // Lane 16 g + r has channel(t, e) of its column in o[.][t][e]; four in a row over e (or over t, where they are apart over e).

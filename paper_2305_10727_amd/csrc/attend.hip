@@ -2,7 +2,6 @@
 // states (cross_attention).  A workgroup's wavefronts have the same columns and deal out the keys: what bounds such a call is the keys'
 // bytes, so they go from memory straight into the registers of the one wavefront that multiplies them.
 #include "attend.h"
-#include <stdlib.h>
 
 namespace gpusq {
 
@@ -99,7 +98,10 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       next = page_of(after(ahead));
       const bool check = key0 + 32 > least || !there;
       h8 p[QT];
-      x.softmax(s, a.c, check, [&](int i, int t, int e) { return key0 + 16 * t + 4 * g + e >= (there ? x.limit[i] : 0); }, p);
+      if (check) x.hide(s, [&](int i, int t, int e) { return key0 + 16 * t + 4 * g + e >= (there ? x.limit[i] : 0); });
+      x.template follow<false>(s, a.c, p);
+      x.weights(s, a.c, p);
+      x.sum(p);
       if (check) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) scales_in_front(v.s[t], there ? len - (key0 + 16 * t + 4 * g) : 0);
@@ -178,7 +180,10 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
           for (int i = 0; i < QT; ++i) s[i][t] = mfma16(k[t][j], x.q[i][j], s[i][t]);
       if (tile + WK < end) load_k((tile + WK) * 32);
       h8 p[QT];
-      x.softmax(s, a.c, MASKED || key0 + 32 > len, [&](int, int t, int e) { return ((vis >> (4 * t + e)) & 1) == 0 || key0 + 16 * t + 4 * g + e >= len; }, p);
+      if (MASKED || key0 + 32 > len) x.hide(s, [&](int, int t, int e) { return ((vis >> (4 * t + e)) & 1) == 0 || key0 + 16 * t + 4 * g + e >= len; });
+      x.template follow<false>(s, a.c, p);
+      x.weights(s, a.c, p);
+      x.sum(p);
 #pragma unroll
       for (int h = 0; h < CH / VW; ++h)
 #pragma unroll
@@ -290,6 +295,31 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict
   }
 }
 
+// Few parts: a thread for four channels of a row
+constexpr int kFewParts = 16;
+__global__ void __launch_bounds__(256) join_few_parts_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml, _Float16* __restrict__ out, int64_t rows,
+                                                              int D, int parts) {
+  const int quads = D / 4, at = threadIdx.x / quads, quad = threadIdx.x - at * quads;
+  const int64_t row = (int64_t)blockIdx.x * (256 / quads) + at;
+  if (at >= 256 / quads || row >= rows) return;
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  float top = -__builtin_inff();
+  for (int p = 0; p < parts; ++p) top = fmaxf(top, part_ml[2 * (p * rows + row)]);
+  float l = 0.0f;
+  f4 o = f4(0);
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const f2 ml = *(const f2*)(part_ml + 2 * (p * rows + row));
+    const f4 v = *(const f4*)(part_o + (p * rows + row) * D + 4 * quad);
+    if (ml[0] == -__builtin_inff()) continue;  // without a visible key: its sums may not be there
+    const float f = __builtin_amdgcn_exp2f(ml[0] - top);
+    l += ml[1] * f;
+    o += v * f;
+  }
+  const float r = l == 0.0f ? 0.0f : 1.0f / l;
+  *(h4*)(out + row * D + 4 * quad) = h4{(_Float16)(o[0] * r), (_Float16)(o[1] * r), (_Float16)(o[2] * r), (_Float16)(o[3] * r)};
+}
+
 template <bool KV4, int DP, int QT, int WK>
 void launch_shape(AttendArgs a, hipStream_t s) {
   a.col_blocks = (int)ceil_div((int64_t)a.q_len * a.rep, 16 * QT);
@@ -323,9 +353,8 @@ AttendParts attend_parts(int64_t batch, int64_t q_len, int64_t heads, int64_t kv
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
   const bool few = cols <= kFewColumns;
   const int64_t groups = batch * kv_heads * ceil_div(cols, few ? (cols <= 16 ? 16 : 32) : tiles_columns(padded_head((int)head_dim)));
-  static int slots = getenv("P_SLOTS") ? atoi(getenv("P_SLOTS")) : 512, leastt = getenv("P_LEAST") ? atoi(getenv("P_LEAST")) : 16;
-  int64_t parts = few ? ceil_div(256, groups) : slots / groups;
-  const int64_t most = ceil_div(tiles, few ? 32 : leastt);
+  int64_t parts = few ? ceil_div(256, groups) : 512 / groups;
+  const int64_t most = ceil_div(tiles, few ? 32 : 16);
   parts = parts < 1 ? 1 : parts < most ? parts : most;
   if (parts > kMostParts) parts = kMostParts;
   AttendParts p;
@@ -348,7 +377,10 @@ static gpusq_status run(AttendArgs a, bool kv4, const AttendParts& p, void* work
     DP == 64 ? launch_head<false, 64>(a, s) : DP == 128 ? launch_head<false, 128>(a, s) : launch_head<false, 256>(a, s);
   gpusq_status st = check_launch();
   if (st != GPUSQ_OK || p.parts == 1) return st;
-  join_parts_kernel<<<(unsigned)rows, 256, 0, s>>>(a.part_o, a.part_ml, a.out, (int)rows, a.D, p.parts);
+  if (p.parts <= kFewParts)
+    join_few_parts_kernel<<<(unsigned)ceil_div(rows, 256 / (a.D / 4)), 256, 0, s>>>(a.part_o, a.part_ml, a.out, rows, a.D, p.parts);
+  else
+    join_parts_kernel<<<(unsigned)rows, 256, 0, s>>>(a.part_o, a.part_ml, a.out, (int)rows, a.D, p.parts);
   return check_launch();
 }
 

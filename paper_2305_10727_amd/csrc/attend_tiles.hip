@@ -74,10 +74,10 @@ struct Codes {
   int len, num_pages, kv_heads, kh, wave, lane;
   bool there;
 
-  __device__ __forceinline__ Codes(const AttendArgs& a, const Work& w, int len_, int wave_, int lane_)
+  __device__ __forceinline__ Codes(const AttendArgs& a, const Work& w, int len_, int wave_, int lane_, const uint8_t*)
       : cache(a.cache), table(a.table + (int64_t)w.b * a.max_pages), len(len_), num_pages(a.num_pages), kv_heads(a.kv_heads), kh(w.kh), wave(wave_), lane(lane_), there(false) {}
 
-  __device__ __forceinline__ void load(int key0) {
+  __device__ __forceinline__ void load(int, int key0) {
     const int number = table[key0 >> 6];
     there = (unsigned)number < (unsigned)num_pages;  // (a number that is no page is read as page 0, and not seen)
     const uint8_t* page = cache + ((int64_t)(there ? number : 0) * kv_heads + kh) * page_bytes(DP);
@@ -118,10 +118,10 @@ struct Codes {
   }
 };
 
-constexpr int tile_waves_per_simd(int DP, int QT) { return DP > 128 ? 1 : DP / 64 * QT <= 4 ? 2 : 1; }
+constexpr int tile_waves_per_simd(bool kv4, int DP) { return DP > 128 && kv4 ? 1 : DP > 64 ? 2 : kv4 ? 3 : 4; }
 
 template <bool KV4, int DP, int QT, int NW, int KT, bool MASKED>
-__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP, QT)) attend_tiles_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP)) attend_tiles_kernel(const AttendArgs a) {
   static_assert(!KV4 || (KT == 64 && NW == 4), "a page, 16 keys a wavefront");
   constexpr int J = DP / 32, CH = DP / 16, NT = 64 * NW, kTile = KT * kRow<DP>;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * 2 * kTile];  // [buffer][keys, values]
@@ -135,14 +135,24 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP, QT)) attend_t
   const int cols = span.nq * a.rep, col_tiles = (cols + 15) >> 4, groups = (col_tiles + NW * QT - 1) / (NW * QT);
   if (w.block >= groups) return;
   const int tile0 = w.block * col_tiles / groups, tile1 = (w.block + 1) * col_tiles / groups;
-  Columns<KV4, DP, QT> x;
-  // (block i of a wavefront beyond the workgroup's last: columns that are no columns)
-  x.load(a, span, w.kh, g, r, [&](int i) { return tile0 + wave + NW * i < tile1 ? 16 * (tile0 + wave + NW * i) : cols; });
   const bool works = tile0 + wave < tile1;
   const int least = span.sees(16 * (tile0 + wave) / a.rep);
   const int last = 16 * tile1 < cols ? 16 * tile1 - 1 : cols - 1;
   const int most = span.sees(last / a.rep);
   const int first_key = w.part * a.part_tiles * 32, end_key = first_key + a.part_tiles * 32 < most ? first_key + a.part_tiles * 32 : most;
+  typedef typename std::conditional<KV4, Codes<DP>, States<DP, KT, NW>>::type Stage;
+  Stage stage(a, w, span.len, wave, lane, lds);
+  if (!KV4 && a.D < DP) {  // the pieces beyond the head: zeros, once
+    for (int i = threadIdx.x; i < 4 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
+    __syncthreads();
+  }
+  if (first_key < end_key) stage.load(0, first_key);
+  Columns<KV4, DP, QT> x;
+  // (block i of a wavefront beyond the workgroup's last: columns that are no columns)
+  x.load(a, span, w.kh, g, r, [&](int i) { return tile0 + wave + NW * i < tile1 ? 16 * (tile0 + wave + NW * i) : cols; });
+  // The queries are waited for here: their first use is inside the loop, where the compiler, which does not know of the copies to LDS, would
+  // wait for all of these as well.  (165 us for what takes 137 with the wait here.)
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
 
   // this lane's key operands and value operands: pieces by their places
   int key_at[J], value_at[CH];
@@ -174,8 +184,10 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP, QT)) attend_t
         shown[0] = *(const unsigned*)&seen[32 * half + 4 * g];
         shown[1] = *(const unsigned*)&seen[32 * half + 16 + 4 * g];
       }
-      x.softmax(s, a.c, MASKED || !there || key0 + 32 * half + 32 > least,
-                [&](int i, int t, int e) { return (shown[t] >> (8 * e) & 1) == 0 || at + 16 * t + e >= (there ? x.limit[i] : 0); }, p);
+      if (MASKED || !there || key0 + 32 * half + 32 > least) x.hide(s, [&](int i, int t, int e) { return (shown[t] >> (8 * e) & 1) == 0 || at + 16 * t + e >= (there ? x.limit[i] : 0); });
+      x.template follow<false>(s, a.c, p);
+      x.weights(s, a.c, p);
+      x.sum(p);
 #pragma unroll
       for (int t = 0; t < CH; ++t) {
         const h4 v0 = read_transposed(tile + value_at[t] + 32 * half * kRow<DP>), v1 = read_transposed(tile + value_at[t] + (32 * half + 16) * kRow<DP>);
@@ -187,15 +199,13 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP, QT)) attend_t
   };
 
   if constexpr (KV4) {
-    Codes<DP> stage(a, w, span.len, wave, lane);
     auto put = [&](int buf) {
       stage.write(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile);
       if (threadIdx.x == 0) pages[buf] = stage.there;
     };
     if (first_key < end_key) {
-      stage.load(first_key);
       put(0);
-      if (first_key + KT < end_key) stage.load(first_key + KT);
+      if (first_key + KT < end_key) stage.load(0, first_key + KT);
     }
     int buf = 0;
     for (int key0 = first_key; key0 < end_key; key0 += KT) {
@@ -203,17 +213,11 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP, QT)) attend_t
       if (works) multiply(buf, key0, pages[buf] != 0);
       if (key0 + KT < end_key) {
         put(buf ^ 1);
-        if (key0 + 2 * KT < end_key) stage.load(key0 + 2 * KT);
+        if (key0 + 2 * KT < end_key) stage.load(0, key0 + 2 * KT);
       }
       buf ^= 1;
     }
   } else {
-    const States<DP, KT, NW> stage(a, w, span.len, wave, lane, lds);
-    if (a.D < DP) {  // the pieces beyond the head: zeros, once
-      for (int i = threadIdx.x; i < 4 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
-      __syncthreads();
-    }
-    if (first_key < end_key) stage.load(0, first_key);
     int buf = 0;
     for (int key0 = first_key; key0 < end_key; key0 += KT) {
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // this tile is there, and nobody reads the other buffer
@@ -257,7 +261,7 @@ void launch_attend_tiles(bool kv4, AttendArgs a, hipStream_t s) {
   if (kv4)
     DP == 64 ? launch_shape<true, 64, 2, 4, 64>(a, s) : DP == 128 ? launch_shape<true, 128, 2, 4, 64>(a, s) : launch_shape<true, 256, 1, 4, 64>(a, s);
   else
-    DP == 64 ? launch_shape<false, 64, 2, 4, 64>(a, s) : DP == 128 ? launch_shape<false, 128, 2, 4, 64>(a, s) : launch_shape<false, 256, 1, 4, 64>(a, s);
+    DP == 64 ? launch_shape<false, 64, 2, 4, 32>(a, s) : DP == 128 ? launch_shape<false, 128, 2, 4, 32>(a, s) : launch_shape<false, 256, 1, 4, 32>(a, s);
 }
 
 }  // namespace gpusq
