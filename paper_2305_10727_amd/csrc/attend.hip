@@ -59,6 +59,9 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
   const int most = span.sees((col0 + 16 * QT < cols ? col0 + 16 * QT - 1 : cols - 1) / a.rep);
   const int tiles = most > 0 ? (most + 31) >> 5 : 0;
   const int begin = w.part * a.part_tiles, end = begin + a.part_tiles < tiles ? begin + a.part_tiles : tiles;
+  // The first keys, values and the queries are waited for together, in front of the loop: left to itself the compiler waits at its top, for
+  // whatever order these were requested in, which in later rounds means for the values requested just before.
+  auto first_wait = [] { __builtin_amdgcn_s_waitcnt(0x0F70); };  // vmcnt(0)
 
   if constexpr (KV4) {
     // a wavefront takes whole pages: both halves of one, then the next of its own
@@ -71,12 +74,13 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
     int tile = begin + 2 * wk;
     // Page numbers are read a tile ahead of the keys, keys a product ahead, whether there are more or not: of loads that are left out at the
     // end the compiler makes registers without a value, and has then put 72 times a scale where the scale was.  (Also a branch less.)
-    // a number that is no page is read as page 0 and not seen
+    // A number that is no page is read as page 0 and not seen.
     int number = page_of(tile), next = page_of(after(tile));
     bool there = (unsigned)number < (unsigned)a.num_pages;
     const uint8_t* page = page_at(there ? number : 0);
     k.load(page, 0, g, r);  // (without a tile of its own: page 0, not used)
     v.load(page, 0, g, r);
+    first_wait();
     while (tile < end) {
       const int key0 = tile * 32;
       f4 s[QT][2] = {};
@@ -158,6 +162,7 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       load_k(tile * 32);
       load_v(tile * 32);
     }
+    first_wait();
     for (; tile < end; tile += WK) {
       const int key0 = tile * 32;
       unsigned vis = 0xFFu;

@@ -43,7 +43,12 @@ __device__ __forceinline__ float group_scale(float amax) {
 // The eight codes of a word (code + 8 in 4 bits) as products with the scale: pair p is nibble p of the lower half and of the upper one.
 // A nibble in bits 4..7 of 0x5400 is 64 + nibble; (64 + nibble) s - 72 s is the exact product, 72 s having 11 significant bits at most.
 // 11 instructions for 8 values.
-__device__ __forceinline__ unsigned nibbles_at_4(unsigned w) { return (w & 0x00f000f0u) | 0x54005400u; }
+// (One instruction, its constants in registers: with two literal constants the compiler makes two.)
+__device__ __forceinline__ unsigned nibbles_at_4(unsigned w) {
+  unsigned mask = 0x00f000f0u, base = 0x54005400u, d;
+  asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(d) : "v"(w), "s"(mask), "v"(base));
+  return d;
+}
 __device__ __forceinline__ void codes_to_halves(unsigned w, h2 s, h2 m72s, h2 (&out)[4]) {
   out[0] = __builtin_elementwise_fma(__builtin_bit_cast(h2, nibbles_at_4(w << 4)), s, m72s);
   out[1] = __builtin_elementwise_fma(__builtin_bit_cast(h2, nibbles_at_4(w)), s, m72s);
