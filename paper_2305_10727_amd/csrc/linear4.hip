@@ -95,94 +95,125 @@ struct Linear4Args {
   int M, N, K, kt, epilogue;
 };
 
-// MT columns of 16 activation rows, NF tiles of 16 channels, NW wavefronts; GROUP channels of a scale
-template <int MT, int NF, int NW, int GROUP, bool F32>
-__global__ void __launch_bounds__(64 * NW) linear_int4_kernel(const Linear4Args a) {
-  constexpr int PER = 128 / GROUP, CH = GROUP / 32;  // groups of a step, products of a group
-  __shared__ f4 part[NW][NF * MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
-  const int nt = (a.N + 15) >> 4;
-  const int tile0 = blockIdx.x * NF, m0 = blockIdx.y * 16 * MT;
-  const u4* codes[NF];
-  const h4* scales[NF];
+// Channels n .. n + 3 of row m, if they are there (N % 4 == 0: they are inside or outside together)
+template <bool F32>
+__device__ __forceinline__ void store_channels(const Linear4Args& a, f4 y, int n, int m) {
+  if (n >= a.N || m >= a.M) return;
+  if (a.epilogue & GPUSQ_EPI_BIAS) y += *(const f4*)(a.bias + n);
+  if (a.epilogue & GPUSQ_EPI_GELU) {
 #pragma unroll
-  for (int f = 0; f < NF; ++f) {
-    const int64_t tile = tile0 + f < nt ? tile0 + f : nt - 1;  // (a tile beyond the last is computed again and not stored)
-    codes[f] = (const u4*)(a.W + tile * a.kt * 1024) + lane;
-    scales[f] = (const h4*)(a.W + (int64_t)nt * a.kt * 1024 + tile * a.kt * PER * 32) + g;
+    for (int e = 0; e < 4; ++e) y[e] = gelu_exact(y[e]);
   }
-  const _Float16* x[MT];
+  const int64_t at = (int64_t)m * a.N + n;
+  if constexpr (F32)
+    *(f4*)((float*)a.Y + at) = y;
+  else
+    *(h4*)((_Float16*)a.Y + at) = h4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
+}
+
+// A few rows: a workgroup takes one tile of 16 channels after another, each wavefront the same S steps of all of them, so that its rows (MT
+// columns of 16) stay in registers.  (A load of 16 bytes a lane takes the first-level cache 16 clocks, whether its lanes ask for the same
+// bytes or not: a step's rows cost four times what its weights do.)  A longer K is taken in chunks of S NW steps, the tiles' sums waiting in LDS.
+template <int MT, int NW, int S, bool CHUNKS, int GROUP, bool F32>
+__global__ void __launch_bounds__(64 * NW, NW / 4) linear_int4_rows_kernel(const Linear4Args a) {
+  constexpr int PER = 128 / GROUP, CH = GROUP / 32;
+  extern __shared__ __attribute__((aligned(16))) f4 lds[];  // [2][NW][MT][64], and with chunks [tiles of the workgroup][MT][64]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
+  const int nt = (a.N + 15) >> 4, chunks = CHUNKS ? (a.kt + NW * S - 1) / (NW * S) : 1;
+  const int m0 = blockIdx.y * 16 * MT;
+  f4* totals = lds + 2 * NW * MT * 64;
+  struct Weights {
+    u4 w[S];
+    h4 s[S][PER];
+  };
+  auto load = [&](int chunk, int tile, Weights& x) {
+    const u4* codes = (const u4*)(a.W + (int64_t)tile * a.kt * 1024) + lane;
+    const h4* scales = (const h4*)(a.W + (int64_t)nt * a.kt * 1024 + (int64_t)tile * a.kt * PER * 32) + g;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int at = (chunk * NW + wave) * S + i, step = at < a.kt ? at : a.kt - 1;  // (a step beyond the last: that one again, with rows of zeros)
+      x.w[i] = codes[(int64_t)step * 64];
+#pragma unroll
+      for (int p = 0; p < PER; ++p) x.s[i][p] = scales[(step * PER + p) * 4];
+    }
+  };
+  const _Float16* rows[MT];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int row = m0 + 16 * m + r < a.M ? m0 + 16 * m + r : a.M - 1;  // (columns beyond the last row repeat it and are not stored)
-    x[m] = a.X + (int64_t)row * a.K + 8 * g;
+    rows[m] = a.X + (int64_t)row * a.K + 8 * g;
   }
-  f4 acc[NF][MT] = {};
-  for (int step = wave; step < a.kt; step += NW) {
-    u4 w[NF];
-    h4 s[NF][PER];
-    h8 b[MT][4];
-#pragma unroll
-    for (int f = 0; f < NF; ++f) {
-      w[f] = codes[f][(int64_t)step * 64];
-#pragma unroll
-      for (int p = 0; p < PER; ++p) s[f][p] = scales[f][(step * PER + p) * 4];
-    }
+  Weights next;
+  load(0, blockIdx.x, next);
+  int buf = 0, turn = 0;
+  for (int chunk = 0; chunk < chunks; ++chunk) {
+    h8 b[MT][S][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) b[m][j] = 128 * step + 32 * j < a.K ? *(const h8*)(x[m] + 128 * step + 32 * j) : h8(0);
+      for (int i = 0; i < S; ++i)
 #pragma unroll
-    for (int f = 0; f < NF; ++f)
-#pragma unroll
-      for (int p = 0; p < PER; ++p) {
-        f4 sum[MT] = {};
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const int j = p * CH + c;
-          h2 v[4];
-          codes_to_halves(w[f][j], v);
-          const h8 wa = {v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
-#pragma unroll
-          for (int m = 0; m < MT; ++m) sum[m] = mfma16(wa, b[m][j], sum[m]);
+        for (int j = 0; j < 4; ++j) {
+          const int k = 128 * ((chunk * NW + wave) * S + i) + 32 * j;
+          b[m][i][j] = k < a.K ? *(const h8*)(rows[m] + k) : h8(0);
         }
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): else the loop waits for the rows again, and with them for the next tile's weights
+    for (int tile = blockIdx.x, n = 0; tile < nt; tile += gridDim.x, ++n) {
+      const Weights now = next;
+      const int ahead = tile + gridDim.x;
+      if constexpr (CHUNKS)
+        load(ahead < nt || chunk + 1 == chunks ? chunk : chunk + 1, ahead < nt ? ahead : chunk + 1 == chunks ? tile : blockIdx.x, next);
+      else
+        load(0, ahead < nt ? ahead : tile, next);  // (behind the last one: that one again)
+      f4 acc[MT] = {};
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+      for (int i = 0; i < S; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[f][m][e] = __builtin_fmaf(sum[m][e], (float)s[f][p][e], acc[f][m][e]);
+        for (int p = 0; p < PER; ++p) {
+          f4 sum[MT] = {};
+#pragma unroll
+          for (int c = 0; c < CH; ++c) {
+            h2 v[4];
+            codes_to_halves(now.w[i][p * CH + c], v);
+            const h8 wa = {v[0][0], v[0][1], v[1][0], v[1][1], v[2][0], v[2][1], v[3][0], v[3][1]};
+#pragma unroll
+            for (int m = 0; m < MT; ++m) sum[m] = mfma16(wa, b[m][i][p * CH + c], sum[m]);
+          }
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][e] = __builtin_fmaf(sum[m][e], (float)now.s[i][p][e], acc[m][e]);
+        }
+      f4* part = lds + buf * NW * MT * 64;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) part[(wave * MT + m) * 64 + lane] = acc[m];
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (the next weights stay in flight)
+      // MT wavefronts add up, others from tile to tile
+      const int m = wave >= turn ? wave - turn : wave - turn + NW;
+      if (m < MT) {
+        f4 y = part[m * 64 + lane];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) y += part[(w * MT + m) * 64 + lane];
+        f4* total = totals + (n * MT + m) * 64 + lane;
+        if (CHUNKS && chunk > 0) y += *total;
+        if (CHUNKS && chunk + 1 < chunks)
+          *total = y;
+        else
+          store_channels<F32>(a, y, tile * 16 + 4 * g, m0 + 16 * m + r);
       }
-  }
-#pragma unroll
-  for (int f = 0; f < NF; ++f)
-#pragma unroll
-    for (int m = 0; m < MT; ++m) part[wave][f * MT + m][lane] = acc[f][m];
-  __syncthreads();
-  for (int i = threadIdx.x; i < NF * MT * 64; i += 64 * NW) {
-    const int fm = i >> 6, l = i & 63;
-    f4 y = part[0][fm][l];
-#pragma unroll
-    for (int w = 1; w < NW; ++w) y += part[w][fm][l];
-    const int n = (tile0 + fm / MT) * 16 + 4 * (l >> 4), m = m0 + fm % MT * 16 + (l & 15);
-    if (n >= a.N || m >= a.M) continue;  // (N % 4 == 0: four channels are inside or outside together)
-    if (a.epilogue & GPUSQ_EPI_BIAS) y += *(const f4*)(a.bias + n);
-    if (a.epilogue & GPUSQ_EPI_GELU) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = gelu_exact(y[e]);
-    }
-    const int64_t at = (int64_t)m * a.N + n;
-    if constexpr (F32) {
-      *(f4*)((float*)a.Y + at) = y;
-    } else {
-      const h4 out = {(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
-      *(h4*)((_Float16*)a.Y + at) = out;
+      buf ^= 1;
+      turn = turn + MT < NW ? turn + MT : 0;
     }
   }
 }
 
-template <int MT, int NF, int NW>
-void launch_shape(const Linear4Args& a, int group, bool f32, hipStream_t s) {
-  const dim3 grid((unsigned)ceil_div(ceil_div(a.N, 16), NF), (unsigned)ceil_div(a.M, 16 * MT));
-#define GPUSQ_LINEAR4(G, F) linear_int4_kernel<MT, NF, NW, G, F><<<grid, 64 * NW, 0, s>>>(a)
+template <int MT, int NW, int S, bool CHUNKS>
+void launch_rows(const Linear4Args& a, int group, bool f32, hipStream_t s) {
+  // one workgroup a CU, with as many tiles each (and no more sums than LDS holds)
+  const int64_t nt = ceil_div(a.N, 16), each = ceil_div(nt, num_cus()), most = 160 / MT - 2 * NW, per = CHUNKS && each > most ? most : each;
+  const size_t lds = (size_t)(2 * NW + (CHUNKS ? per : 0)) * MT * 1024;
+  const dim3 grid((unsigned)ceil_div(nt, per), (unsigned)ceil_div(a.M, 16 * MT));
+#define GPUSQ_LINEAR4(G, F) linear_int4_rows_kernel<MT, NW, S, CHUNKS, G, F><<<grid, 64 * NW, lds, s>>>(a)
   if (group == 32)
     f32 ? GPUSQ_LINEAR4(32, true) : GPUSQ_LINEAR4(32, false);
   else if (group == 64)
@@ -215,12 +246,21 @@ gpusq_status launch_pack_int4_groups(const int8_t* codes, const void* scales, in
 gpusq_status launch_linear_int4(const void* X, const void* W, int group, const float* bias, void* Y, bool f32, int64_t M, int64_t N, int64_t K, int epilogue,
                                 hipStream_t s) {
   const Linear4Args a{(const _Float16*)X, (const uint8_t*)W, bias, Y, (int)M, (int)N, (int)K, (int)ceil_div(K, 128), epilogue};
+  // The fewest steps a wavefront that K needs: registers for rows, and wavefronts for as much of the weights in flight as there are
+  // (8 wavefronts rather than 16 up to K = 2048: 1024 -> 1024 for one row 2.7 us, 3.4 with 16; 5120 -> 13824 10.9 with 8, 10.2 with 16).
   if (M <= 16)
-    launch_shape<1, 1, 8>(a, group, f32, s);
+    a.kt <= 8    ? launch_rows<1, 8, 1, false>(a, group, f32, s)
+    : a.kt <= 16 ? launch_rows<1, 8, 2, false>(a, group, f32, s)
+    : a.kt <= 32 ? launch_rows<1, 16, 2, false>(a, group, f32, s)
+    : a.kt <= 48 ? launch_rows<1, 16, 3, false>(a, group, f32, s)
+    : a.kt <= 64 ? launch_rows<1, 16, 4, false>(a, group, f32, s)
+                 : launch_rows<1, 16, 4, true>(a, group, f32, s);
   else if (M <= 32)
-    launch_shape<2, 2, 8>(a, group, f32, s);
+    a.kt <= 16   ? launch_rows<2, 16, 1, false>(a, group, f32, s)
+    : a.kt <= 32 ? launch_rows<2, 16, 2, false>(a, group, f32, s)
+                 : launch_rows<2, 16, 2, true>(a, group, f32, s);
   else
-    launch_shape<4, 2, 8>(a, group, f32, s);
+    a.kt <= 16 ? launch_rows<4, 16, 1, false>(a, group, f32, s) : launch_rows<4, 16, 1, true>(a, group, f32, s);
   return check_launch();
 }
 
