@@ -20,8 +20,9 @@ struct QkArgs {
   const int32_t *positions, *slots;
   _Float16 *q_out, *k_out, *v_out;
   uint8_t* cache;
-  int64_t vectors;
-  int heads, kv_heads, D, R, table_rows, num_pages, norm, interleaved, per_token;
+  int heads, kv_heads, D, R, table_rows, num_pages, norm;
+  int vectors, per_token;   // of this launch: below 2^31
+  unsigned magic, shift;    // vector / per_token = (vector * magic >> 32) >> shift
   float eps;
 };
 
@@ -36,49 +37,65 @@ __device__ __forceinline__ f4 load_quad(const T* p) {
 }
 __device__ __forceinline__ void store_quad(_Float16* p, f4 v) { *(h4*)p = h4{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]}; }
 
-// T: type of the projection; L: lanes of a vector (a power of two, 8 L >= D); CACHE: keys and values go into the cache
-template <typename T, int L, bool CACHE>
+// T: type of the projection.  INTER: pairs are neighbours (or nothing turns).  CACHE: keys and values go into the cache.  L: lanes of a vector,
+// 8, 16 or 32, with CACHE those of the head as it is padded; 0: as many as it needs, a.D / 8, side by side in a wavefront.
+template <typename T, int L_, bool INTER, bool CACHE>
 __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const QkArgs a) {
-  constexpr int VECS = 256 / L;
-  __shared__ unsigned most[CACHE ? VECS : 1][8];  // of the groups of 32 channels, as the bits of non-negative floats
-  const int sub = threadIdx.x / L, lane = threadIdx.x % L;
-  const int64_t vec = (int64_t)blockIdx.x * VECS + sub;
-  const bool in_vec = vec < a.vectors;
-  const int64_t t = in_vec ? vec / a.per_token : 0;
-  const int h = in_vec ? (int)(vec - t * a.per_token) : 0;
-  const bool in = in_vec && 8 * lane < a.D;
-  const bool is_q = h < a.heads, is_v = h >= a.heads + a.kv_heads;
+  const int L = L_ != 0 ? L_ : a.D / 8, lane = threadIdx.x & 63;
+  const int in_wave = L_ != 0 ? lane / L_ : (int)((unsigned)lane * (unsigned)(65536 / L + 1) >> 16), at = lane - in_wave * L;  // (exact: lane < 64, L <= 32)
+  const int of_wave = 64 / L, sub = (threadIdx.x >> 6) * of_wave + in_wave;
+  __shared__ unsigned most[CACHE ? 256 / (CACHE ? L_ : 1) : 1][8];  // of the groups of 32 channels, as the bits of non-negative floats
+  const int vec = blockIdx.x * (4 * of_wave) + sub;
+  const bool in_vec = in_wave < of_wave && vec < a.vectors;
+  const int token = in_vec ? (int)(__umulhi((unsigned)vec, a.magic) >> a.shift) : 0, h = in_vec ? vec - token * a.per_token : 0;
+  const int64_t t = token;
+  const bool in = in_vec && 8 * at < a.D;
+  const bool is_q = h < a.heads, is_v = CACHE && h >= a.heads + a.kv_heads;
   // the two quads
-  const bool turns = !is_v && 8 * lane < a.R;
-  const int lo = turns && !a.interleaved ? 4 * lane : 8 * lane, hi = turns && !a.interleaved ? a.R / 2 + 4 * lane : 8 * lane + 4;
-  f4 x = f4(0), y = f4(0);
+  const bool turns = !is_v && 8 * at < a.R;
+  const int lo = turns && !INTER ? 4 * at : 8 * at, hi = turns && !INTER ? a.R / 2 + 4 * at : 8 * at + 4;
+  f4 x = f4(0), y = f4(0), c = f4(0), s = f4(0), wx = f4(1), wy = f4(1);
   if (in) {
     const T* row = (const T*)a.qkv + t * a.row_stride + (int64_t)h * a.D;
     x = load_quad(row + lo);
-    y = load_quad(row + hi);
+    y = load_quad(row + (INTER ? lo + 4 : hi));
+    if (turns) {
+      int p = a.positions[t];
+      p = p < 0 ? 0 : p < a.table_rows ? p : a.table_rows - 1;  // (a place beyond the table: its end)
+      const int64_t from = (int64_t)p * (a.R / 2) + 4 * at;
+      c = *(const f4*)(a.cos + from);
+      s = *(const f4*)(a.sin + from);
+    }
+    const float* w = is_q ? a.q_weight : a.k_weight;
+    if (w != nullptr && !is_v) {
+      wx = *(const f4*)(w + lo);
+      wy = *(const f4*)(w + hi);
+    }
   }
   if (a.norm) {
     float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum += x[e] * x[e] + y[e] * y[e];
+    for (int e = 0; e < 4; ++e) sum = __builtin_fmaf(x[e], x[e], __builtin_fmaf(y[e], y[e], sum));
+    if constexpr (L_ != 0) {
 #pragma unroll
-    for (int d = 1; d < L; d *= 2) sum += __shfl_xor(sum, d);
-    if (!is_v && in) {
-      const float r = 1.0f / __fsqrt_rn(sum / (float)a.D + a.eps);
+      for (int d = 1; d < L_; d *= 2) sum += __shfl_xor(sum, d);
+    } else {  // sums of the lanes from this one on; the first lane's is the vector's
+      for (int d = 1; d < L; d *= 2) {
+        const float other = __shfl(sum, lane + d);
+        sum += at + d < L ? other : 0.0f;
+      }
+      sum = __shfl(sum, lane - at);
+    }
+    if (!is_v) {
+      const float r = __builtin_amdgcn_rsqf(sum / (float)a.D + a.eps);
       x *= r;
       y *= r;
-      const float* w = is_q ? a.q_weight : a.k_weight;
-      if (w != nullptr) {
-        x *= *(const f4*)(w + lo);
-        y *= *(const f4*)(w + hi);
-      }
+      x *= wx;
+      y *= wy;
     }
   }
   if (in && turns) {
-    int p = a.positions[t];
-    p = p < 0 ? 0 : p < a.table_rows ? p : a.table_rows - 1;  // (a place beyond the table: its end)
-    const f4 c = *(const f4*)(a.cos + (int64_t)p * (a.R / 2) + 4 * lane), s = *(const f4*)(a.sin + (int64_t)p * (a.R / 2) + 4 * lane);
-    if (a.interleaved) {
+    if (INTER) {
       const f4 u = {x[0], x[2], y[0], y[2]}, v = {x[1], x[3], y[1], y[3]};
       const f4 m = u * c - v * s, n = u * s + v * c;
       x = f4{m[0], n[0], m[1], n[1]};
@@ -92,17 +109,21 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const QkArgs a) {
   if (is_q || !CACHE) {
     if (in) {
       _Float16* out = is_q ? a.q_out + (t * a.heads + h) * a.D : a.k_out + (t * a.kv_heads + (h - a.heads)) * a.D;
-      store_quad(out + lo, x);
-      store_quad(out + hi, y);
+      if constexpr (INTER) {
+        *(h8*)(out + lo) = h8{(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3], (_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
+      } else {
+        store_quad(out + lo, x);
+        store_quad(out + hi, y);
+      }
     }
     if constexpr (!CACHE) return;
   }
   if constexpr (CACHE) {
-    // (No wavefront leaves before the barriers.  Channels beyond the head are quads of zeros, which the lanes beyond it write: 8 L is what
-    // the head is padded to.)
-    for (int i = threadIdx.x; i < VECS * 8; i += 256) (&most[0][0])[i] = 0;
+    // (No wavefront leaves before the barriers.  Channels beyond the head are quads of zeros, which the lanes beyond it write: 8 L is what the
+    // head is padded to.)
+    for (int i = threadIdx.x; i < 256 / L_ * 8; i += 256) (&most[0][0])[i] = 0;
     __syncthreads();
-    constexpr int DP = 8 * L;
+    constexpr int DP = 8 * L_;
     const bool keeps = in_vec && !is_q;
     if (keeps && in) {
       float mx = 0.0f, my = 0.0f;
@@ -151,20 +172,31 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const QkArgs a) {
 }
 
 template <typename T, int L>
-gpusq_status launch_lanes(const QkArgs& a, hipStream_t s) {
-  const int64_t blocks = ceil_div(a.vectors, 256 / L);
-  if (blocks > INT32_MAX) return GPUSQ_ERR_SHAPE;
-  if (a.cache != nullptr)
-    qk_norm_rope_kernel<T, L, true><<<(unsigned)blocks, 256, 0, s>>>(a);
+void launch_lanes(const QkArgs& a, bool interleaved, hipStream_t s) {
+  const unsigned blocks = (unsigned)ceil_div(a.vectors, 4 * (64 / (L != 0 ? L : a.D / 8)));
+  if (interleaved || a.R == 0)
+    qk_norm_rope_kernel<T, L, true, false><<<blocks, 256, 0, s>>>(a);
   else
-    qk_norm_rope_kernel<T, L, false><<<(unsigned)blocks, 256, 0, s>>>(a);
-  return check_launch();
+    qk_norm_rope_kernel<T, L, false, false><<<blocks, 256, 0, s>>>(a);
 }
-
+template <typename T, int L>
+void launch_cached(const QkArgs& a, bool interleaved, hipStream_t s) {
+  const unsigned blocks = (unsigned)ceil_div(a.vectors, 256 / L);
+  if (interleaved || a.R == 0)
+    qk_norm_rope_kernel<T, L, true, true><<<blocks, 256, 0, s>>>(a);
+  else
+    qk_norm_rope_kernel<T, L, false, true><<<blocks, 256, 0, s>>>(a);
+}
 template <typename T>
-gpusq_status launch_typed(const QkArgs& a, hipStream_t s) {
-  if (a.D <= 64) return launch_lanes<T, 8>(a, s);
-  return a.D <= 128 ? launch_lanes<T, 16>(a, s) : launch_lanes<T, 32>(a, s);
+void launch_typed(const QkArgs& a, bool interleaved, hipStream_t s) {
+  if (a.cache != nullptr)
+    a.D <= 64 ? launch_cached<T, 8>(a, interleaved, s) : a.D <= 128 ? launch_cached<T, 16>(a, interleaved, s) : launch_cached<T, 32>(a, interleaved, s);
+  else if (a.D == 64)
+    launch_lanes<T, 8>(a, interleaved, s);
+  else if (a.D == 128)
+    launch_lanes<T, 16>(a, interleaved, s);
+  else
+    launch_lanes<T, 0>(a, interleaved, s);
 }
 
 }  // namespace
@@ -173,10 +205,21 @@ gpusq_status launch_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_st
                                  const float* q_weight, const float* k_weight, float eps, const float* cos, const float* sin, const int32_t* positions,
                                  int64_t table_rows, int64_t R, int interleaved, void* q_out, void* k_out, void* v_out, void* cache, const int32_t* slots,
                                  int64_t num_pages, hipStream_t s) {
-  const int per_token = (int)(heads + kv_heads + (cache != nullptr ? kv_heads : 0));
-  const QkArgs a{qkv, row_stride, q_weight, k_weight, cos, sin, positions, slots, (_Float16*)q_out, (_Float16*)k_out, (_Float16*)v_out, (uint8_t*)cache,
-                 T * per_token, (int)heads, (int)kv_heads, (int)D, (int)R, (int)table_rows, (int)num_pages, norm, interleaved, per_token, eps};
-  return dt == GPUSQ_F32 ? launch_typed<float>(a, s) : launch_typed<_Float16>(a, s);
+  const int64_t per_token = heads + kv_heads + (cache != nullptr ? kv_heads : 0), most = INT32_MAX / per_token;
+  unsigned bits = 1;  // per_token >= 2
+  while ((int64_t)1 << bits < per_token) ++bits;
+  const unsigned magic = (unsigned)(((uint64_t)1 << (31 + bits)) / per_token + 1);
+  for (int64_t from = 0; from < T; from += most) {  // (vectors are counted in 31 bits)
+    const int64_t n = T - from < most ? T - from : most;
+    const QkArgs a{(const uint8_t*)qkv + from * row_stride * (dt == GPUSQ_F32 ? 4 : 2), row_stride, q_weight, k_weight, cos, sin, positions ? positions + from : nullptr,
+                   slots ? slots + from : nullptr, (_Float16*)q_out + from * heads * D, k_out ? (_Float16*)k_out + from * kv_heads * D : nullptr,
+                   v_out ? (_Float16*)v_out + from * kv_heads * D : nullptr, (uint8_t*)cache, (int)heads, (int)kv_heads, (int)D, (int)R, (int)table_rows,
+                   (int)num_pages, norm, (int)(n * per_token), (int)per_token, magic, bits - 1, eps};
+    dt == GPUSQ_F32 ? launch_typed<float>(a, interleaved != 0, s) : launch_typed<_Float16>(a, interleaved != 0, s);
+    const gpusq_status st = check_launch();
+    if (st != GPUSQ_OK) return st;
+  }
+  return GPUSQ_OK;
 }
 
 }  // namespace gpusq
