@@ -286,3 +286,67 @@ class EncoderBlockLinears:
     def replay(self):
         self.graph.replay()
         return self.fc2.Y
+
+
+class DecoderLayer:
+    """One layer of a decoder that answers from images which the layers above have encoded, as it serves: attention over its own tokens in a
+    4-bit cache, attention to the encoder's states, two feed-forward layers; its weights in 4 bits with a scale for each group.
+    A step of some tokens is nine launches of the library (one more for each attention whose keys are cut into parts),
+        [norm], qkv, norms of the heads + rotation + append to the cache, attention over the cache, output, [residual],
+        [norm], queries, attention to the states, output, [residual], [norm], fc1 (GELU), fc2, [residual]:
+    the norms in front of the linear layers are the caller's (`norms`: three callables [T, D] fp16 -> [T, D] fp16), the residuals torch's.  The keys and values of the states come from many rows at once: a 2:4 sparse fp16 layer, run once an image (`see`).
+    capture() records a step into a HIP graph."""
+
+    def __init__(self, D, heads, kv_heads, head_dim, hidden, batch, states, states_dim, pages, group=64, device="cuda"):
+        self.D, self.heads, self.kv_heads, self.head_dim, self.hidden, self.group = D, heads, kv_heads, head_dim, hidden, group
+        self.batch, self.states = batch, states
+        self.cache = G.kv4_cache(pages, kv_heads, head_dim, device=device)
+        self.states_kv = SparseLinear(batch * states, states_dim, 2 * kv_heads * head_dim, "fp16", bias=True, device=device)
+        self.widths = dict(qkv=((heads + 2 * kv_heads) * head_dim, D), out=(D, heads * head_dim), query=(heads * head_dim, D), states_out=(D, heads * head_dim),
+                           fc1=(hidden, D), fc2=(D, hidden))
+        self.packed = {}
+        self.graph = None
+
+    def prepare_weights(self, weights, states_weight):
+        """weights: fp32 [N, K] by the names of `widths`; states_weight [2 kv_heads head_dim, states_dim] (keys, then values)"""
+        for name, (N, K) in self.widths.items():
+            W = weights[name]
+            if W.shape != (N, K):
+                raise ValueError("%s: [%d, %d] wanted" % (name, N, K))
+            self.packed[name] = G.pack_int4_groups(*G.quantize_groups_int4(W, self.group), self.group)
+        self.states_kv.prepare_weights(states_weight)
+
+    def see(self, states, bias):
+        """states [batch, states, states_dim] fp16 of the encoder: their keys and values, for every step that follows"""
+        self.states_kv.forward(states, bias)
+
+    def _linear(self, name, x, gelu=False):
+        return G.linear_int4(x, self.packed[name], self.widths[name][0], self.group, gelu=gelu)
+
+    def forward(self, x, norms, rope, positions, slots, block_table, kv_lens, head_weights=(None, None), state_lens=None):
+        """x [T, D] fp16, T / batch new tokens of each sequence; rope: (cos, sin); positions, slots [T], block_table [batch, pages of a sequence],
+        kv_lens [batch] (with the new tokens), state_lens [batch] or None: int32.  -> [T, D] fp16"""
+        T, H, hd = x.shape[0], self.heads, self.head_dim
+        q = G.qk_norm_rope(self._linear("qkv", norms[0](x)), H, self.kv_heads, hd, q_weight=head_weights[0], k_weight=head_weights[1], cos=rope[0], sin=rope[1],
+                           positions=positions, cache=self.cache, slots=slots)
+        a = G.attention_kv4(q, self.cache, block_table, kv_lens, max_q=T // self.batch)
+        x = x + self._linear("out", a.view(T, H * hd))
+        q = self._linear("query", norms[1](x)).view(self.batch, T // self.batch, H, hd)
+        kv = self.states_kv.Y.view(self.batch, self.states, 2 * self.kv_heads, hd)
+        a = G.cross_attention(q, kv[:, :, :self.kv_heads], kv[:, :, self.kv_heads:], kv_lens=state_lens)
+        x = x + self._linear("states_out", a.view(T, H * hd))
+        return x + self._linear("fc2", self._linear("fc1", norms[2](x), gelu=True))
+
+    def capture(self, *args, **kwargs):
+        """Records forward() on these tensors into a HIP graph (after one eager run that loads every kernel): replay() reruns it on what they
+        hold then, into the same output."""
+        self.forward(*args, **kwargs)
+        torch.cuda.synchronize()
+        self.graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(self.graph):
+            self.out = self.forward(*args, **kwargs)
+        return self.graph
+
+    def replay(self):
+        self.graph.replay()
+        return self.out
