@@ -102,7 +102,7 @@ gpusq_status gpusq_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_str
 
 size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads, int64_t head_dim) {
   if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !is_size(tokens) || !is_size(batch) || !is_size(max_q) || !is_size(max_pages)) return 0;
-  return parts_bytes(attend_parts(batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens), tokens, heads, head_dim);
+  return parts_bytes(attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens), tokens, heads, head_dim);
 }
 
 gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* kv_lens, const int32_t* cu_q, void* out,
@@ -116,7 +116,7 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
   if (max_q > tokens || (!cu_q && tokens != batch * max_q)) return GPUSQ_ERR_SHAPE;
   AttentionKv4 x{q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim, 0.0f};
   if (!score_scale(scale, head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
-  const AttendParts p = attend_parts(batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens);
+  const AttendParts p = attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens);
   if (!is_countable(batch, max_q, heads, p)) return GPUSQ_ERR_SHAPE;
   if (p.parts > 1 && !workspace) return GPUSQ_ERR_NULL;
   if (!aligned16(q) || !aligned16(cache) || !aligned16(out) || !aligned16(workspace) || !aligned4(block_table) || !aligned4(kv_lens) || !aligned4(cu_q))
@@ -126,7 +126,7 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
 
 size_t gpusq_cross_attention_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads, int64_t head_dim) {
   if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !is_size(batch) || !is_size(q_len) || !is_size(kv_len)) return 0;
-  return parts_bytes(attend_parts(batch, q_len, heads, kv_heads, head_dim, kv_len), batch * q_len, heads, head_dim);
+  return parts_bytes(attend_parts(false, batch, q_len, heads, kv_heads, head_dim, kv_len), batch * q_len, heads, head_dim);
 }
 
 gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, const int32_t* kv_lens, const uint8_t* key_mask, void* out, void* workspace,
@@ -146,7 +146,7 @@ gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, 
       if (strides[i] % 8 != 0) return GPUSQ_ERR_ALIGN;
     }
   if (!score_scale(scale, head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
-  const AttendParts p = attend_parts(batch, q_len, heads, kv_heads, head_dim, kv_len);
+  const AttendParts p = attend_parts(false, batch, q_len, heads, kv_heads, head_dim, kv_len);
   if (!is_countable(batch, q_len, heads, p)) return GPUSQ_ERR_SHAPE;
   if (p.parts > 1 && !workspace) return GPUSQ_ERR_NULL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(workspace) || !aligned4(kv_lens)) return GPUSQ_ERR_ALIGN;

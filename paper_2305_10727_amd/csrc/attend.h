@@ -219,7 +219,7 @@ struct Columns {
 constexpr int kFewColumns = 32;
 // (a tile of 64 tokens in 32-bit offsets)
 inline bool tiles_reach(bool kv4, const AttendArgs& a) { return kv4 || (a.k_token < (1 << 24) && a.v_token < (1 << 24)); }
-constexpr int tiles_columns(int DP) { return DP > 128 ? 64 : 128; }
+constexpr int tiles_columns(bool kv4, int DP) { return (DP > 128 ? 64 : 128) * (kv4 ? 2 : 1); }
 void launch_attend_tiles(bool kv4, AttendArgs a, hipStream_t s);
 
 }  // namespace gpusq

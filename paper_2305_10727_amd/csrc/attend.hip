@@ -11,31 +11,28 @@ namespace {
 template <int DP>
 struct Keys4 {
   static constexpr int J = DP / 32;
-  unsigned w[2][J];
-  h2 s[2][J / 2];
+  typename WordsOf<J>::type w[2];
+  typename WordsOf<J / 2>::type s[2];
   __device__ __forceinline__ void load(const uint8_t* page, int half, int g, int r) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int key = half * 32 + t * 16 + r;
-      load_words<J>(page + key * (DP / 2) + g * J * 4, w[t]);
-      unsigned u[J / 2];
-      if constexpr (J == 2) u[0] = *(const unsigned*)(page + key_scales_at(DP) + key * J * 2);
-      else load_words<J / 2>(page + key_scales_at(DP) + key * J * 2, u);
-#pragma unroll
-      for (int i = 0; i < J / 2; ++i) s[t][i] = __builtin_bit_cast(h2, u[i]);
+      w[t] = load_words<J>(page + key * (DP / 2) + g * J * 4);
+      s[t] = load_words<J / 2>(page + key_scales_at(DP) + key * J * 2);
     }
   }
 };
 template <int DP>
 struct Values4 {
   static constexpr int CH = DP / 16;
-  unsigned w[2][CH / 2], s[2][2];
+  typename WordsOf<CH / 2>::type w[2];
+  u2 s[2];
   __device__ __forceinline__ void load(const uint8_t* page, int half, int g, int r) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int quad = half * 8 + t * 4 + g;
-      load_words<CH / 2>(page + value_codes_at(DP) + (quad * 16 + r) * (2 * CH), w[t]);
-      load_words<2>(page + value_scales_at(DP) + (r * CH / 32 * kPageTokens + quad * 4) * 2, s[t]);
+      w[t] = load_words<CH / 2>(page + value_codes_at(DP) + (quad * 16 + r) * (2 * CH));
+      s[t] = load_words<2>(page + value_scales_at(DP) + (r * CH / 32 * kPageTokens + quad * 4) * 2);
     }
   }
 };
@@ -88,7 +85,7 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-          const h2 sc = {k.s[t][j / 2][j & 1], k.s[t][j / 2][j & 1]};
+          const h2 pair = __builtin_bit_cast(h2, (unsigned)k.s[t][j / 2]), sc = {pair[j & 1], pair[j & 1]};
           h2 c[4];
           codes_to_halves(k.w[t][j], sc, sc * (_Float16)-72.0f, c);
           const h8 ka = join(c[0], c[1], c[2], c[3]);
@@ -108,12 +105,12 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       x.sum(p);
       if (check) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) scales_in_front(v.s[t], there ? len - (key0 + 16 * t + 4 * g) : 0);
+        for (int t = 0; t < 2; ++t) v.s[t] = scales_in_front(v.s[t], there ? len - (key0 + 16 * t + 4 * g) : 0);
       }
       h2 sc[4], off[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        sc[i] = __builtin_bit_cast(h2, v.s[i >> 1][i & 1]);
+        sc[i] = __builtin_bit_cast(h2, (unsigned)v.s[i >> 1][i & 1]);
         off[i] = sc[i] * (_Float16)-72.0f;
       }
 #pragma unroll
@@ -354,11 +351,11 @@ void launch_head(const AttendArgs& a, hipStream_t s) {
 // The keys are cut into parts where the (batch, key head, block of columns) are too few workgroups for the device, of 32 tiles (1024 keys)
 // at least for few columns, of 16 for many.
 // Few columns: 256 workgroups, one a CU (8 key heads, 131071 tokens: 38.9 us; 512 39.7, 1024 45, 2048 55).
-AttendParts attend_parts(int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys) {
+AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys) {
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
   const bool few = cols <= kFewColumns;
-  const int64_t groups = batch * kv_heads * ceil_div(cols, few ? (cols <= 16 ? 16 : 32) : tiles_columns(padded_head((int)head_dim)));
-  int64_t parts = few ? ceil_div(256, groups) : 512 / groups;
+  const int64_t groups = batch * kv_heads * ceil_div(cols, few ? (cols <= 16 ? 16 : 32) : tiles_columns(kv4, padded_head((int)head_dim)));
+  int64_t parts = few ? ceil_div(256, groups) : (kv4 ? 256 : 512) / groups;
   const int64_t most = ceil_div(tiles, few ? 32 : 16);
   parts = parts < 1 ? 1 : parts < most ? parts : most;
   if (parts > kMostParts) parts = kMostParts;
@@ -408,7 +405,7 @@ gpusq_status launch_attention_kv4(const AttentionKv4& x, hipStream_t s) {
   a.num_pages = (int)x.num_pages;
   a.tokens = (int)x.tokens;
   a.lens = x.kv_lens;
-  return run(a, true, attend_parts(x.batch, x.max_q, x.heads, x.kv_heads, x.head_dim, x.max_pages * kPageTokens), x.workspace, s);
+  return run(a, true, attend_parts(true, x.batch, x.max_q, x.heads, x.kv_heads, x.head_dim, x.max_pages * kPageTokens), x.workspace, s);
 }
 
 gpusq_status launch_cross_attention(const CrossAttention& x, hipStream_t s) {
@@ -436,7 +433,7 @@ gpusq_status launch_cross_attention(const CrossAttention& x, hipStream_t s) {
   a.c = x.scale * kLog2e;
   a.lens = x.kv_lens;
   a.mask = x.key_mask;
-  return run(a, false, attend_parts(x.batch, x.q_len, x.heads, x.kv_heads, x.head_dim, x.kv_len), x.workspace, s);
+  return run(a, false, attend_parts(false, x.batch, x.q_len, x.heads, x.kv_heads, x.head_dim, x.kv_len), x.workspace, s);
 }
 
 }  // namespace gpusq

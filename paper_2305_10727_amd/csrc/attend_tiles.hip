@@ -37,7 +37,7 @@ struct States {
   uint32_t lds;
   int row[COPIES], piece[COPIES], len, D2;
 
-  __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles)
+  __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles, int)
       : kp((const uint8_t*)(a.k + w.b * a.k_batch + w.kh * a.k_head)), vp((const uint8_t*)(a.v + w.b * a.v_batch + w.kh * a.v_head)), k_row(2 * a.k_token), v_row(2 * a.v_token),
         lds(lds_address(tiles) + wave * COPIES * 1024), len(len_), D2(2 * a.D) {
 #pragma unroll
@@ -63,66 +63,87 @@ struct States {
 };
 
 // ---- the cache's codes on their way -----------------------------------------------------------------------------------------------------
-// KT = 64: a page.  Wavefront w has keys 16 w .. + 15: lane 16 g + r pieces 4 j + g of key r, and channels CH r .. of the quad of values 4 w + g.
-template <int DP>
+// Each wavefront has 16 tokens' keys (lane 16 g + r pieces 4 j + g of key r) or 16 tokens' values (channels CH r .. of quad g).
+template <int DP, int KT, int NW>
 struct Codes {
+  static_assert(KT / 8 == NW, "16 keys or values a wavefront");
   static constexpr int J = DP / 32, CH = DP / 16;
-  unsigned kw[J], vw[CH / 2], vs[2];
-  h2 ks[J / 2];
+  static constexpr int SW = J > 4 ? J / 2 : 2;
+  typename WordsOf<J>::type w;   // codes, of a key or of a quad of values
+  typename WordsOf<SW>::type s;  // scales: J / 2 words of a key, 2 of a quad of values
   const uint8_t* cache;
   const int32_t* table;
-  int len, num_pages, kv_heads, kh, wave, lane;
-  bool there;
+  int len, num_pages, kv_heads, kh, part, lane, last_page, number;
+  bool values, there;
 
-  __device__ __forceinline__ Codes(const AttendArgs& a, const Work& w, int len_, int wave_, int lane_, const uint8_t*)
-      : cache(a.cache), table(a.table + (int64_t)w.b * a.max_pages), len(len_), num_pages(a.num_pages), kv_heads(a.kv_heads), kh(w.kh), wave(wave_), lane(lane_), there(false) {}
-
+  // (a page's number is read a tile ahead of its words: first_key's here)
+  __device__ __forceinline__ Codes(const AttendArgs& a, const Work& w, int len_, int wave, int lane_, const uint8_t*, int first_key)
+      : cache(a.cache), table(a.table + (int64_t)w.b * a.max_pages), len(len_), num_pages(a.num_pages), kv_heads(a.kv_heads), kh(w.kh), part(wave % (NW / 2)), lane(lane_),
+        last_page((len_ - 1) >> 6), number(0), values(wave >= NW / 2), there(false) {
+    if (first_key < len_) number = table[first_key >> 6];
+  }
   __device__ __forceinline__ void load(int, int key0) {
-    const int number = table[key0 >> 6];
     there = (unsigned)number < (unsigned)num_pages;  // (a number that is no page is read as page 0, and not seen)
     const uint8_t* page = cache + ((int64_t)(there ? number : 0) * kv_heads + kh) * page_bytes(DP);
-    const int g = lane >> 4, r = lane & 15, key = wave * 16 + r, quad = wave * 4 + g;
-    load_words<J>(page + key * (DP / 2) + g * J * 4, kw);
-    unsigned u[J / 2];
-    if constexpr (J == 2) u[0] = *(const unsigned*)(page + key_scales_at(DP) + key * J * 2);
-    else load_words<J / 2>(page + key_scales_at(DP) + key * J * 2, u);
+    const int after = (key0 + KT) >> 6;
+    number = table[after < last_page ? after : last_page];
+    const int g = lane >> 4, r = lane & 15, token = (key0 & 63) + part * 16;
+    if (!values) {
+      w = load_words<J>(page + (token + r) * (DP / 2) + g * J * 4);
+      const auto u = load_words<J / 2>(page + key_scales_at(DP) + (token + r) * J * 2);
 #pragma unroll
-    for (int i = 0; i < J / 2; ++i) ks[i] = __builtin_bit_cast(h2, u[i]);
-    load_words<CH / 2>(page + value_codes_at(DP) + (quad * 16 + r) * (2 * CH), vw);
-    load_words<2>(page + value_scales_at(DP) + (r * CH / 32 * kPageTokens + quad * 4) * 2, vs);
-    if (!there || key0 + 64 > len) scales_in_front(vs, there ? len - (key0 + quad * 4) : 0);
-  }
-  __device__ __forceinline__ void write(uint8_t* keys, uint8_t* values) const {
-    const int g = lane >> 4, r = lane & 15;
-#pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const h2 sc = {ks[j / 2][j & 1], ks[j / 2][j & 1]};
-      h2 c[4];
-      codes_to_halves(kw[j], sc, sc * (_Float16)-72.0f, c);
-      *(h8*)(keys + (wave * 16 + r) * kRow<DP> + place<DP>(r, 4 * j + g) * 16) = join(c[0], c[1], c[2], c[3]);
+      for (int i = 0; i < SW; ++i) s[i] = i < J / 2 ? u[i] : 0u;
+    } else {
+      const int quad = (token >> 2) + g;
+      w = load_words<J>(page + value_codes_at(DP) + (quad * 16 + r) * (2 * CH));
+      u2 u = load_words<2>(page + value_scales_at(DP) + (r * CH / 32 * kPageTokens + quad * 4) * 2);
+      if (!there || key0 + KT > len) u = scales_in_front(u, there ? len - (key0 + part * 16 + 4 * g) : 0);
+      s[0] = u[0];
+      s[1] = u[1];
     }
-    const h2 s0 = __builtin_bit_cast(h2, vs[0]), s1 = __builtin_bit_cast(h2, vs[1]), off0 = s0 * (_Float16)-72.0f, off1 = s1 * (_Float16)-72.0f;
+  }
+  __device__ __forceinline__ void write(uint8_t* rows_of_keys, uint8_t* rows_of_values) const {
+    const int g = lane >> 4, r = lane & 15;
+    if (!values) {
 #pragma unroll
-    for (int qd = 0; qd < CH / 4; ++qd) {
-      h2 c0[4], c1[4];
-      codes_to_halves(vw[qd], s0, off0, c0);
-      codes_to_halves(vw[CH / 4 + qd], s1, off1, c1);
-      const int piece = (CH * r + 4 * qd) >> 3, half = CH == 4 ? r & 1 : qd & 1;
+      for (int j = 0; j < J; ++j) {
+        const h2 pair = __builtin_bit_cast(h2, (unsigned)s[j / 2]), sc = {pair[j & 1], pair[j & 1]};
+        h2 c[4];
+        codes_to_halves(w[j], sc, sc * (_Float16)-72.0f, c);
+        *(h8*)(rows_of_keys + (part * 16 + r) * kRow<DP> + place<DP>(r, 4 * j + g) * 16) = join(c[0], c[1], c[2], c[3]);
+      }
+      return;
+    }
+    const h2 s0 = __builtin_bit_cast(h2, (unsigned)s[0]), s1 = __builtin_bit_cast(h2, (unsigned)s[1]), off0 = s0 * (_Float16)-72.0f, off1 = s1 * (_Float16)-72.0f;
+    constexpr int Q = CH >= 8 ? 2 : 1;  // quads of channels that are a piece of a row, or its half
+#pragma unroll
+    for (int q0 = 0; q0 < CH / 4; q0 += Q) {
+      h2 c[Q][2][4];  // [quad][tokens 0, 1 and 2, 3][channel]
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        codes_to_halves(w[q0 + i], s0, off0, c[i][0]);
+        codes_to_halves(w[CH / 4 + q0 + i], s1, off1, c[i][1]);
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const h2(&c)[4] = e < 2 ? c0 : c1;
         const int token = 4 * g + e;
-        *(h4*)(values + (wave * 16 + token) * kRow<DP> + place<DP>(token, piece) * 16 + half * 8) = h4{c[0][e & 1], c[1][e & 1], c[2][e & 1], c[3][e & 1]};
+        uint8_t* at = rows_of_values + (part * 16 + token) * kRow<DP> + place<DP>(token, (CH * r + 4 * q0) >> 3) * 16;
+        const h2(&x)[4] = c[0][e >> 1], (&y)[4] = c[Q - 1][e >> 1];
+        if constexpr (Q == 2)
+          *(h8*)at = h8{x[0][e & 1], x[1][e & 1], x[2][e & 1], x[3][e & 1], y[0][e & 1], y[1][e & 1], y[2][e & 1], y[3][e & 1]};
+        else
+          *(h4*)(at + (r & 1) * 8) = h4{x[0][e & 1], x[1][e & 1], x[2][e & 1], x[3][e & 1]};
       }
     }
   }
 };
 
-constexpr int tile_waves_per_simd(bool kv4, int DP) { return DP > 128 && kv4 ? 1 : DP > 64 ? 2 : kv4 ? 3 : 4; }
+// (the cache: 8 wavefronts on tiles of 64 keys, one workgroup a CU, as the codes are unpacked once for all of them: chunks of 300 94 us, with 4
+// wavefronts on tiles of 32, three workgroups a CU, 117)
+constexpr int tile_waves_per_simd(int DP) { return DP > 64 ? 2 : 4; }
 
 template <bool KV4, int DP, int QT, int NW, int KT, bool MASKED>
-__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP)) attend_tiles_kernel(const AttendArgs a) {
-  static_assert(!KV4 || (KT == 64 && NW == 4), "a page, 16 keys a wavefront");
+__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP)) attend_tiles_kernel(const AttendArgs a) {
   constexpr int J = DP / 32, CH = DP / 16, NT = 64 * NW, kTile = KT * kRow<DP>;
   __shared__ __attribute__((aligned(16))) uint8_t lds[2 * 2 * kTile];  // [buffer][keys, values]
   __shared__ __attribute__((aligned(4))) uint8_t seen[MASKED ? KT : 4];
@@ -140,8 +161,8 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP)) attend_
   const int last = 16 * tile1 < cols ? 16 * tile1 - 1 : cols - 1;
   const int most = span.sees(last / a.rep);
   const int first_key = w.part * a.part_tiles * 32, end_key = first_key + a.part_tiles * 32 < most ? first_key + a.part_tiles * 32 : most;
-  typedef typename std::conditional<KV4, Codes<DP>, States<DP, KT, NW>>::type Stage;
-  Stage stage(a, w, span.len, wave, lane, lds);
+  typedef typename std::conditional<KV4, Codes<DP, KT, NW>, States<DP, KT, NW>>::type Stage;
+  Stage stage(a, w, span.len, wave, lane, lds, first_key);
   if (!KV4 && a.D < DP) {  // the pieces beyond the head: zeros, once
     for (int i = threadIdx.x; i < 4 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
     __syncthreads();
@@ -210,11 +231,13 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP)) attend_
     int buf = 0;
     for (int key0 = first_key; key0 < end_key; key0 += KT) {
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (loads for registers stay in flight)
-      if (works) multiply(buf, key0, pages[buf] != 0);
+      // the next tile, whose words have had the time of the one before, goes to LDS first: nobody waits for the writes at the next barrier
+      const bool there = pages[buf] != 0;
       if (key0 + KT < end_key) {
         put(buf ^ 1);
         if (key0 + 2 * KT < end_key) stage.load(0, key0 + 2 * KT);
       }
+      if (works) multiply(buf, key0, there);
       buf ^= 1;
     }
   } else {
@@ -259,7 +282,7 @@ void launch_shape(AttendArgs a, hipStream_t s) {
 void launch_attend_tiles(bool kv4, AttendArgs a, hipStream_t s) {
   const int DP = padded_head(a.D);
   if (kv4)
-    DP == 64 ? launch_shape<true, 64, 2, 4, 64>(a, s) : DP == 128 ? launch_shape<true, 128, 2, 4, 64>(a, s) : launch_shape<true, 256, 1, 4, 64>(a, s);
+    DP == 64 ? launch_shape<true, 64, 2, 8, 64>(a, s) : DP == 128 ? launch_shape<true, 128, 2, 8, 64>(a, s) : launch_shape<true, 256, 1, 8, 64>(a, s);
   else
     DP == 64 ? launch_shape<false, 64, 2, 4, 32>(a, s) : DP == 128 ? launch_shape<false, 128, 2, 4, 32>(a, s) : launch_shape<false, 256, 1, 4, 32>(a, s);
 }

@@ -66,26 +66,25 @@ __device__ __forceinline__ void codes_to_halves(unsigned w, h2 (&out)[4]) {
 
 // N words, in vectors of up to four
 template <int N>
-__device__ __forceinline__ void load_words(const uint8_t* p, unsigned (&w)[N]) {
-  if constexpr (N == 2) {
-    const u2 v = *(const u2*)p;
-    w[0] = v[0];
-    w[1] = v[1];
+struct WordsOf {
+  typedef unsigned type __attribute__((ext_vector_type(N)));
+};
+template <int N>
+__device__ __forceinline__ typename WordsOf<N>::type load_words(const uint8_t* p) {
+  if constexpr (N == 8) {
+    const u4 a = *(const u4*)p, b = *(const u4*)(p + 16);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  } else if constexpr (N == 1) {
+    return *(const unsigned*)p;
   } else {
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const u4 v = *(const u4*)(p + 4 * i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[i + j] = v[j];
-    }
+    return *(const typename WordsOf<N>::type*)p;
   }
 }
 
 // Scales of four tokens as two pairs; those of tokens from `left` on are 0 (places behind the last token may hold anything: a scale of
 // theirs may be infinite or NaN, and 0 times it too).
-__device__ __forceinline__ void scales_in_front(unsigned (&s)[2], int left) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) s[i] &= left > 2 * i + 1 ? 0xFFFFFFFFu : left > 2 * i ? 0xFFFFu : 0u;
+__device__ __forceinline__ u2 scales_in_front(u2 s, int left) {
+  return u2{s[0] & (left > 1 ? 0xFFFFFFFFu : left > 0 ? 0xFFFFu : 0u), s[1] & (left > 3 ? 0xFFFFFFFFu : left > 2 ? 0xFFFFu : 0u)};
 }
 
 // v_mfma_f32_16x16x32_f16: lane 16 g + r has row (column) r and k = 8 g .. + 7 of the operands, column r and rows 4 g .. + 3 of the result
