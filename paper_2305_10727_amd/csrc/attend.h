@@ -50,20 +50,23 @@ struct Work {
   int b, kh, part, block;
   __device__ __forceinline__ bool find(const AttendArgs& a) {
     const int units = a.batch * a.kv_heads * a.parts, xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
+    // (divisions take a scalar unit that has none some forty instructions each: none by 1)
     int unit;
     if (in_turn(units)) {
-      block = local % a.col_blocks;
-      unit = local / a.col_blocks * 8 + xcd;
+      const int first = a.col_blocks == 1 ? local : local / a.col_blocks;
+      block = local - first * a.col_blocks;
+      unit = first * 8 + xcd;
       if (unit >= units) return false;
     } else {
       const int total = units * a.col_blocks, per_xcd = (total + 7) >> 3, at = xcd * per_xcd + local;
       if (local >= per_xcd || at >= total) return false;
-      block = at % a.col_blocks;
-      unit = at / a.col_blocks;
+      unit = a.col_blocks == 1 ? at : at / a.col_blocks;
+      block = at - unit * a.col_blocks;
     }
-    part = unit % a.parts;
-    b = unit / a.parts / a.kv_heads;
-    kh = unit / a.parts % a.kv_heads;
+    const int pair = a.parts == 1 ? unit : unit / a.parts;
+    part = unit - pair * a.parts;
+    b = a.batch == 1 ? 0 : pair / a.kv_heads;
+    kh = pair - b * a.kv_heads;
     return true;
   }
   static __host__ __device__ __forceinline__ bool in_turn(int64_t units) { return units >= 64 || units % 8 == 0; }
@@ -188,10 +191,8 @@ struct Columns {
     for (int i = 0; i < QT; ++i) l[i] = mfma16(h8{u, u, u, u, u, u, u, u}, p[i], l[i]);
   }
 
-  // Lane 16 g + r has channel(t, e) of its column in o[.][t][e]; four in a row over e (or over t, where they are apart over e).
-  template <class Channel>
-  __device__ __forceinline__ void store(const AttendArgs& a, int part, Channel channel, int g) const {
-    const bool over_e = channel(0, 1) == channel(0, 0) + 1;
+  // Lane 16 g + r has channels 16 t + 4 g .. + 3 of its column in o[.][t].
+  __device__ __forceinline__ void store(const AttendArgs& a, int part, int g) const {
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
       if (row[i] < 0) continue;
@@ -202,14 +203,13 @@ struct Columns {
         a.part_ml[2 * at + 1] = l[i][0];
       }
 #pragma unroll
-      for (int n = 0; n < CH; ++n) {
-        const int t = over_e ? n : n / 4 * 4, e = over_e ? 0 : n % 4, c = channel(t, e);
-        const f4 v = over_e ? o[i][t] : f4{o[i][t][e], o[i][t + 1][e], o[i][t + 2][e], o[i][t + 3][e]};
+      for (int t = 0; t < CH; ++t) {
+        const int c = 16 * t + 4 * g;
         if (c >= a.D) continue;
         if (a.parts > 1)
-          *(f4*)(a.part_o + at * a.D + c) = v;
+          *(f4*)(a.part_o + at * a.D + c) = o[i][t];
         else
-          *(h4*)(a.out + (int64_t)row[i] * a.D + c) = h4{(_Float16)(v[0] * f), (_Float16)(v[1] * f), (_Float16)(v[2] * f), (_Float16)(v[3] * f)};
+          *(h4*)(a.out + (int64_t)row[i] * a.D + c) = h4{(_Float16)(o[i][t][0] * f), (_Float16)(o[i][t][1] * f), (_Float16)(o[i][t][2] * f), (_Float16)(o[i][t][3] * f)};
       }
     }
   }

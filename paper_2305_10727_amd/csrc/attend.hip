@@ -205,49 +205,53 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
     }
   }
 
-  __shared__ float ml[WK][2][16 * QT];
-  __shared__ f4 sums[WK / 2][QT][CH][64];
-  if (g == 0) {
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      ml[wk][0][16 * i + r] = x.m[i];
-      ml[wk][1][16 * i + r] = x.l[i][0];
-    }
-  }
-  __syncthreads();
+  // One trip through LDS: every wavefront's sums, maxima and sums of weights, then a thread for each (column, four channels).
+  // Column c keeps its quad i in place i ^ (c % 16): what lanes write together lies in different banks.
+  constexpr int QUADS = DP / 4, COLS = 16 * QT;
+  __shared__ f4 sums[WK][COLS][QUADS];
+  __shared__ float ml[WK][2][COLS];
+  __shared__ int rows[COLS];
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
-    float n = ml[0][0][16 * i + r];
+    if (g == 0) {
+      ml[wk][0][16 * i + r] = x.m[i];
+      ml[wk][1][16 * i + r] = x.l[i][0];
+      if (wk == 0) rows[16 * i + r] = x.row[i];
+    }
 #pragma unroll
-    for (int k = 1; k < WK; ++k) n = fmaxf(n, ml[k][0][16 * i + r]);
-    const float ref = n == -__builtin_inff() ? 0.0f : n;
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int t = 0; t < CH; t += 4)
+        sums[wk][16 * i + r][(((4 * g + e) * CH + t) / 4) ^ r] = f4{x.o[i][t][e], x.o[i][t + 1][e], x.o[i][t + 2][e], x.o[i][t + 3][e]};
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < COLS * QUADS; i += 64 * WK) {
+    const int col = i / QUADS, quad = i % QUADS, row = rows[col];
+    if (row < 0 || 4 * quad >= a.D) continue;
+    float top = ml[0][0][col];
+#pragma unroll
+    for (int k = 1; k < WK; ++k) top = fmaxf(top, ml[k][0][col]);
+    const float ref = top == -__builtin_inff() ? 0.0f : top;
     float total = 0.0f;
+    f4 y = f4(0);
 #pragma unroll
-    for (int k = 0; k < WK; ++k) total += ml[k][1][16 * i + r] * __builtin_amdgcn_exp2f(ml[k][0][16 * i + r] - ref);
-    const float f = __builtin_amdgcn_exp2f(x.m[i] - ref);
-#pragma unroll
-    for (int t = 0; t < CH; ++t) x.o[i][t] *= f;
-    x.m[i] = n;
-    x.l[i][0] = total;
-  }
-#pragma unroll
-  for (int n = WK / 2; n > 0; n /= 2) {  // the upper half of the wavefronts hands its sums to the lower half
-    if (wk >= n && wk < 2 * n) {
-#pragma unroll
-      for (int i = 0; i < QT; ++i)
-#pragma unroll
-        for (int t = 0; t < CH; ++t) sums[wk - n][i][t][lane] = x.o[i][t];
+    for (int k = 0; k < WK; ++k) {
+      const float f = __builtin_amdgcn_exp2f(ml[k][0][col] - ref);
+      total += ml[k][1][col] * f;
+      y += sums[k][col][quad ^ (col & 15)] * f;
     }
-    __syncthreads();
-    if (wk < n) {
-#pragma unroll
-      for (int i = 0; i < QT; ++i)
-#pragma unroll
-        for (int t = 0; t < CH; ++t) x.o[i][t] += sums[wk][i][t][lane];
+    if (a.parts > 1) {
+      const int64_t at = (int64_t)w.part * a.tokens * a.heads + row;
+      if (quad == 0) {
+        a.part_ml[2 * at] = top;
+        a.part_ml[2 * at + 1] = total;
+      }
+      *(f4*)(a.part_o + at * a.D + 4 * quad) = y;
+    } else {
+      const float f = total == 0.0f ? 0.0f : 1.0f / total;
+      *(h4*)(a.out + (int64_t)row * a.D + 4 * quad) = h4{(_Float16)(y[0] * f), (_Float16)(y[1] * f), (_Float16)(y[2] * f), (_Float16)(y[3] * f)};
     }
-    __syncthreads();
   }
-  if (wk == 0) x.store(a, w.part, [&](int t, int e) { return CH * (4 * g + e) + t; }, g);
 }
 
 // Joins the parts of a row: a workgroup for each.  Its threads read the parts' maxima side by side, then take (channels, share of the

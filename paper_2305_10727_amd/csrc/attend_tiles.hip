@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP)) attend_tiles
       buf ^= 1;
     }
   }
-  if (works) x.store(a, w.part, [&](int t, int e) { return 16 * t + 4 * g + e; }, g);
+  if (works) x.store(a, w.part, g);
 }
 
 template <bool KV4, int DP, int QT, int NW, int KT>
