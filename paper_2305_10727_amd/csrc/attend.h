@@ -25,7 +25,7 @@ struct AttendArgs {
   int64_t q_batch, q_token, q_head;  // in values
   int64_t o_token;                   // out: [token][heads][D]
   int heads, kv_heads, rep, D, batch, q_len;
-  float c;  // scale * log2(e)
+  float c, inv_c;  // scale * log2(e) and 1 by it
   // over the cache
   const uint8_t* cache;
   const int32_t *table, *cu_q;
@@ -108,6 +108,10 @@ struct Span {
   }
 };
 
+// (One instruction.  A NaN is passed on, which fmaxf would leave out, with another instruction for each operand to see to it: a column with a
+// NaN among its scores has no other value.)
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
+
 // QT blocks of 16 columns of a wavefront
 template <bool KV4, int DP, int QT>
 struct Columns {
@@ -115,7 +119,7 @@ struct Columns {
   h8 q[QT][J];
   int limit[QT], row[QT];  // keys that this lane's column sees; its row of the output, or -1
   f4 o[QT][CH], l[QT];
-  float m[QT];
+  float m[QT], limit_s[QT], off[QT];  // the maxima in log2 units; the scores beyond which they move; what takes them off, and adds the shift
 
   // block i begins at column first(i)
   template <class First>
@@ -129,7 +133,8 @@ struct Columns {
       const _Float16* p = a.q + span.q_base + tok * a.q_token + head * a.q_head;
 #pragma unroll
       for (int j = 0; j < J; ++j) q[i][j] = in && 32 * j + 8 * g < a.D ? *(const h8*)(p + 32 * j + 8 * g) : h8(0);
-      m[i] = -__builtin_inff();
+      m[i] = limit_s[i] = -__builtin_inff();
+      off[i] = kShift;
       l[i] = f4(0);
 #pragma unroll
       for (int t = 0; t < CH; ++t) o[i][t] = f4(0);
@@ -137,79 +142,89 @@ struct Columns {
   }
 
   // Scores^T of 32 keys to p^T, in three steps.  hidden(i, t, e): whether block i's column of this lane does not see key 16 t + 4 g + e
-  template <class Hidden>
-  __device__ __forceinline__ void hide(f4 (&s)[QT][2], Hidden hidden) const {
+  // (of the first N blocks)
+  template <int N, class Hidden>
+  __device__ __forceinline__ void hide(f4 (&s)[N][2], Hidden hidden) const {
 #pragma unroll
-    for (int i = 0; i < QT; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[i][t][e] = hidden(i, t, e) ? -__builtin_inff() : s[i][t][e];
   }
-  // Moves the maxima if a score passes one by kSlack, and rescales the sums, and weights p that are not in them yet (they become 2^-8 of what
-  // they were, or less, so that their second rounding is of no weight).
-  template <bool PENDING>
-  __device__ __forceinline__ void follow(const f4 (&s)[QT][2], float c, h8 (&p)[QT]) {
-    float top[QT];
+  // Moves the maxima if a score passes one by kSlack, and rescales the sums.
+  template <int N>
+  __device__ __forceinline__ void follow(const f4 (&s)[N][2], const AttendArgs& a) {
+    float top[N];
     bool moves = false;
 #pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])), fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3]))) * c;
-      moves |= top[i] > m[i] + kSlack;
+    for (int i = 0; i < N; ++i) {
+      top[i] = max3(max3(s[i][0][0], s[i][0][1], s[i][0][2]), max3(s[i][0][3], s[i][1][0], s[i][1][1]), max3(s[i][1][2], s[i][1][3], s[i][1][3]));
+      moves |= top[i] > limit_s[i];
     }
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(moves) != 0, 0)) {
 #pragma unroll
-      for (int i = 0; i < QT; ++i) {
+      for (int i = 0; i < N; ++i) {
         float n = fmaxf(top[i], __shfl_xor(top[i], 16));
-        n = fmaxf(n, __shfl_xor(n, 32));
+        n = fmaxf(n, __shfl_xor(n, 32)) * a.c;
         n = fmaxf(n, m[i]);
         const float f = m[i] == n ? 1.0f : __builtin_amdgcn_exp2f(m[i] - n);  // (-inf by -inf: nothing there to scale)
         m[i] = n;
+        limit_s[i] = (n + kSlack) * a.inv_c;
+        off[i] = kShift - (n == -__builtin_inff() ? 0.0f : n);
         l[i] *= f;
 #pragma unroll
         for (int t = 0; t < CH; ++t) o[i][t] *= f;
-        if constexpr (PENDING) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[i][e] = (_Float16)((float)p[i][e] * f);
-        }
       }
     }
   }
-  __device__ __forceinline__ void weights(const f4 (&s)[QT][2], float c, h8 (&p)[QT]) const {
+  template <int N>
+  __device__ __forceinline__ void weights(const f4 (&s)[N][2], float c, h8 (&p)[N]) const {
 #pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      const float off = kShift - (m[i] == -__builtin_inff() ? 0.0f : m[i]);
+    for (int i = 0; i < N; ++i)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[i][4 * t + e] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i][t][e], c, off));
-    }
+        for (int e = 0; e < 4; ++e) p[i][4 * t + e] = (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i][t][e], c, off[i]));
   }
-  __device__ __forceinline__ void sum(const h8 (&p)[QT]) {
+  template <int N>
+  __device__ __forceinline__ void sum(const h8 (&p)[N]) {
     const _Float16 u = (_Float16)1.0f;
 #pragma unroll
-    for (int i = 0; i < QT; ++i) l[i] = mfma16(h8{u, u, u, u, u, u, u, u}, p[i], l[i]);
+    for (int i = 0; i < N; ++i) l[i] = mfma16(h8{u, u, u, u, u, u, u, u}, p[i], l[i]);
   }
 
-  // Lane 16 g + r has channels 16 t + 4 g .. + 3 of its column in o[.][t].
+  // Lane 16 g + r has channels 16 t + 4 g .. + 3 of its column in o[.][t].  Whole results go out by 8 channels: two blocks of channels' odd and
+  // even groups of lanes change places, and four lanes write 64 bytes of a row.
   __device__ __forceinline__ void store(const AttendArgs& a, int part, int g) const {
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-      if (row[i] < 0) continue;
       const int64_t at = (int64_t)part * a.tokens * a.heads + row[i];
-      const float f = a.parts > 1 ? 1.0f : l[i][0] == 0.0f ? 0.0f : 1.0f / l[i][0];
-      if (a.parts > 1 && g == 0) {
-        a.part_ml[2 * at] = m[i];
-        a.part_ml[2 * at + 1] = l[i][0];
-      }
+      if (a.parts > 1) {
+        if (row[i] < 0) continue;
+        if (g == 0) {
+          a.part_ml[2 * at] = m[i];
+          a.part_ml[2 * at + 1] = l[i][0];
+        }
 #pragma unroll
-      for (int t = 0; t < CH; ++t) {
-        const int c = 16 * t + 4 * g;
-        if (c >= a.D) continue;
-        if (a.parts > 1)
-          *(f4*)(a.part_o + at * a.D + c) = o[i][t];
-        else
-          *(h4*)(a.out + (int64_t)row[i] * a.D + c) = h4{(_Float16)(o[i][t][0] * f), (_Float16)(o[i][t][1] * f), (_Float16)(o[i][t][2] * f), (_Float16)(o[i][t][3] * f)};
+        for (int t = 0; t < CH; ++t)
+          if (16 * t + 4 * g < a.D) *(f4*)(a.part_o + at * a.D + 16 * t + 4 * g) = o[i][t];
+        continue;
+      }
+      const float f = l[i][0] == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l[i][0]);
+#pragma unroll
+      for (int t = 0; t < CH; t += 2) {
+        u4 w;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const f4 x = o[i][t], y = o[i][t + 1];
+          const h2 p = {(_Float16)(x[2 * e] * f), (_Float16)(x[2 * e + 1] * f)}, q = {(_Float16)(y[2 * e] * f), (_Float16)(y[2 * e + 1] * f)};
+          const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, p), __builtin_bit_cast(uint32_t, q), false, false);
+          w[e] = s[0];
+          w[2 + e] = s[1];
+        }
+        const int c = 16 * (t + (g & 1)) + 8 * (g >> 1);
+        if (row[i] >= 0 && c < a.D) *(u4*)(a.out + (int64_t)row[i] * a.D + c) = w;
       }
     }
   }

@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       const bool check = key0 + 32 > least || !there;
       h8 p[QT];
       if (check) x.hide(s, [&](int i, int t, int e) { return key0 + 16 * t + 4 * g + e >= (there ? x.limit[i] : 0); });
-      x.template follow<false>(s, a.c, p);
+      x.follow(s, a);
       x.weights(s, a.c, p);
       x.sum(p);
       if (check) {
@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       if (tile + WK < end) load_k((tile + WK) * 32);
       h8 p[QT];
       if (MASKED || key0 + 32 > len) x.hide(s, [&](int, int t, int e) { return ((vis >> (4 * t + e)) & 1) == 0 || key0 + 16 * t + 4 * g + e >= len; });
-      x.template follow<false>(s, a.c, p);
+      x.follow(s, a);
       x.weights(s, a.c, p);
       x.sum(p);
 #pragma unroll
@@ -402,6 +402,7 @@ gpusq_status launch_attention_kv4(const AttentionKv4& x, hipStream_t s) {
   a.batch = (int)x.batch;
   a.q_len = (int)x.max_q;
   a.c = x.scale * kLog2e;
+  a.inv_c = 1.0f / a.c;
   a.cache = (const uint8_t*)x.cache;
   a.table = x.block_table;
   a.cu_q = x.cu_q;
@@ -435,6 +436,7 @@ gpusq_status launch_cross_attention(const CrossAttention& x, hipStream_t s) {
   a.kv_len = (int)x.kv_len;
   a.tokens = (int)(x.batch * x.q_len);
   a.c = x.scale * kLog2e;
+  a.inv_c = 1.0f / a.c;
   a.lens = x.kv_lens;
   a.mask = x.key_mask;
   return run(a, false, attend_parts(false, x.batch, x.q_len, x.heads, x.kv_heads, x.head_dim, x.kv_len), x.workspace, s);

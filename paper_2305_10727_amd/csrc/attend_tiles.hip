@@ -1,10 +1,12 @@
 // Attention of many queries (a prompt's chunk over the cache, an image's tokens to its own or another's states): the kernel whose bound is
 // arithmetic.  A workgroup's wavefronts have columns of their own and share the keys: keys and values go through LDS a tile at a time, in rows
 // as they lie in memory, with the 16-byte pieces of a row in places that differ from row to row (place()), so that neither the 16 rows of a
-// key operand nor the transposed reads of a value operand meet in a bank.  Two buffers: while one is multiplied the other is filled.
+// key operand nor the transposed reads of a value operand meet in a bank.  While one buffer is multiplied the others are filled.
 //   fp16 states go from memory to LDS directly; the cache's codes become fp16 numbers on the way, once for all the workgroup's columns.
 #include "attend.h"
 #include "tile_common.h"
+
+#include <type_traits>
 
 namespace gpusq {
 
@@ -27,34 +29,54 @@ __device__ __forceinline__ h4 read_transposed(const uint8_t* p) {
 }
 
 // ---- fp16 states on their way: memory to LDS, 1 KB a wavefront and instruction -----------------------------------------------------------
-template <int DP, int KT, int NW>
+// Behind a mask of bytes only the keys that are seen are copied: what the others hold, which may be anything (0 times it would not be 0), does
+// not get there, and their rows keep what an earlier tile left or the zeros of the beginning.  The first product begins at 0 or -inf by key.
+template <int DP, int KT, int NW, bool MASKED>
 struct States {
   static constexpr int PIECES = DP / 8, ROWS = 64 / PIECES;          // pieces of a row, rows of an instruction
   static constexpr int COPIES = KT / (ROWS * NW);                    // instructions of a wavefront, for keys and for values
-  static_assert(COPIES * ROWS * NW == KT, "whole instructions");
+  static_assert(COPIES > 0 && COPIES * ROWS * NW == KT, "whole instructions");
   const uint8_t *kp, *vp;
   int64_t k_row, v_row;  // bytes
   uint32_t lds;
   int row[COPIES], piece[COPIES], len, D2;
+  const uint8_t* mask;
+  uint8_t byte[COPIES];
+  float* begin;  // [buffer][key of a tile]
+  bool first;    // of a row's lanes
 
-  __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles, int)
+  __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles, float* begin_, int)
       : kp((const uint8_t*)(a.k + w.b * a.k_batch + w.kh * a.k_head)), vp((const uint8_t*)(a.v + w.b * a.v_batch + w.kh * a.v_head)), k_row(2 * a.k_token), v_row(2 * a.v_token),
-        lds(lds_address(tiles) + wave * COPIES * 1024), len(len_), D2(2 * a.D) {
+        lds(lds_address(tiles) + wave * COPIES * 1024), len(len_), D2(2 * a.D),
+        mask(MASKED ? a.mask + (int64_t)w.b * a.kv_len : nullptr), begin(begin_), first(lane % PIECES == 0) {
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
       row[i] = (wave * COPIES + i) * ROWS + lane / PIECES;
       piece[i] = 16 * place<DP>(row[i], lane % PIECES);
     }
   }
+  // the bytes for load(., key0), a tile before it
+  __device__ __forceinline__ void look(int key0) {
+#pragma unroll
+    for (int i = 0; i < COPIES; ++i) byte[i] = mask[key0 + row[i] < len ? key0 + row[i] : len - 1];
+  }
   // Rows from `len` on are its last row once more (finite where that is), pieces beyond the head are left out.
   __device__ __forceinline__ void load(int buf, int key0) const {
     const uint8_t *k = kp + key0 * k_row, *v = vp + key0 * v_row;
     const int last = len - 1 - key0;
+    unsigned sees = ~0u;
+    if constexpr (MASKED) {
+#pragma unroll
+      for (int i = 0; i < COPIES; ++i) sees = row[i] <= last && byte[i] != 0 ? sees : sees & ~(1u << i);
+      asm volatile("" : "+v"(sees));  // (all of the bytes, before a copy: the compiler, which does not count these, would wait for them as well)
+    }
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
       const unsigned r = row[i] < last ? row[i] : last;
       const uint32_t at = lds + buf * (2 * KT * kRow<DP>) + i * 1024;
-      if (piece[i] < D2) {
+      const bool see = !MASKED || (sees >> i & 1) != 0;
+      if (MASKED && first) begin[buf * KT + row[i]] = see ? 0.0f : -__builtin_inff();
+      if (see && piece[i] < D2) {
         copy16_to_lds(k, r * (unsigned)k_row + piece[i], at);
         copy16_to_lds(v, r * (unsigned)v_row + piece[i], at + KT * kRow<DP>);
       }
@@ -77,7 +99,7 @@ struct Codes {
   bool values, there;
 
   // (a page's number is read a tile ahead of its words: first_key's here)
-  __device__ __forceinline__ Codes(const AttendArgs& a, const Work& w, int len_, int wave, int lane_, const uint8_t*, int first_key)
+  __device__ __forceinline__ Codes(const AttendArgs& a, const Work& w, int len_, int wave, int lane_, const uint8_t*, const float*, int first_key)
       : cache(a.cache), table(a.table + (int64_t)w.b * a.max_pages), len(len_), num_pages(a.num_pages), kv_heads(a.kv_heads), kh(w.kh), part(wave % (NW / 2)), lane(lane_),
         last_page((len_ - 1) >> 6), number(0), values(wave >= NW / 2), there(false) {
     if (first_key < len_) number = table[first_key >> 6];
@@ -138,15 +160,23 @@ struct Codes {
   }
 };
 
-// (the cache: 8 wavefronts on tiles of 64 keys, one workgroup a CU, as the codes are unpacked once for all of them: chunks of 300 94 us, with 4
-// wavefronts on tiles of 32, three workgroups a CU, 117)
-constexpr int tile_waves_per_simd(int DP) { return DP > 64 ? 2 : 4; }
+// The cache: 8 wavefronts on tiles of 64 keys, one workgroup a CU, as the codes are unpacked once for all of them (chunks of 300 tokens behind
+// 6000, 32 heads of 128 over 8: 89 us; with 4 wavefronts on tiles of 32 and three workgroups a CU 117.  Heads of 64: 63 us, two workgroups a CU
+// with a register or two in memory 68).
+// States: tiles of 32, as many workgroups a CU as registers allow.  Heads of 64 need more loads on their way than two buffers hold: four (ViT-B's
+// attention, batch 128: 45 us with two, 41 with four); heads of 128, whose tile takes twice as long to multiply, gain nothing (prompts of 1000
+// over 2313 states: 126 us with two, 129 with three).
+constexpr int tile_waves_per_simd(bool kv4, int DP, bool masked) { return kv4 || DP == 256 ? 2 : DP == 64 ? 4 : masked ? 2 : 3; }
+constexpr int state_buffers(int DP) { return DP == 64 ? 4 : 2; }  // (a mask's bytes come one tile ahead of two buffers)
 
-template <bool KV4, int DP, int QT, int NW, int KT, bool MASKED>
-__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP)) attend_tiles_kernel(const AttendArgs a) {
+template <bool KV4, int DP, int QT, int NW, int KT, int NB, bool MASKED>
+__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED)) attend_tiles_kernel(const AttendArgs a) {
+  static_assert(NB == 2 || (NB == 4 && !KV4), "the waits for copies");
+  static_assert(!MASKED || NB == 2, "bytes of one tile");
+  static_assert(QT <= 2, "count below QT is 1 or 0");
   constexpr int J = DP / 32, CH = DP / 16, NT = 64 * NW, kTile = KT * kRow<DP>;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * 2 * kTile];  // [buffer][keys, values]
-  __shared__ __attribute__((aligned(4))) uint8_t seen[MASKED ? KT : 4];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[NB * 2 * kTile];  // [buffer][keys, values]
+  __shared__ __attribute__((aligned(16))) float begin[MASKED ? NB * KT : 4];
   __shared__ int pages[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
   Work w;
@@ -156,23 +186,30 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP)) attend_tiles
   const int cols = span.nq * a.rep, col_tiles = (cols + 15) >> 4, groups = (col_tiles + NW * QT - 1) / (NW * QT);
   if (w.block >= groups) return;
   const int tile0 = w.block * col_tiles / groups, tile1 = (w.block + 1) * col_tiles / groups;
-  const bool works = tile0 + wave < tile1;
   const int least = span.sees(16 * (tile0 + wave) / a.rep);
   const int last = 16 * tile1 < cols ? 16 * tile1 - 1 : cols - 1;
   const int most = span.sees(last / a.rep);
   const int first_key = w.part * a.part_tiles * 32, end_key = first_key + a.part_tiles * 32 < most ? first_key + a.part_tiles * 32 : most;
-  typedef typename std::conditional<KV4, Codes<DP, KT, NW>, States<DP, KT, NW>>::type Stage;
-  Stage stage(a, w, span.len, wave, lane, lds, first_key);
-  if (!KV4 && a.D < DP) {  // the pieces beyond the head: zeros, once
-    for (int i = threadIdx.x; i < 4 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
+  typedef typename std::conditional<KV4, Codes<DP, KT, NW>, States<DP, KT, NW, MASKED>>::type Stage;
+  Stage stage(a, w, span.len, wave, lane, lds, begin, first_key);
+  if (!KV4 && (MASKED || a.D < DP)) {  // the pieces beyond the head, and rows that are not copied: zeros, once
+    for (int i = threadIdx.x; i < NB * 2 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
     __syncthreads();
   }
-  if (first_key < end_key) stage.load(0, first_key);
+  if constexpr (KV4) {
+    if (first_key < end_key) stage.load(0, first_key);
+  } else {
+    if (MASKED && first_key < end_key) stage.look(first_key);
+#pragma unroll
+    for (int i = 0; i < NB - 1; ++i)
+      if (first_key + i * KT < end_key) stage.load(i, first_key + i * KT);
+    if (MASKED && first_key + KT < end_key) stage.look(first_key + KT);
+  }
   Columns<KV4, DP, QT> x;
   // (block i of a wavefront beyond the workgroup's last: columns that are no columns)
   x.load(a, span, w.kh, g, r, [&](int i) { return tile0 + wave + NW * i < tile1 ? 16 * (tile0 + wave + NW * i) : cols; });
   // The queries are waited for here: their first use is inside the loop, where the compiler, which does not know of the copies to LDS, would
-  // wait for all of these as well.  (165 us for what takes 137 with the wait here.)
+  // wait for all of these as well, in every turn.
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
 
   // this lane's key operands and value operands: pieces by their places
@@ -182,31 +219,31 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP)) attend_tiles
 #pragma unroll
   for (int t = 0; t < CH; ++t) {
     const int row = 4 * g + (r >> 2);
-    value_at[t] = kTile + row * kRow<DP> + place<DP>(row, 2 * t + (r >> 1 & 1)) * 16 + (r & 1) * 8;
+    value_at[t] = kTile + row * kRow<DP> + place<DP>(row, 2 * t + ((r & 3) >> 1)) * 16 + (r & 1) * 8;
   }
 
-  auto multiply = [&](int buf, int key0, bool there) {
+  auto multiply = [&](auto blocks, int buf, int key0, bool there) {
+    constexpr int N = decltype(blocks)::value;
     const uint8_t* tile = lds + buf * 2 * kTile;
 #pragma unroll
     for (int half = 0; half < KT / 32; ++half) {
-      f4 s[QT][2] = {};
+      f4 s[N][2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const f4 begins = MASKED ? *(const f4*)&begin[buf * KT + 32 * half + 16 * t + 4 * g] : f4(0);
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i][t] = begins;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
           const h8 k = *(const h8*)(tile + key_at[j] + (2 * half + t) * 16 * kRow<DP>);
 #pragma unroll
-          for (int i = 0; i < QT; ++i) s[i][t] = mfma16(k, x.q[i][j], s[i][t]);
+          for (int i = 0; i < N; ++i) s[i][t] = mfma16(k, x.q[i][j], s[i][t]);
         }
-      h8 p[QT];
-      const int at = key0 + 32 * half + 4 * g;
-      unsigned shown[2] = {~0u, ~0u};
-      if constexpr (MASKED) {
-        shown[0] = *(const unsigned*)&seen[32 * half + 4 * g];
-        shown[1] = *(const unsigned*)&seen[32 * half + 16 + 4 * g];
       }
-      if (MASKED || !there || key0 + 32 * half + 32 > least) x.hide(s, [&](int i, int t, int e) { return (shown[t] >> (8 * e) & 1) == 0 || at + 16 * t + e >= (there ? x.limit[i] : 0); });
-      x.template follow<false>(s, a.c, p);
+      h8 p[N];
+      const int at = key0 + 32 * half + 4 * g;
+      if (!MASKED && (!there || key0 + 32 * half + 32 > least)) x.hide(s, [&](int i, int t, int e) { return at + 16 * t + e >= (there ? x.limit[i] : 0); });
+      x.follow(s, a);
       x.weights(s, a.c, p);
       x.sum(p);
 #pragma unroll
@@ -214,67 +251,76 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(DP)) attend_tiles
         const h4 v0 = read_transposed(tile + value_at[t] + 32 * half * kRow<DP>), v1 = read_transposed(tile + value_at[t] + (32 * half + 16) * kRow<DP>);
         const h8 v = __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int i = 0; i < QT; ++i) x.o[i][t] = mfma16(v, p[i], x.o[i][t]);
+        for (int i = 0; i < N; ++i) x.o[i][t] = mfma16(v, p[i], x.o[i][t]);
       }
     }
   };
 
-  if constexpr (KV4) {
-    auto put = [&](int buf) {
-      stage.write(lds + buf * 2 * kTile, lds + buf * 2 * kTile + kTile);
-      if (threadIdx.x == 0) pages[buf] = stage.there;
-    };
-    if (first_key < end_key) {
-      put(0);
-      if (first_key + KT < end_key) stage.load(0, first_key + KT);
-    }
+  // The loop over the tiles for N blocks of columns: wavefronts meet at its barriers, whichever of its copies they are in.
+  auto run = [&](auto blocks) {
     int buf = 0;
-    for (int key0 = first_key; key0 < end_key; key0 += KT) {
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (loads for registers stay in flight)
-      // the next tile, whose words have had the time of the one before, goes to LDS first: nobody waits for the writes at the next barrier
-      const bool there = pages[buf] != 0;
-      if (key0 + KT < end_key) {
-        put(buf ^ 1);
-        if (key0 + 2 * KT < end_key) stage.load(0, key0 + 2 * KT);
+    if constexpr (KV4) {
+      auto put = [&](int to) {
+        stage.write(lds + to * 2 * kTile, lds + to * 2 * kTile + kTile);
+        if (threadIdx.x == 0) pages[to] = stage.there;
+      };
+      if (first_key < end_key) {
+        put(0);
+        if (first_key + KT < end_key) stage.load(0, first_key + KT);
       }
-      if (works) multiply(buf, key0, there);
-      buf ^= 1;
-    }
-  } else {
-    int buf = 0;
-    for (int key0 = first_key; key0 < end_key; key0 += KT) {
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");  // this tile is there, and nobody reads the other buffer
-      if (key0 + KT < end_key) stage.load(buf ^ 1, key0 + KT);
-      if constexpr (MASKED) {
-        // what is not seen may hold anything: 0 times it would not be 0
-        uint8_t* values = lds + buf * 2 * kTile + kTile;
-        const uint8_t* mask = a.mask + (int64_t)w.b * a.kv_len;
-        for (int i = threadIdx.x; i < KT * DP / 8; i += NT) {
-          const int row = i / (DP / 8);
-          const bool see = key0 + row < span.len && mask[key0 + row] != 0;
-          if (!see) *(u4*)(values + i * 16) = u4(0);
-          if (i % (DP / 8) == 0) seen[row] = see;
+      for (int key0 = first_key; key0 < end_key; key0 += KT) {
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (loads for registers stay in flight)
+        // the next tile, whose words have had the time of the one before, goes to LDS first: nobody waits for the writes at the next barrier
+        const bool there = pages[buf] != 0;
+        if (key0 + KT < end_key) {
+          put(buf ^ 1);
+          if (key0 + 2 * KT < end_key) stage.load(0, key0 + 2 * KT);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if constexpr (decltype(blocks)::value > 0) multiply(blocks, buf, key0, there);
+        buf ^= 1;
       }
-      if (works) multiply(buf, key0, true);
-      buf ^= 1;
+    } else {
+      for (int key0 = first_key; key0 < end_key; key0 += KT) {
+        // this tile is there (of the wavefront's own copies, which come back in order, only later tiles' are left), and nobody reads the buffer of
+        // the one before it
+        const int later = (end_key - key0 - 1) / KT;
+        if (NB == 4 && later >= 2)
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(4 * Stage::COPIES) : "memory");
+        else if (NB == 4 && later >= 1)
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * Stage::COPIES) : "memory");
+        else
+          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (key0 + (NB - 1) * KT < end_key) {
+          stage.load(buf == 0 ? NB - 1 : buf - 1, key0 + (NB - 1) * KT);
+          if (MASKED && key0 + NB * KT < end_key) stage.look(key0 + NB * KT);
+        }
+        if constexpr (decltype(blocks)::value > 0) multiply(blocks, buf, key0, true);
+        buf = buf + 1 < NB ? buf + 1 : 0;
+      }
     }
-  }
-  if (works) x.store(a, w.part, g);
+  };
+  // a wavefront whose last block is none leaves it out
+  const int count = tile1 - tile0 - wave > 0 ? (tile1 - tile0 - wave + NW - 1) / NW : 0;
+  if (count == QT)
+    run(std::integral_constant<int, QT>());
+  else if (count == 1)
+    run(std::integral_constant<int, 1>());
+  else
+    run(std::integral_constant<int, 0>());
+  if (count > 0) x.store(a, w.part, g);
 }
 
-template <bool KV4, int DP, int QT, int NW, int KT>
+template <bool KV4, int DP, int QT, int NW, int KT, int NB>
 void launch_shape(AttendArgs a, hipStream_t s) {
   a.col_blocks = (int)ceil_div((int64_t)a.q_len * a.rep, 16 * QT * NW);
   const unsigned blocks = Work::workgroups(a);
   if constexpr (!KV4) {
     if (a.mask != nullptr) {
-      attend_tiles_kernel<KV4, DP, QT, NW, KT, true><<<blocks, 64 * NW, 0, s>>>(a);
+      attend_tiles_kernel<KV4, DP, QT, NW, KT, 2, true><<<blocks, 64 * NW, 0, s>>>(a);
       return;
     }
   }
-  attend_tiles_kernel<KV4, DP, QT, NW, KT, false><<<blocks, 64 * NW, 0, s>>>(a);
+  attend_tiles_kernel<KV4, DP, QT, NW, KT, NB, false><<<blocks, 64 * NW, 0, s>>>(a);
 }
 
 }  // namespace
@@ -282,9 +328,10 @@ void launch_shape(AttendArgs a, hipStream_t s) {
 void launch_attend_tiles(bool kv4, AttendArgs a, hipStream_t s) {
   const int DP = padded_head(a.D);
   if (kv4)
-    DP == 64 ? launch_shape<true, 64, 2, 8, 64>(a, s) : DP == 128 ? launch_shape<true, 128, 2, 8, 64>(a, s) : launch_shape<true, 256, 1, 8, 64>(a, s);
+    DP == 64 ? launch_shape<true, 64, 2, 8, 64, 2>(a, s) : DP == 128 ? launch_shape<true, 128, 2, 8, 64, 2>(a, s) : launch_shape<true, 256, 1, 8, 64, 2>(a, s);
   else
-    DP == 64 ? launch_shape<false, 64, 2, 4, 32>(a, s) : DP == 128 ? launch_shape<false, 128, 2, 4, 32>(a, s) : launch_shape<false, 256, 1, 4, 32>(a, s);
+    DP == 64 ? launch_shape<false, 64, 2, 4, 32, state_buffers(64)>(a, s)
+    : DP == 128 ? launch_shape<false, 128, 2, 4, 32, state_buffers(128)>(a, s) : launch_shape<false, 256, 1, 4, 32, state_buffers(256)>(a, s);
 }
 
 }  // namespace gpusq
