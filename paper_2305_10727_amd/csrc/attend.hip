@@ -339,15 +339,18 @@ void launch_shape(AttendArgs a, hipStream_t s) {
   attend_few_kernel<KV4, DP, QT, WK, false><<<blocks, 64 * WK, 0, s>>>(a);
 }
 
+// The columns of a workgroup.  (Two blocks of heads of 256 do not fit the registers of a wavefront.)
+int few_columns(int64_t cols, int DP) { return cols <= 16 || DP == 256 ? 16 : 32; }
+
 template <bool KV4, int DP>
 void launch_head(const AttendArgs& a, hipStream_t s) {
   const int64_t cols = (int64_t)a.q_len * a.rep;
-  if (cols <= 16)
-    launch_shape<KV4, DP, 1, 8>(a, s);
-  else if (cols <= kFewColumns || !tiles_reach(KV4, a))
-    launch_shape<KV4, DP, 2, 4>(a, s);
-  else
+  if (cols > kFewColumns && tiles_reach(KV4, a))
     launch_attend_tiles(KV4, a, s);
+  else if (few_columns(cols, DP) == 16)
+    launch_shape<KV4, DP, 1, 8>(a, s);
+  else if constexpr (DP < 256)
+    launch_shape<KV4, DP, 2, 4>(a, s);
 }
 
 }  // namespace
@@ -358,7 +361,7 @@ void launch_head(const AttendArgs& a, hipStream_t s) {
 AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys) {
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
   const bool few = cols <= kFewColumns;
-  const int64_t groups = batch * kv_heads * ceil_div(cols, few ? (cols <= 16 ? 16 : 32) : tiles_columns(kv4, padded_head((int)head_dim)));
+  const int64_t groups = batch * kv_heads * ceil_div(cols, few ? few_columns(cols, padded_head((int)head_dim)) : tiles_columns(kv4, padded_head((int)head_dim)));
   int64_t parts = few ? ceil_div(256, groups) : (kv4 ? 256 : 512) / groups;
   const int64_t most = ceil_div(tiles, few ? 32 : 16);
   parts = parts < 1 ? 1 : parts < most ? parts : most;
