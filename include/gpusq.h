@@ -411,7 +411,8 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
  * k, v [batch][kv_len][kv_heads], vectors of head_dim fp16 values, each dimension with a stride of its own in values (a multiple of 8,
  * GPUSQ_ERR_ALIGN; not negative), so that heads may lie in a packed projection or apart.
  *   kv_lens (or NULL): keys of batch b beyond kv_lens[b] are not seen; key_mask (or NULL) [batch][kv_len] bytes: keys of a 0 are not seen.
- *   What is not seen may hold anything, NaN included.  scale, out [batch][q_len][heads][head_dim] and workspace as above. */
+ *   What is not seen may hold anything, NaN included; a channel with an infinity among the values seen is infinite or NaN.
+ *   scale, out [batch][q_len][heads][head_dim] and workspace as above. */
 size_t gpusq_cross_attention_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads, int64_t head_dim);
 gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, const int32_t* kv_lens, const uint8_t* key_mask, void* out,
                                    void* workspace, int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads,

@@ -257,6 +257,59 @@ def test_long_states_are_cut_and_joined(g):
         _check(y, *_cross_expected(q, k, v, seen, D ** -0.5))
 
 
+# many columns of every padding, histories and states cut into parts; what no key leaves anything for, a whole part among it
+@pytest.mark.parametrize("D", [64, 128, 200])
+def test_many_queries_over_parts(g, D):
+    counts, lens, H, G = [90, 40], [2100, 90], 4, 1
+    assert g.lib().gpusq_attention_kv4_workspace_bytes(sum(counts), 2, 90, -(-2100 // 64), H, G, D) > 0
+    c = _Cache(lens, G, D, seed=31)
+    q = np.random.default_rng(32).standard_normal((sum(counts), H, D)).astype(np.float16)
+    _check(_run(g, c, q, counts), *c.expected(q, counts, D ** -0.5))
+    B, Tq, S = 2, 45, 1500
+    assert g.lib().gpusq_cross_attention_workspace_bytes(B, Tq, S, H, G, D) > 0
+    q, k, v = _normal(33, B, Tq, H, D), _normal(34, B, S, G, D), _normal(35, B, S, G, D)
+    bytes_ = (np.random.default_rng(36).random((B, S)) < 0.5).astype(np.uint8)
+    bytes_[0, :700], bytes_[1, 400:] = 0, 0
+    lens = np.array([1203, 1500], np.int32)
+    for use_lens, use_bytes in ((False, False), (True, False), (False, True), (True, True)):
+        seen = np.ones((B, S), bool)
+        if use_lens:
+            seen &= np.arange(S)[None] < lens[:, None]
+        if use_bytes:
+            seen &= bytes_ != 0
+        a, b = (np.where(seen[..., None, None], x, np.float16(np.nan)) for x in (k, v))
+        y = g.cross_attention(dev(q), dev(a), dev(b), kv_lens=dev(lens) if use_lens else None, key_mask=dev(bytes_) if use_bytes else None)
+        _check(y, *_cross_expected(q, np.where(seen[..., None, None], k, 0), np.where(seen[..., None, None], v, 0), seen, D ** -0.5))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("Tq", [10, 90])
+def test_masks_that_hide_whole_tiles(g, D, Tq):
+    """Keys seen only at the end, at the beginning, one here and there, none: hidden ones hold NaN"""
+    B, S, H = 4, 230, 2
+    seen = np.zeros((B, S), bool)
+    seen[0, 200:], seen[1, :3], seen[2, [0, 63, 64, 129, 229]] = True, True, True
+    q, k, v = _normal(41, B, Tq, H, D), _normal(42, B, S, 1, D), _normal(43, B, S, 1, D)
+    y = g.cross_attention(dev(q), *(dev(np.where(seen[..., None, None], x, np.float16(np.nan))) for x in (k, v)), key_mask=dev(seen))
+    _check(y, *_cross_expected(q, k, v, seen, D ** -0.5))
+    assert not host(y)[3].any()
+
+
+def test_states_far_apart(g):
+    """A stride of 2^24 values from token to token, for few queries and many"""
+    S, D = 40, 64
+    big = torch.zeros(S * 2**24, dtype=torch.float16, device="cuda")
+    far = big.as_strided((1, S, 1, D), (0, 2**24, D, 1))
+    k, v = _normal(51, 1, S, 1, D), _normal(52, 1, S, 1, D)
+    far.copy_(dev(k))
+    for Tq in (3, 50):
+        q = _normal(53, 1, Tq, 2, D)
+        exp, off = _cross_expected(q, k, v, np.ones((1, S), bool), D ** -0.5)
+        _check(g.cross_attention(dev(q), far, dev(v)), exp, off)
+        exp, off = _cross_expected(q, v, k, np.ones((1, S), bool), D ** -0.5)
+        _check(g.cross_attention(dev(q), dev(v), far), exp, off)
+
+
 def test_infinite_and_nan_operands_keep_to_their_rows(g):
     q, k, v = _normal(7, 1, 40, 2, 64), _normal(8, 1, 70, 2, 64), _normal(9, 1, 70, 2, 64)
     clean = host(g.cross_attention(dev(q), dev(k), dev(v)))

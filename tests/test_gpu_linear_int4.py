@@ -71,6 +71,44 @@ def test_product(g, M, N, K, group):
         _check(host(y), X, codes, scales, group, bias if use_bias else None, gelu, K)
 
 
+# K beyond what a wavefront keeps of its rows at once, for each number of rows, and at the edges of what it keeps
+@pytest.mark.parametrize("M", [1, 16, 17, 33])
+@pytest.mark.parametrize("K,group", [(2048, 128), (2112, 64), (4096, 32), (4224, 128), (6144, 64), (6176, 32), (8192, 32), (8320, 128), (16512, 64)])
+def test_long_rows(g, M, K, group):
+    N = 36
+    codes, scales = _weights(N, K, group, M + K)
+    r = np.random.default_rng(M)
+    X, bias = r.standard_normal((M, K)).astype(np.float16), r.standard_normal(N).astype(np.float32)
+    packed = g.pack_int4_groups(dev(codes), dev(scales), group)
+    for gelu, dt in ((False, torch.float16), (True, torch.float32)):
+        y = g.linear_int4(dev(X), packed, N, group, bias=dev(bias), gelu=gelu, out_dtype=dt)
+        _check(host(y), X, codes, scales, group, bias, gelu, K)
+
+
+# so many channels that a workgroup has several tiles of them; more than LDS has sums for
+@pytest.mark.parametrize("M,N,K,group", [(1, 12308, 256, 128), (17, 12308, 160, 32), (3, 4500, 8448, 128), (40, 33000, 2176, 64)])
+def test_many_channels(g, M, N, K, group):
+    r = np.random.default_rng(M)
+    codes = r.integers(-8, 8, (N, K), dtype=np.int8)
+    scales = (r.uniform(0.5, 2, (N, K // group)) * 0.01).astype(np.float16)
+    X, bias = r.standard_normal((M, K)).astype(np.float16), r.standard_normal(N).astype(np.float32)
+    y = host(g.linear_int4(dev(X), g.pack_int4_groups(dev(codes), dev(scales), group), N, group, bias=dev(bias)))
+    some = np.unique(np.concatenate([np.arange(20), r.integers(0, N, 400), np.arange(N - 200, N)]))
+    _check(y[:, some], X, codes[some], scales[some], group, bias[some], False, K)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.float32])
+def test_gelu_of_large_values(g, dt):
+    """Far beyond where it is the identity or 0, and infinite"""
+    N, K = 8, 32
+    codes = np.ones((N, K), np.int8)
+    packed = g.pack_int4_groups(dev(codes), dev(np.ones((N, 1), np.float16)), 32)
+    X = np.zeros((6, K), np.float16)
+    X[:, 0] = 30000, -30000, 12, -12, np.inf, 0
+    y = host(g.linear_int4(dev(X), packed, N, 32, gelu=True, out_dtype=dt)).astype(np.float64)  # (1e-30 in fp16 would be 0)
+    assert (y[0] == 30000).all() and (y[1] == 0).all() and (y[2] == 12).all() and (np.abs(y[3]) < 1e-30).all() and (y[4] == np.inf).all() and (y[5] == 0).all()
+
+
 def test_scales_of_every_size(g):
     """subnormal, huge and zero scales: the sums of a group meet them in 32 bits"""
     N, K, group = 32, 512, 32
