@@ -1,6 +1,9 @@
 // Attention of few queries to keys and values of another length: over the paged 4-bit cache (attention_kv4) and over an encoder's fp16
 // states (cross_attention).  A workgroup's wavefronts have the same columns and deal out the keys: what bounds such a call is the keys'
 // bytes, so they go from memory straight into the registers of the one wavefront that multiplies them.
+// Over the cache, one new token, 32 heads of 128 over 8: 131071 tokens (151 MB) in 37 us with the join, 4.0 TB/s; 64 sequences of up to 4096
+// (191 MB) 48 us, 4.0 TB/s.  A large copy has 5.0.  One token to the 257 states of an image, 16 heads of 80: 5.7 us, a launch and four trips
+// to memory (queries and first keys, second keys, the sums through LDS, the output).
 #include "attend.h"
 
 namespace gpusq {
@@ -357,7 +360,7 @@ void launch_head(const AttendArgs& a, hipStream_t s) {
 
 // The keys are cut into parts where the (batch, key head, block of columns) are too few workgroups for the device, of 32 tiles (1024 keys)
 // at least for few columns, of 16 for many.
-// Few columns: 256 workgroups, one a CU (8 key heads, 131071 tokens: 38.9 us; 512 39.7, 1024 45, 2048 55).
+// Few columns: 256 workgroups, one a CU (8 key heads, 131071 tokens: 37.4 us; 512 workgroups 38.0, 1024 42.7).
 AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys) {
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
   const bool few = cols <= kFewColumns;

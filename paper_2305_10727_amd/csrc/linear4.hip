@@ -9,6 +9,8 @@
 //   - codes are turned into fp16 integers, exact, and the products of a group summed in 32 bits before its scale, in 32 bits too,
 //     multiplies the sum: nothing is rounded before the output, whatever the scales;
 //   - a workgroup's wavefronts share its channels and deal out the steps of K; their sums meet in LDS once, at the end.
+// 5120 -> 13824 with GELU for one row (36.6 MB): 10.5 us, 3.5 TB/s; 8192 -> 24576 for 13 rows (109 MB): 26 us, 4.2 TB/s; a large copy has 5.0.
+// 1024 -> 1024 for one row: 3.1 us, a launch and three trips to memory.
 #include "epilogue.h"
 #include "kv4.h"
 

@@ -7,6 +7,8 @@
 // of channels: the quads that turn with each other (4 i .. and R / 2 + 4 i .., or 8 i .. + 7 where pairs are neighbours), so that the
 // rotation stays inside the lane and both ways of pairing read the same four cosines and sines.  Statistics are in 32 bits, and so is
 // everything up to the one rounding of a result (fp16, or the codes of the cache).
+// Queries and keys of 128 images of 257 tokens, 16 heads of 80: 337 MB in 78 us, 4.3 TB/s where a large copy has 5.0.  509 tokens of 32 + 8 + 8
+// heads of 128 into the cache: 6.3 us, 3.5 for one token: a launch and three trips to memory (slots and positions, rows, stores).
 #include "kv4.h"
 
 namespace gpusq {
@@ -205,7 +207,7 @@ gpusq_status launch_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_st
                                  const float* q_weight, const float* k_weight, float eps, const float* cos, const float* sin, const int32_t* positions,
                                  int64_t table_rows, int64_t R, int interleaved, void* q_out, void* k_out, void* v_out, void* cache, const int32_t* slots,
                                  int64_t num_pages, hipStream_t s) {
-  const int64_t per_token = heads + kv_heads + (cache != nullptr ? kv_heads : 0), most = INT32_MAX / per_token;
+  const int64_t per_token = heads + kv_heads + (cache != nullptr ? kv_heads : 0), most = (INT32_MAX - 256) / per_token;  // (a last workgroup's count stays in range)
   unsigned bits = 1;  // per_token >= 2
   while ((int64_t)1 << bits < per_token) ++bits;
   const unsigned magic = (unsigned)(((uint64_t)1 << (31 + bits)) / per_token + 1);
