@@ -304,26 +304,37 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict
   }
 }
 
-// Few parts: a thread for four channels of a row
-constexpr int kFewParts = 16;
+// Few parts: a thread for four channels of a row.  The maxima are requested side by side, and so are the sums, four parts at a time.
+constexpr int kFewParts = 8;
 __global__ void __launch_bounds__(256) join_few_parts_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml, _Float16* __restrict__ out, int64_t rows,
                                                               int D, int parts) {
   const int quads = D / 4, at = threadIdx.x / quads, quad = threadIdx.x - at * quads;
   const int64_t row = (int64_t)blockIdx.x * (256 / quads) + at;
   if (at >= 256 / quads || row >= rows) return;
   typedef float f2 __attribute__((ext_vector_type(2)));
-  float top = -__builtin_inff();
-  for (int p = 0; p < parts; ++p) top = fmaxf(top, part_ml[2 * (p * rows + row)]);
+  f2 ml[kFewParts];
+#pragma unroll
+  for (int p = 0; p < kFewParts; ++p)
+    ml[p] = p < parts ? *(const f2*)(part_ml + 2 * (p * rows + row)) : f2{-__builtin_inff(), 0.0f};
+  float top = ml[0][0];
+#pragma unroll
+  for (int p = 1; p < kFewParts; ++p) top = fmaxf(top, ml[p][0]);
   float l = 0.0f;
   f4 o = f4(0);
-#pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const f2 ml = *(const f2*)(part_ml + 2 * (p * rows + row));
-    const f4 v = *(const f4*)(part_o + (p * rows + row) * D + 4 * quad);
-    if (ml[0] == -__builtin_inff()) continue;  // without a visible key: its sums may not be there
-    const float f = __builtin_amdgcn_exp2f(ml[0] - top);
-    l += ml[1] * f;
-    o += v * f;
+#pragma unroll
+  for (int p0 = 0; p0 < kFewParts; p0 += 4) {
+    if (p0 >= parts) break;
+    f4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = *(const f4*)(part_o + ((p0 + i < parts ? p0 + i : parts - 1) * rows + row) * D + 4 * quad);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f2 x = ml[p0 + i];
+      const bool none = x[0] == -__builtin_inff();  // a part without a visible key: its sums may not be there
+      const float f = none ? 0.0f : __builtin_amdgcn_exp2f(x[0] - top);
+      l += none ? 0.0f : x[1] * f;
+      o += none ? f4(0) : v[i] * f;
+    }
   }
   const float r = l == 0.0f ? 0.0f : 1.0f / l;
   *(h4*)(out + row * D + 4 * quad) = h4{(_Float16)(o[0] * r), (_Float16)(o[1] * r), (_Float16)(o[2] * r), (_Float16)(o[3] * r)};
@@ -358,15 +369,19 @@ void launch_head(const AttendArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// The keys are cut into parts where the (batch, key head, block of columns) are too few workgroups for the device, of 32 tiles (1024 keys)
-// at least for few columns, of 16 for many.
-// Few columns: 256 workgroups, one a CU (8 key heads, 131071 tokens: 37.4 us; 512 workgroups 38.0, 1024 42.7).
+// The keys are cut into parts where the (batch, key head, block of columns) are too few workgroups for the device.
+// Few columns: 256 workgroups, one a CU (8 key heads, 131071 tokens: 37.4 us; 512 workgroups 38.0, 1024 42.7), with 8 tiles (256 keys) each or
+// more: a tile for each wavefront.  (One token, in one piece and in parts: of 32 heads over 8 of 128 after 8000 tokens 10.5 in 32 parts, 12.8 in 8;
+// 16 heads of 128 to 1000 states 12.3 and 8.6, of 256 24 and 13.)  What one piece does in 8.5 us stays one, as the second launch and the workspace
+// take the host 4: 1024 keys at most, over the cache 128K channels of keys, over states 64K (16 heads of 64, 1000 states: 8.3 and 7.2).
+// Many columns: parts of 16 tiles at least.
 AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys) {
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
   const bool few = cols <= kFewColumns;
   const int64_t groups = batch * kv_heads * ceil_div(cols, few ? few_columns(cols, padded_head((int)head_dim)) : tiles_columns(kv4, padded_head((int)head_dim)));
   int64_t parts = few ? ceil_div(256, groups) : (kv4 ? 256 : 512) / groups;
-  const int64_t most = ceil_div(tiles, few ? 32 : 16);
+  const int64_t one = (kv4 ? 4096 : 2048) / padded_head((int)head_dim);
+  const int64_t most = !few ? ceil_div(tiles, 16) : tiles <= (one < 32 ? one : 32) ? 1 : ceil_div(tiles, 8);
   parts = parts < 1 ? 1 : parts < most ? parts : most;
   if (parts > kMostParts) parts = kMostParts;
   AttendParts p;
