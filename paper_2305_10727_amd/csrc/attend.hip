@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict
   if ((tid & 63) == 0) wave_max[tid >> 6] = top;
   __syncthreads();
   top = fmaxf(fmaxf(wave_max[0], wave_max[1]), fmaxf(wave_max[2], wave_max[3]));
-  const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - top);  // a part without a visible key: its sums may not be there
+  const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - top);  // a part without a visible key (scores that are no numbers: 0 times its sum is NaN)
   weight[tid] = f;
   l *= f;
 #pragma unroll
@@ -330,7 +330,8 @@ __global__ void __launch_bounds__(256) join_few_parts_kernel(const float* __rest
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f2 x = ml[p0 + i];
-      const bool none = x[0] == -__builtin_inff();  // a part without a visible key: its sums may not be there
+      // a part without a visible key (one whose scores are no numbers has no maximum either, but its sum is NaN, and has to be the row's)
+      const bool none = x[0] == -__builtin_inff() && x[1] == 0.0f;
       const float f = none ? 0.0f : __builtin_amdgcn_exp2f(x[0] - top);
       l += none ? 0.0f : x[1] * f;
       o += none ? f4(0) : v[i] * f;

@@ -370,3 +370,48 @@ def test_refusals(g):
             g.cross_attention(**{**ok, **change})
     with pytest.raises(g.GpusqError):
         g.cross_attention(f16(1, 1, 1, 264), f16(1, 1, 1, 264), f16(1, 1, 1, 264))
+
+
+def _repeated(table, batch):
+    return dev(np.repeat(table, batch, 0))
+
+
+# how many sequences leave room for so many parts (few queries, many queries to states, many over the cache)
+PARTS = {1: (256, 300, 200), 2: (128, 200, 100), 8: (32, 64, 32), 9: (29, 56, 28)}
+
+
+@pytest.mark.parametrize("parts", sorted(PARTS))
+@pytest.mark.parametrize("Tq", [1, 40])
+def test_a_query_that_is_no_number_stays_one_over_parts(g, parts, Tq):
+    """Keys in one piece, in few parts and in many: a query with a NaN has no answer in any, and the others have theirs; keys that are no
+    numbers in one part only leave no query an answer"""
+    S, D = 4608, 64
+    B = PARTS[parts][0 if Tq == 1 else 1]
+    assert g.lib().gpusq_cross_attention_workspace_bytes(B, Tq, S, 1, 1, D) == (parts > 1) * parts * B * Tq * (D + 2) * 4
+    q, k, v = _normal(61, B, Tq, 1, D), _normal(62, 1, S, 1, D), _normal(63, 1, S, 1, D)
+    whole = lambda x: dev(x).expand(B, S, 1, D)  # noqa: E731
+    clean = host(g.cross_attention(dev(q), whole(k), whole(v)))
+    broken = q.copy()
+    broken[1, 0, 0, 5] = np.nan
+    y = host(g.cross_attention(dev(broken), whole(k), whole(v)))
+    assert np.isnan(y[1, 0]).all()
+    assert np.array_equal(np.delete(y, 1, 0), np.delete(clean, 1, 0))
+    exp, off = _cross_expected(q[1:2, 1:], k, v, np.ones((1, S), bool), D ** -0.5)
+    assert (np.abs(y[1:2, 1:] - exp) <= off).all()
+    k[:, -(S // parts):] = np.nan
+    assert np.isnan(host(g.cross_attention(dev(q), whole(k), whole(v)))).all()
+
+    B = PARTS[parts][0 if Tq == 1 else 2]
+    assert g.lib().gpusq_attention_kv4_workspace_bytes(B * Tq, B, Tq, S // 64, 1, 1, D) == (parts > 1) * parts * B * Tq * (D + 2) * 4
+    c = _Cache([S], 1, D, seed=64)
+    args = dev(c.pages), _repeated(c.table, B), dev(np.full(B, S, np.int32))
+    q = _normal(65, B * Tq, 1, D)
+    clean = host(g.attention_kv4(dev(q), *args, max_q=Tq))
+    broken = q.copy()
+    broken[Tq, 0, 5] = np.nan
+    y = host(g.attention_kv4(dev(broken), *args, max_q=Tq))
+    assert np.isnan(y[Tq]).all()
+    rest = np.delete(np.arange(B * Tq), np.arange(Tq, 2 * Tq))
+    assert np.array_equal(y[rest], clean[rest])
+    exp, off = c.expected(q[Tq:2 * Tq], [Tq], D ** -0.5)
+    assert (np.abs(y[Tq + 1:2 * Tq] - exp[1:]) <= off[1:]).all()
