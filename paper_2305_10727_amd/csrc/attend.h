@@ -13,6 +13,7 @@
 // P is rounded to fp16 for the matrix instruction (the one rounding between the scores and the output); its sum is that of the rounded
 // values, in 32 bits, one matrix instruction with a first operand of ones instead of 8 additions a lane.
 #pragma once
+#include "attend_plan.h"
 #include "kv4.h"
 
 namespace gpusq {

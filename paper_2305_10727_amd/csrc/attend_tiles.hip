@@ -188,7 +188,8 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
   // blocks of 16 columns, dealt out evenly over the workgroups that they need and then over the wavefronts
   const int cols = span.nq * a.rep, col_tiles = (cols + 15) >> 4, groups = (col_tiles + NW * QT - 1) / (NW * QT);
   if (w.block >= groups) return;
-  const int tile0 = w.block * col_tiles / groups, tile1 = (w.block + 1) * col_tiles / groups;
+  const ColumnShare share = column_share(col_tiles, groups, w.block);
+  const int tile0 = share.first, tile1 = share.last;
   const int least = span.sees(16 * (tile0 + wave) / a.rep);
   const int last = 16 * tile1 < cols ? 16 * tile1 - 1 : cols - 1;
   const int most = span.sees(last / a.rep);

@@ -1,12 +1,14 @@
 """Host-only checks of the decoder's operators: arguments that are refused before anything is launched, sizes of buffers, the places of the
 4-bit formats.  No kernel is launched here."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
 
 import decoder_reference as ref
-from test_abi_host import lib  # noqa: F401
+from test_abi_host import ROOT, lib  # noqa: F401
 
 OK, ERR_NULL, ERR_SHAPE, ERR_ALIGN, ERR_UNSUPPORTED = range(5)
 P, ODD = 0x10000, 0x10008  # never dereferenced: every call below fails validation first
@@ -131,3 +133,14 @@ def test_formats_read_back():
         assert np.array_equal(K, exp) and np.array_equal(V, -exp)
         assert np.array_equal(exp.astype(np.float16).astype(np.float64), exp)  # fp16 numbers
         assert (np.abs(exp - x) <= 0.56 * s.astype(np.float64).repeat(32, -1)[..., :D]).all()
+
+
+def test_plans_of_attention(tmp_path):
+    """Who takes which columns of an attention, walked on the host with the code the kernels read it with (attend_plan_walk.cpp)"""
+    exe = str(tmp_path / "walk")
+    build = subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-Werror", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                            "-I", os.path.join(ROOT, "paper_2305_10727_amd", "csrc"), os.path.join(ROOT, "tests", "attend_plan_walk.cpp"), "-o", exe],
+                           capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and run.stdout == "ok\n", run.stdout

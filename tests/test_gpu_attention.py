@@ -415,3 +415,26 @@ def test_a_query_that_is_no_number_stays_one_over_parts(g, parts, Tq):
     assert np.array_equal(y[rest], clean[rest])
     exp, off = c.expected(q[Tq:2 * Tq], [Tq], D ** -0.5)
     assert (np.abs(y[Tq + 1:2 * Tq] - exp[1:]) <= off[1:]).all()
+
+
+def test_columns_whose_products_pass_32_bits(g):
+    """Three million columns of one key head: every row is answered, from its own query"""
+    n, H, D, S = 47000, 64, 64, 40
+    c = _Cache([S], 1, D, seed=66)
+    q = torch.randn((n, H, D), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").half()
+    out = torch.full((n, H, D), 7, dtype=torch.float16, device="cuda")
+    g.attention_kv4(q, dev(c.pages), dev(c.table), dev(np.array([S], np.int32)), max_q=n, out=out)
+    exp, off = c.expected(host(q[-S:]), [S], D ** -0.5)  # the last queries see the tokens, those before them nothing
+    _check(out[-S:], exp, off)
+    assert not out[:-S].any()
+    k, v = _normal(67, 1, S, 1, D), _normal(68, 1, S, 1, D)
+    out.fill_(7)
+    g.cross_attention(q[None], dev(k), dev(v), out=out[None])
+    K, V = dev(k)[0, :, 0].double(), dev(v)[0, :, 0].double()
+    for a in range(0, n, 4700):  # the bounds of decoder_reference.attend
+        x = q[a:a + 4700].double().view(-1, D)
+        w = torch.softmax(x @ K.t().contiguous() * D ** -0.5, 1)
+        delta = 2 * D * 2.0 ** -24 * D ** -0.5 * (x.abs() @ K.abs().t().contiguous())
+        y = w @ V
+        off = (w * (2.0 ** -11 + 2.0 ** -20 + delta + (w * delta).sum(1, keepdim=True))) @ V.abs() + 2.0 ** -31 * V.abs().sum(0) + 2.0 ** -11 * y.abs() + 2.0 ** -24
+        assert ((out[a:a + 4700].double().view(-1, D) - y).abs() <= off).all()
