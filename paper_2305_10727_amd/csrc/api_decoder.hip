@@ -1,6 +1,7 @@
 // C ABI of the decoder's operators: argument validation, status codes, dispatch to the kernels.  No computation happens here.
 #include <math.h>
 
+#include "attend_plan.h"
 #include "kv4.h"
 
 using namespace gpusq;
@@ -136,7 +137,7 @@ gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, 
   if (!q || !k || !v || !out) return GPUSQ_ERR_NULL;
   gpusq_status st = check_heads(heads, kv_heads, head_dim);
   if (st != GPUSQ_OK) return st;
-  if (!is_size(batch) || !is_size(q_len) || !is_size(kv_len) || kv_len > INT32_MAX - 64) return GPUSQ_ERR_SHAPE;
+  if (!is_size(batch) || !is_size(q_len) || !is_size(kv_len) || kv_len > kMostStates) return GPUSQ_ERR_SHAPE;
   if (batch * q_len > INT32_MAX / heads || batch * q_len * heads * head_dim > kMaxElems) return GPUSQ_ERR_SHAPE;
   CrossAttention x{q, k, v, kv_lens, key_mask, out, workspace, batch, q_len, kv_len, heads, kv_heads, head_dim, {q_batch_stride, q_stride, q_head_stride},
                    {k_batch_stride, k_stride, k_head_stride}, {v_batch_stride, v_stride, v_head_stride}, 0.0f};

@@ -26,4 +26,20 @@ __host__ __device__ inline ColumnShare column_share(int col_tiles, int groups, i
   return s;
 }
 
+// The keys of part `part` of part_tiles tiles of 32 keys, of columns that see `most` keys.  (The sum of a part's beginning and its length
+// passes 31 bits, not 32.)
+struct KeyRange {
+  int begin, end;
+};
+__host__ __device__ inline KeyRange keys_of_part(int part, int part_tiles, int most) {
+  KeyRange k;
+  k.begin = part * part_tiles * 32;
+  const unsigned end = (unsigned)k.begin + (unsigned)part_tiles * 32;
+  k.end = most < 0 || end > (unsigned)most ? most : (int)end;
+  return k;
+}
+// A loop over the keys looks kMostAhead keys beyond a tile's first (four tiles of 32, two of 64), so fp16 states are kMostStates at most; a cache's
+// are whole pages of 64, fewer than that.
+constexpr int kMostAhead = 128, kMostStates = INT32_MAX - kMostAhead;
+
 }  // namespace gpusq

@@ -39,8 +39,8 @@ struct States {
   static constexpr int PIECES = DP / 8, ROWS = 64 / PIECES;          // pieces of a row, rows of an instruction
   static constexpr int COPIES = KT / (ROWS * NW);                    // instructions of a wavefront, for keys and for values
   static_assert(COPIES > 0 && COPIES * ROWS * NW == KT, "whole instructions");
-  const uint8_t *kp, *vp;
-  int64_t k_row, v_row;  // bytes
+  const uint8_t *kp, *vp;  // of the next tile to load: tiles are loaded in order
+  int64_t k_row, v_row;    // bytes
   uint32_t lds;
   int row[COPIES], piece[COPIES], len, D2;
   const uint8_t* mask;
@@ -48,8 +48,9 @@ struct States {
   float* begin;  // [buffer][key of a tile]
   bool first;    // of a row's lanes
 
-  __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles, float* begin_, int)
-      : kp((const uint8_t*)(a.k + w.b * a.k_batch + w.kh * a.k_head)), vp((const uint8_t*)(a.v + w.b * a.v_batch + w.kh * a.v_head)), k_row(2 * a.k_token), v_row(2 * a.v_token),
+  __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles, float* begin_, int first_key)
+      : kp((const uint8_t*)(a.k + w.b * a.k_batch + w.kh * a.k_head + first_key * a.k_token)),
+        vp((const uint8_t*)(a.v + w.b * a.v_batch + w.kh * a.v_head + first_key * a.v_token)), k_row(2 * a.k_token), v_row(2 * a.v_token),
         lds(lds_address(tiles) + wave * COPIES * 1024), len(len_), D2(2 * a.D),
         mask(MASKED ? a.mask + (int64_t)w.b * a.kv_len : nullptr), begin(begin_), first(lane % PIECES == 0) {
 #pragma unroll
@@ -64,8 +65,10 @@ struct States {
     for (int i = 0; i < COPIES; ++i) byte[i] = mask[key0 + row[i] < len ? key0 + row[i] : len - 1];
   }
   // Rows from `len` on are its last row once more (finite where that is), pieces beyond the head are left out.
-  __device__ __forceinline__ void load(int buf, int key0) const {
-    const uint8_t *k = kp + key0 * k_row, *v = vp + key0 * v_row;
+  __device__ __forceinline__ void load(int buf, int key0) {
+    const uint8_t *k = kp, *v = vp;
+    kp += KT * k_row;
+    vp += KT * v_row;
     const int last = len - 1 - key0;
     unsigned sees = ~0u;
     if constexpr (MASKED) {
@@ -177,6 +180,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
   static_assert(NB == 2 || (NB == 4 && !KV4), "the waits for copies");
   static_assert(!MASKED || NB == 2, "bytes of one tile");
   static_assert(QT <= 2, "count below QT is 1 or 0");
+  static_assert(NB * KT <= kMostAhead, "key0 + NB * KT");
   constexpr int J = DP / 32, CH = DP / 16, NT = 64 * NW, kTile = KT * kRow<DP>;
   __shared__ __attribute__((aligned(16))) uint8_t lds[NB * 2 * kTile];  // [buffer][keys, values]
   __shared__ __attribute__((aligned(16))) float begin[MASKED ? NB * KT : 4];
@@ -193,7 +197,8 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
   const int least = span.sees(16 * (tile0 + wave) / a.rep);
   const int last = 16 * tile1 < cols ? 16 * tile1 - 1 : cols - 1;
   const int most = span.sees(last / a.rep);
-  const int first_key = w.part * a.part_tiles * 32, end_key = first_key + a.part_tiles * 32 < most ? first_key + a.part_tiles * 32 : most;
+  const KeyRange keys = keys_of_part(w.part, a.part_tiles, most);
+  const int first_key = keys.begin, end_key = keys.end;
   typedef typename std::conditional<KV4, Codes<DP, KT, NW>, States<DP, KT, NW, MASKED>>::type Stage;
   Stage stage(a, w, span.len, wave, lane, lds, begin, first_key);
   if (!KV4 && (MASKED || a.D < DP)) {  // the pieces beyond the head, and rows that are not copied: zeros, once

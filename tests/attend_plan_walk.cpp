@@ -1,4 +1,4 @@
-// Walks the plans of attention as its workgroups do (csrc/attend_plan.h), over sizes that no test launches.  Prints "ok", or what fails.
+// Walks the plans of attention as its workgroups do (csrc/attend_plan.h), columns and keys, over sizes that no test launches.  Prints "ok", or what fails.
 #include <math.h>
 #include <stdio.h>
 
@@ -23,6 +23,23 @@ static const char* columns(int64_t cols, int most) {
   return next == col_tiles ? nullptr : "blocks of columns not covered";
 }
 
+// `most` keys over parts of part_tiles tiles: each key in one part, and what a loop looks ahead of its last tile is a number
+static const char* keys(int most, int part_tiles, int parts) {
+  int64_t next = 0;
+  for (int p = 0; p < parts; ++p) {
+    const KeyRange k = keys_of_part(p, part_tiles, most);
+    if (k.begin >= most) {
+      if (k.end > k.begin) return "keys that are not there";
+      continue;
+    }
+    if (k.begin != next || k.end <= k.begin || k.end - (int64_t)k.begin > (int64_t)part_tiles * 32) return "keys of a part";
+    if (k.end != most && k.end % 64 != 0) return "half a page";
+    if ((int64_t)k.end - 1 + kMostAhead > INT32_MAX) return "keys ahead";
+    next = k.end;
+  }
+  return next == (most > 0 ? most : 0) ? nullptr : "keys not covered";
+}
+
 int main() {
   // around where products with the number of blocks pass 2^31 and 2^32, and up to what 31 bits of columns allow
   for (const int most : {4, 8, 16})
@@ -32,9 +49,20 @@ int main() {
         if (const char* wrong = columns(cols, most)) return printf("%s: %lld columns, %d a workgroup\n", wrong, (long long)cols, 16 * most), 1;
       }
   std::mt19937_64 rng(1);
+  // lengths up to the longest that is taken, columns that see none of them
+  for (int i = 0; i < 100000; ++i) {
+    const int length = i < 2000 ? kMostStates - i : (int)exp2(std::uniform_real_distribution<double>(0, 30.999)(rng));
+    const int64_t tiles = ceil_div(length, 32), part_tiles = ceil_div(ceil_div(tiles, 1 + (int64_t)(rng() % 256)), 2) * 2;
+    const int seen[] = {length, (int)(rng() % length), 0, -(int)(rng() % length)};
+    for (const int most : seen)
+      if (const char* wrong = keys(most, (int)part_tiles, (int)ceil_div(tiles, part_tiles)))
+        return printf("%s: %d of %d keys, parts of %d tiles\n", wrong, most, length, (int)part_tiles), 1;
+  }
   for (int i = 0; i < 2000; ++i) {
     const int64_t cols = (int64_t)exp2(std::uniform_real_distribution<double>(0, 24)(rng));
     if (const char* wrong = columns(cols, 4 << (rng() % 3))) return printf("%s: %lld columns\n", wrong, (long long)cols), 1;
   }
+  const int64_t pages = INT32_MAX / 64 - 1;  // of a sequence, at most; a loop is at one's beginning
+  if (64 * (pages - 1) + kMostAhead > INT32_MAX) return printf("pages ahead\n"), 1;
   printf("ok\n");
 }

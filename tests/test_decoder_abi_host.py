@@ -144,3 +144,10 @@ def test_plans_of_attention(tmp_path):
     assert build.returncode == 0, build.stderr
     run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert run.returncode == 0 and run.stdout == "ok\n", run.stdout
+
+
+def test_states_that_a_loop_cannot_look_beyond(g):
+    """The most states: what the loops over the keys look ahead of a tile stays a number of 31 bits"""
+    base = dict(q=P, k=P, v=P, lens=None, mask=None, out=P, ws=P, batch=1, q_len=100, kv_len=2**31 - 129, heads=1, kv_heads=1, head_dim=64, qb=64, qt=64, qh=64, kb=0, kt=0, kh=64, vb=0,
+                vt=0, vh=64, scale=-1.0, stream=None)
+    _refuses(g, "gpusq_cross_attention", base, [(ERR_UNSUPPORTED, dict()), (ERR_SHAPE, dict(kv_len=2**31 - 128)), (ERR_SHAPE, dict(kv_len=2**31 - 65))])
