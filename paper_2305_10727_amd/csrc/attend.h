@@ -77,22 +77,25 @@ struct Work {
   }
 };
 
-// The tokens of a batch's queries, the keys that it has
+// The tokens of a batch's queries (nq that are answered), the keys that it has, those in front of its first query (fewer than none, if it has more
+// queries than keys)
 template <bool KV4>
 struct Span {
-  int t0, nq, len;
+  int t0, nq, len, before;
   int64_t q_base;
   __device__ __forceinline__ Span(const AttendArgs& a, int b) : t0(b * a.q_len), nq(a.q_len) {
     if constexpr (KV4) {
       if (a.cu_q != nullptr) {
         t0 = a.cu_q[b];
         const int t1 = a.cu_q[b + 1];
-        nq = t0 >= 0 && t1 <= a.tokens && t1 > t0 ? (t1 - t0 < a.q_len ? t1 - t0 : a.q_len) : 0;
+        nq = t0 >= 0 && t1 <= a.tokens && t1 > t0 ? t1 - t0 : 0;
       }
       q_base = (int64_t)t0 * a.q_token;
       const int most = a.max_pages * kPageTokens;
       len = a.lens[b];
       len = len < 0 ? 0 : len < most ? len : most;
+      before = len - nq;  // (of all of its queries, also where more of them are there than are answered)
+      nq = nq < a.q_len ? nq : a.q_len;
     } else {
       q_base = b * a.q_batch;
       len = a.kv_len;
@@ -104,7 +107,7 @@ struct Span {
   }
   // keys that the query of token `tok` sees
   __device__ __forceinline__ int sees(int tok) const {
-    const int limit = KV4 ? len - nq + tok + 1 : len;
+    const int limit = KV4 ? before + tok + 1 : len;
     return limit < len ? limit : len;
   }
 };

@@ -574,11 +574,14 @@ def _workspace(like, given, nbytes):
     return given
 
 
-def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=1, scale=None, out=None, workspace=None):
+def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=None, scale=None, out=None, workspace=None):
     """gpusq_attention_kv4: q [tokens,heads,head_dim] fp16, cache [pages,kv_heads,bytes], block_table [batch,max_pages] int32, kv_lens [batch] int32,
-    cu_q [batch + 1] int32 (None: max_q queries each) -> [tokens,heads,head_dim] fp16"""
+    cu_q [batch + 1] int32 (None: max_q queries each) -> [tokens,heads,head_dim] fp16.  max_q: the most queries of a sequence; by default 1 without
+    cu_q, and with it as many as there are tokens: every query is answered, at the cost of workgroups for that many of each sequence."""
     _want(_is(q, torch.float16, -1, -1, -1), "q: [tokens, heads, head_dim] float16 on the GPU")
     tokens, heads, D = q.shape
+    if max_q is None:
+        max_q = 1 if cu_q is None else tokens
     _want(_is(cache, torch.uint8, -1, -1, _size("gpusq_kv4_page_bytes", 1, D)), "cache: pages of kv4_cache of q's head_dim")
     pages, kv_heads, _ = cache.shape
     _want(_is(block_table, torch.int32, -1, -1), "block_table: [batch, max_pages] int32 on the GPU")

@@ -438,3 +438,20 @@ def test_columns_whose_products_pass_32_bits(g):
         y = w @ V
         off = (w * (2.0 ** -11 + 2.0 ** -20 + delta + (w * delta).sum(1, keepdim=True))) @ V.abs() + 2.0 ** -31 * V.abs().sum(0) + 2.0 ** -11 * y.abs() + 2.0 ** -24
         assert ((out[a:a + 4700].double().view(-1, D) - y).abs() <= off).all()
+
+
+# of few queries and many, over keys in one piece and in parts
+@pytest.mark.parametrize("lens,counts,max_q", [([300, 64, 9], [5, 2, 1], 1), ([300, 64, 7], [5, 2, 7], 3), ([9001, 70], [6, 2], 2), ([400, 130], [70, 41], 40), ([5000, 90], [120, 33], 50)])
+def test_more_new_tokens_than_max_q(g, lens, counts, max_q):
+    """The first max_q of a sequence are answered, as what they are: they do not see the tokens behind them.  Without max_q all are."""
+    G, D, H = 1, 64, 2
+    c = _Cache(lens, G, D, seed=71)
+    q = _normal(72, sum(counts), H, D)
+    exp, off = c.expected(q, counts, D ** -0.5)
+    cu = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    args = dev(q), dev(c.pages), dev(c.table), dev(np.array(lens, np.int32)), dev(cu)
+    y = host(g.attention_kv4(*args, max_q=max_q)).astype(np.float64)
+    answered = np.concatenate([np.arange(a, min(a + max_q, b)) for a, b in zip(cu, cu[1:])])
+    assert (np.abs(y - exp) <= off)[answered].all()
+    y = host(g.attention_kv4(*args)).astype(np.float64)
+    assert (np.abs(y - exp) <= off).all()
