@@ -502,14 +502,18 @@ def quantize_groups_int4(W, group):
     return codes, scales
 
 
-def pack_int4_groups(codes, scales, group):
+def pack_int4_groups(codes, scales, group, out=None):
     """gpusq_pack_int4_groups: codes [N,K] int8 of -8..7, scales [N,K/group] fp16 -> the operand of linear_int4 (uint8)"""
     _want(_is(codes, torch.int8, -1, -1), "codes: [N, K] int8 on the GPU")
     N, K = codes.shape
     _want(_is(scales, torch.float16, N, K // max(group, 1)), "scales: [N, K / group] float16 on the GPU")
-    packed = _empty(codes, torch.uint8, max(_size("gpusq_int4_groups_packed_bytes", N, K, group), 16))
-    calls.gpusq_pack_int4_groups(codes, scales, group, packed, N, K)
-    return packed
+    nbytes = max(_size("gpusq_int4_groups_packed_bytes", N, K, group), 16)
+    if out is None:
+        out = _empty(codes, torch.uint8, nbytes)
+    else:
+        _want(_is(out, torch.uint8, nbytes), "out: the operand of another layer than N, K and group say")
+    calls.gpusq_pack_int4_groups(codes, scales, group, out, N, K)
+    return out
 
 
 def linear_int4(X, packed, N, group, bias=None, gelu=False, out_dtype=torch.float16, out=None):

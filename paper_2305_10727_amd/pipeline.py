@@ -308,12 +308,14 @@ class DecoderLayer:
         self.graph = None
 
     def prepare_weights(self, weights, states_weight):
-        """weights: fp32 [N, K] by the names of `widths`; states_weight [2 kv_heads head_dim, states_dim] (keys, then values)"""
-        for name, (N, K) in self.widths.items():
+        """weights: fp32 [N, K] by the names of `widths`; states_weight [2 kv_heads head_dim, states_dim] (keys, then values).  Weights that are
+        prepared again go to where the former ones were: a captured step follows them."""
+        for name, size in self.widths.items():
+            if weights[name].shape != size:
+                raise ValueError("%s: [%d, %d] wanted" % (name, *size))
+        for name in self.widths:
             W = weights[name]
-            if W.shape != (N, K):
-                raise ValueError("%s: [%d, %d] wanted" % (name, N, K))
-            self.packed[name] = G.pack_int4_groups(*G.quantize_groups_int4(W, self.group), self.group)
+            self.packed[name] = G.pack_int4_groups(*G.quantize_groups_int4(W, self.group), self.group, out=self.packed.get(name))
         self.states_kv.prepare_weights(states_weight)
 
     def see(self, states, bias):
@@ -339,12 +341,13 @@ class DecoderLayer:
 
     def capture(self, *args, **kwargs):
         """Records forward() on these tensors into a HIP graph (after one eager run that loads every kernel): replay() reruns it on what they
-        hold then, into the same output."""
+        hold then, into the same output.  They are kept here, as the graph has their addresses."""
         self.forward(*args, **kwargs)
         torch.cuda.synchronize()
-        self.graph = torch.cuda.CUDAGraph()
-        with torch.cuda.graph(self.graph):
-            self.out = self.forward(*args, **kwargs)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = self.forward(*args, **kwargs)
+        self.graph, self.out, self.captured = graph, out, (args, kwargs)
         return self.graph
 
     def replay(self):

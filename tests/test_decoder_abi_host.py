@@ -151,3 +151,18 @@ def test_states_that_a_loop_cannot_look_beyond(g):
     base = dict(q=P, k=P, v=P, lens=None, mask=None, out=P, ws=P, batch=1, q_len=100, kv_len=2**31 - 129, heads=1, kv_heads=1, head_dim=64, qb=64, qt=64, qh=64, kb=0, kt=0, kh=64, vb=0,
                 vt=0, vh=64, scale=-1.0, stream=None)
     _refuses(g, "gpusq_cross_attention", base, [(ERR_UNSUPPORTED, dict()), (ERR_SHAPE, dict(kv_len=2**31 - 128)), (ERR_SHAPE, dict(kv_len=2**31 - 65))])
+
+
+def test_a_layer_keeps_its_weights_where_they_are(g, monkeypatch):
+    """A captured step of pipeline.DecoderLayer has the addresses of its weights: preparing others does not move them"""
+    torch = pytest.importorskip("torch")
+    from paper_2305_10727_amd import pipeline
+    layer = pipeline.DecoderLayer(64, 2, 1, 32, 128, 1, 8, 64, 1, device="cpu")
+    monkeypatch.setattr(layer.states_kv, "prepare_weights", lambda W: None)
+    monkeypatch.setattr(g, "quantize_groups_int4", lambda W, group: (W, W))
+    monkeypatch.setattr(g, "pack_int4_groups", lambda codes, scales, group, out=None: torch.empty(codes.numel(), dtype=torch.uint8) if out is None else out)
+    weights = {n: torch.zeros(shape) for n, shape in layer.widths.items()}
+    layer.prepare_weights(weights, None)
+    first = dict(layer.packed)
+    layer.prepare_weights(weights, None)
+    assert set(first) == set(layer.widths) and all(layer.packed[n] is first[n] for n in first)

@@ -106,3 +106,47 @@ def test_replayed_from_a_graph(setup):
         eager = layer.forward(*args, **kw)
         torch.cuda.synchronize()
         assert torch.equal(got, eager) and torch.equal(kept, layer.cache)
+
+
+def test_weights_prepared_again_behind_a_capture(g, setup):
+    """A captured step follows the layer's weights as an eager one does, and keeps the tensors that it was captured with"""
+    from paper_2305_10727_amd.pipeline import DecoderLayer
+    layer = DecoderLayer(D, H, KV, HD, HIDDEN, B, S, SD, PAGES, group=GROUP)
+
+    def prepare(seed):
+        r = np.random.default_rng(seed)
+        layer.prepare_weights({n: dev((r.standard_normal(shape) * 0.06).astype(np.float32)) for n, shape in layer.widths.items()},
+                              dev((r.standard_normal((2 * KV * HD, SD)) * 0.06).astype(np.float32)))
+        layer.see(dev(setup["states"]), dev(setup["bias"]))
+
+    def arguments():
+        i = _inputs(setup, 0, 1, 40)
+        return (i["x"], (_rms, _rms, _rms), (dev(setup["cos"]), dev(setup["sin"])), i["positions"], i["slots"], dev(setup["table"]), i["kv_lens"]), \
+            dict(head_weights=[dev(w) for w in setup["weights"]], state_lens=dev(setup["state_lens"]))
+
+    prepare(50)
+    args, kw = arguments()
+    layer.capture(*args, **kw)
+    del args, kw
+    results = []
+    for seed in (50, 51, 52):
+        prepare(seed)
+        filler = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (64, 512, 4096, 16384, 65536, 1 << 20) for _ in range(8)]  # NaN where something was freed
+        got = layer.replay().clone()
+        torch.cuda.synchronize()
+        args, kw = arguments()
+        eager = layer.forward(*args, **kw)
+        assert torch.equal(got, eager)
+        results.append(got)
+        del filler
+    assert not torch.equal(results[0], results[1]) and not torch.equal(results[1], results[2])
+
+
+def test_packed_weights_go_where_they_are_told_to(g):
+    codes, scales = g.quantize_groups_int4(torch.randn((36, 256), device="cuda"), 64)
+    packed = g.pack_int4_groups(codes, scales, 64)
+    out = torch.zeros_like(packed)
+    assert g.pack_int4_groups(codes, scales, 64, out=out) is out and torch.equal(out, packed)
+    for bad in (out[:-16], out.to(torch.int8), out.cpu()):
+        with pytest.raises(ValueError):
+            g.pack_int4_groups(codes, scales, 64, out=bad)
