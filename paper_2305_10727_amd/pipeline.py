@@ -329,6 +329,10 @@ class DecoderLayer:
         """x [T, D] fp16, T / batch new tokens of each sequence; rope: (cos, sin); positions, slots [T], block_table [batch, pages of a sequence],
         kv_lens [batch] (with the new tokens), state_lens [batch] or None: int32.  -> [T, D] fp16"""
         T, H, hd = x.shape[0], self.heads, self.head_dim
+        # what a later call would refuse, before the tokens are in the cache
+        G._want(T % self.batch == 0, "x: as many tokens of each of the %d sequences" % self.batch)
+        G._want(G._is(block_table, torch.int32, self.batch, -1) and G._is(kv_lens, torch.int32, self.batch) and
+                (state_lens is None or G._is(state_lens, torch.int32, self.batch)), "block_table: [batch, pages] int32, kv_lens and state_lens: [batch] int32, on the GPU")
         q = G.qk_norm_rope(self._linear("qkv", norms[0](x)), H, self.kv_heads, hd, q_weight=head_weights[0], k_weight=head_weights[1], cos=rope[0], sin=rope[1],
                            positions=positions, cache=self.cache, slots=slots)
         a = G.attention_kv4(q, self.cache, block_table, kv_lens, max_q=T // self.batch)

@@ -150,3 +150,22 @@ def test_packed_weights_go_where_they_are_told_to(g):
     for bad in (out[:-16], out.to(torch.int8), out.cpu()):
         with pytest.raises(ValueError):
             g.pack_int4_groups(codes, scales, 64, out=bad)
+
+
+def test_what_a_later_call_would_refuse_is_not_in_the_cache(setup):
+    """Tokens that the sequences cannot share, a table or lengths of another batch or type: refused before anything is written"""
+    layer, good = setup["layer"], _inputs(setup, 3, 2, 30)
+    before = layer.cache.clone()
+    table, state_lens = dev(setup["table"]), dev(setup["state_lens"])
+
+    def step(i, table=table, state_lens=state_lens, kv_lens=good["kv_lens"]):
+        return layer.forward(i["x"], (_rms, _rms, _rms), (dev(setup["cos"]), dev(setup["sin"])), i["positions"], i["slots"], table, kv_lens, state_lens=state_lens)
+
+    for bad in (lambda: step({n: t[:4].contiguous() for n, t in good.items()}), lambda: step(good, table=table[:2].contiguous()), lambda: step(good, table=table.long()),
+                lambda: step(good, state_lens=state_lens[:1].contiguous()), lambda: step(good, kv_lens=good["kv_lens"].cpu())):
+        with pytest.raises(ValueError):
+            bad()
+        assert torch.equal(before, layer.cache)
+    step(good)
+    assert not torch.equal(before, layer.cache)
+    layer.cache.copy_(before)
