@@ -348,7 +348,8 @@ gpusq_status gpusq_gemm_int8_dense(const int8_t* Xq, const int8_t* Wq, const flo
 /* ---- the operators of a decoder that reads what the encoder's layers above have made: products with 4-bit weights for a few tokens,
  * the norm and rotation of queries and keys, attention over a 4-bit cache of the decoder's own tokens, attention to the encoder's states.
  * They serve: none has a gradient.  head_dim is a multiple of 8 up to 256 (GPUSQ_ERR_UNSUPPORTED), heads a multiple of kv_heads
- * (GPUSQ_ERR_SHAPE): query head h reads key head h / (heads / kv_heads).  Outputs must not overlap inputs.
+ * (GPUSQ_ERR_SHAPE): query head h reads key head h / (heads / kv_heads).  Outputs must not overlap inputs.  Sizes whose launch would have
+ * 2^32 threads or more (8.4 million pairs of a sequence and a key head, matrices of 2^35 weights) are GPUSQ_ERR_SHAPE.
  *
  * Linear layers on 4-bit weights with a scale for each `group` (32, 64 or 128; GPUSQ_ERR_UNSUPPORTED) consecutive weights of a row,
  * K % group == 0:  W[n][k] = codes[n][k] * scales[n][k / group].
@@ -410,7 +411,7 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
 /* Attention of q_len queries to kv_len keys and values of another source, or of the same one, without a causal mask: q [batch][q_len][heads],
  * k, v [batch][kv_len][kv_heads], vectors of head_dim fp16 values, each dimension with a stride of its own in values (a multiple of 8,
  * GPUSQ_ERR_ALIGN; not negative), so that heads may lie in a packed projection or apart.
- *   kv_lens (or NULL): keys of batch b beyond kv_lens[b] are not seen; key_mask (or NULL) [batch][kv_len] bytes: keys of a 0 are not seen.
+ *   kv_len: at most 2^31 - 129.  kv_lens (or NULL): keys of batch b beyond kv_lens[b] are not seen; key_mask (or NULL) [batch][kv_len] bytes: keys of a 0 are not seen.
  *   What is not seen may hold anything, NaN included; a channel with an infinity among the values seen is infinite or NaN.
  *   scale, out [batch][q_len][heads][head_dim] and workspace as above. */
 size_t gpusq_cross_attention_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads, int64_t head_dim);

@@ -9,6 +9,8 @@ using namespace gpusq;
 namespace {
 constexpr int64_t kMaxElems = (int64_t)1 << 40;
 
+constexpr int64_t kMostPages = INT32_MAX / kPageTokens - 1;  // of a sequence: tokens are counted in 31 bits, a page beyond the last too
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 bool is_size(int64_t n) { return n > 0 && n <= INT32_MAX; }
@@ -25,9 +27,11 @@ gpusq_status check_heads(int64_t heads, int64_t kv_heads, int64_t D) {
   return D % 8 == 0 && D <= 256 ? GPUSQ_OK : GPUSQ_ERR_UNSUPPORTED;
 }
 
-// workgroups of an attention, at 16 columns each and with every part: must be countable
-bool is_countable(int64_t batch, int64_t q_len, int64_t heads, const AttendParts& p) {
-  return (batch + 8) * (heads + 8) <= INT32_MAX && (batch + 8) * (heads + 8) * ceil_div(q_len, 16) <= INT32_MAX / p.parts;
+// whether the launches of an attention and of its parts' join count their threads
+bool is_launchable(bool kv4, int64_t batch, int64_t q_len, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t D, const AttendParts& p, bool reach) {
+  const int64_t cols = q_len * (heads / kv_heads);
+  return attend_launchable(batch * kv_heads * p.parts, cols, attend_shape(kv4, padded_head((int)D), cols, reach)) &&
+         (p.parts == 1 || launchable(join_workgroups(tokens * heads, D, p.parts), 256));
 }
 
 // the scale of the scores: positive; 0 stands for 1 / sqrt(D)
@@ -52,6 +56,7 @@ gpusq_status gpusq_quantize_groups_int4(const float* W, int group, int8_t* codes
   if (!W || !codes || !scales) return GPUSQ_ERR_NULL;
   gpusq_status st = check_groups(N, K, group);
   if (st != GPUSQ_OK) return st;
+  if (!launchable(ceil_div(N * K, 8 * 256), 256)) return GPUSQ_ERR_SHAPE;
   if (!aligned16(W) || !aligned16(codes) || !aligned16(scales)) return GPUSQ_ERR_ALIGN;
   return launch_quantize_groups_int4(W, group, codes, scales, N, K, (hipStream_t)stream);
 }
@@ -60,6 +65,7 @@ gpusq_status gpusq_pack_int4_groups(const int8_t* codes, const void* scales, int
   if (!codes || !scales || !packed) return GPUSQ_ERR_NULL;
   gpusq_status st = check_groups(N, K, group);
   if (st != GPUSQ_OK) return st;
+  if (!launchable(ceil_div(N, 16) * ceil_div(K, 128), 256)) return GPUSQ_ERR_SHAPE;
   if (!aligned16(codes) || !aligned16(scales) || !aligned16(packed)) return GPUSQ_ERR_ALIGN;
   return launch_pack_int4_groups(codes, scales, group, packed, N, K, (hipStream_t)stream);
 }
@@ -103,6 +109,7 @@ gpusq_status gpusq_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_str
 
 size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads, int64_t head_dim) {
   if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !is_size(tokens) || !is_size(batch) || !is_size(max_q) || !is_size(max_pages)) return 0;
+  if (max_pages > kMostPages) return 0;
   return parts_bytes(attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens), tokens, heads, head_dim);
 }
 
@@ -113,12 +120,12 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
   gpusq_status st = check_heads(heads, kv_heads, head_dim);
   if (st != GPUSQ_OK) return st;
   if (!is_size(tokens) || !is_size(batch) || !is_size(max_q) || !is_size(max_pages) || !is_size(num_pages)) return GPUSQ_ERR_SHAPE;
-  if (max_pages > INT32_MAX / kPageTokens - 1 || tokens * heads > INT32_MAX || tokens * heads * head_dim > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (max_pages > kMostPages || tokens * heads > INT32_MAX || tokens * heads * head_dim > kMaxElems) return GPUSQ_ERR_SHAPE;
   if (max_q > tokens || (!cu_q && tokens != batch * max_q)) return GPUSQ_ERR_SHAPE;
   AttentionKv4 x{q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim, 0.0f};
   if (!score_scale(scale, head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
   const AttendParts p = attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens);
-  if (!is_countable(batch, max_q, heads, p)) return GPUSQ_ERR_SHAPE;
+  if (!is_launchable(true, batch, max_q, tokens, heads, kv_heads, head_dim, p, true)) return GPUSQ_ERR_SHAPE;
   if (p.parts > 1 && !workspace) return GPUSQ_ERR_NULL;
   if (!aligned16(q) || !aligned16(cache) || !aligned16(out) || !aligned16(workspace) || !aligned4(block_table) || !aligned4(kv_lens) || !aligned4(cu_q))
     return GPUSQ_ERR_ALIGN;
@@ -148,7 +155,7 @@ gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, 
     }
   if (!score_scale(scale, head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
   const AttendParts p = attend_parts(false, batch, q_len, heads, kv_heads, head_dim, kv_len);
-  if (!is_countable(batch, q_len, heads, p)) return GPUSQ_ERR_SHAPE;
+  if (!is_launchable(false, batch, q_len, batch * q_len, heads, kv_heads, head_dim, p, tiles_reach(k_stride, v_stride))) return GPUSQ_ERR_SHAPE;
   if (p.parts > 1 && !workspace) return GPUSQ_ERR_NULL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(workspace) || !aligned4(kv_lens)) return GPUSQ_ERR_ALIGN;
   return launch_cross_attention(x, (hipStream_t)stream);

@@ -53,7 +53,7 @@ struct Work {
     const int units = a.batch * a.kv_heads * a.parts, xcd = blockIdx.x & 7, local = blockIdx.x >> 3;
     // (divisions take a scalar unit that has none some forty instructions each: none by 1)
     int unit;
-    if (in_turn(units)) {
+    if (attend_in_turn(units)) {
       const int first = a.col_blocks == 1 ? local : local / a.col_blocks;
       block = local - first * a.col_blocks;
       unit = first * 8 + xcd;
@@ -70,11 +70,7 @@ struct Work {
     kh = pair - b * a.kv_heads;
     return true;
   }
-  static __host__ __device__ __forceinline__ bool in_turn(int64_t units) { return units >= 64 || units % 8 == 0; }
-  static unsigned workgroups(const AttendArgs& a) {
-    const int64_t units = (int64_t)a.batch * a.kv_heads * a.parts;
-    return (unsigned)(in_turn(units) ? ceil_div(units, 8) * 8 * a.col_blocks : ceil_div(units * a.col_blocks, 8) * 8);
-  }
+  static unsigned workgroups(const AttendArgs& a) { return (unsigned)attend_workgroups((int64_t)a.batch * a.kv_heads * a.parts, a.col_blocks); }
 };
 
 // The tokens of a batch's queries (nq that are answered), the keys that it has, those in front of its first query (fewer than none, if it has more
@@ -234,11 +230,7 @@ struct Columns {
   }
 };
 
-// the kernel for many columns (attend_tiles.hip), and how many a workgroup takes
-constexpr int kFewColumns = 32;
-// (a tile of 64 tokens in 32-bit offsets)
-inline bool tiles_reach(bool kv4, const AttendArgs& a) { return kv4 || (a.k_token < (1 << 24) && a.v_token < (1 << 24)); }
-constexpr int tiles_columns(bool kv4, int DP) { return (DP > 128 ? 64 : 128) * (kv4 ? 2 : 1); }
+// the kernel for many columns (attend_tiles.hip)
 void launch_attend_tiles(bool kv4, AttendArgs a, hipStream_t s);
 
 }  // namespace gpusq

@@ -305,7 +305,6 @@ __global__ void __launch_bounds__(256) join_parts_kernel(const float* __restrict
 }
 
 // Few parts: a thread for four channels of a row.  The maxima are requested side by side, and so are the sums, four parts at a time.
-constexpr int kFewParts = 8;
 __global__ void __launch_bounds__(256) join_few_parts_kernel(const float* __restrict__ part_o, const float* __restrict__ part_ml, _Float16* __restrict__ out, int64_t rows,
                                                               int D, int parts) {
   const int quads = D / 4, at = threadIdx.x / quads, quad = threadIdx.x - at * quads;
@@ -354,15 +353,12 @@ void launch_shape(AttendArgs a, hipStream_t s) {
   attend_few_kernel<KV4, DP, QT, WK, false><<<blocks, 64 * WK, 0, s>>>(a);
 }
 
-// The columns of a workgroup.  (Two blocks of heads of 256 do not fit the registers of a wavefront.)
-int few_columns(int64_t cols, int DP) { return cols <= 16 || DP == 256 ? 16 : 32; }
-
 template <bool KV4, int DP>
 void launch_head(const AttendArgs& a, hipStream_t s) {
-  const int64_t cols = (int64_t)a.q_len * a.rep;
-  if (cols > kFewColumns && tiles_reach(KV4, a))
+  const AttendShape shape = attend_shape(KV4, DP, (int64_t)a.q_len * a.rep, KV4 || tiles_reach(a.k_token, a.v_token));
+  if (shape.many)
     launch_attend_tiles(KV4, a, s);
-  else if (few_columns(cols, DP) == 16)
+  else if (shape.columns == 16)
     launch_shape<KV4, DP, 1, 8>(a, s);
   else if constexpr (DP < 256)
     launch_shape<KV4, DP, 2, 4>(a, s);
@@ -378,8 +374,9 @@ void launch_head(const AttendArgs& a, hipStream_t s) {
 // Many columns: parts of 16 tiles at least.
 AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys) {
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
-  const bool few = cols <= kFewColumns;
-  const int64_t groups = batch * kv_heads * ceil_div(cols, few ? few_columns(cols, padded_head((int)head_dim)) : tiles_columns(kv4, padded_head((int)head_dim)));
+  const AttendShape shape = attend_shape(kv4, padded_head((int)head_dim), cols, true);
+  const bool few = !shape.many;
+  const int64_t groups = batch * kv_heads * ceil_div(cols, shape.columns);
   int64_t parts = few ? ceil_div(256, groups) : (kv4 ? 256 : 512) / groups;
   const int64_t one = (kv4 ? 4096 : 2048) / padded_head((int)head_dim);
   const int64_t most = !few ? ceil_div(tiles, 16) : tiles <= (one < 32 ? one : 32) ? 1 : ceil_div(tiles, 8);
@@ -406,9 +403,9 @@ static gpusq_status run(AttendArgs a, bool kv4, const AttendParts& p, void* work
   gpusq_status st = check_launch();
   if (st != GPUSQ_OK || p.parts == 1) return st;
   if (p.parts <= kFewParts)
-    join_few_parts_kernel<<<(unsigned)ceil_div(rows, 256 / (a.D / 4)), 256, 0, s>>>(a.part_o, a.part_ml, a.out, rows, a.D, p.parts);
+    join_few_parts_kernel<<<(unsigned)join_workgroups(rows, a.D, p.parts), 256, 0, s>>>(a.part_o, a.part_ml, a.out, rows, a.D, p.parts);
   else
-    join_parts_kernel<<<(unsigned)rows, 256, 0, s>>>(a.part_o, a.part_ml, a.out, (int)rows, a.D, p.parts);
+    join_parts_kernel<<<(unsigned)join_workgroups(rows, a.D, p.parts), 256, 0, s>>>(a.part_o, a.part_ml, a.out, (int)rows, a.D, p.parts);
   return check_launch();
 }
 

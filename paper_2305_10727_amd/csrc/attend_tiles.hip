@@ -321,6 +321,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
 
 template <bool KV4, int DP, int QT, int NW, int KT, int NB>
 void launch_shape(AttendArgs a, hipStream_t s) {
+  static_assert(16 * QT * NW == tiles_columns(KV4, DP) && 64 * NW == tiles_threads(KV4), "as the host counts workgroups");
   a.col_blocks = (int)ceil_div((int64_t)a.q_len * a.rep, 16 * QT * NW);
   const unsigned blocks = Work::workgroups(a);
   if constexpr (!KV4) {

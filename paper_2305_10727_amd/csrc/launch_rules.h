@@ -19,6 +19,16 @@ inline PrunePairsGrid prune_pairs_grid(int64_t N, int64_t K) {
   return PrunePairsGrid{per_rows, ceil_div(per_rows, 256), ceil_div(chunks, 8 * per_rows)};
 }
 
+// A launch counts its threads in 32 bits.
+inline bool launchable(int64_t workgroups, int64_t threads) { return workgroups <= UINT32_MAX / threads; }
+
+// How many tokens of `per_token` heads' vectors one launch of qk_norm_rope_kernel takes, whose workgroups of 256 threads have `in_workgroup` vectors each:
+// vectors are counted in 31 bits, a last workgroup's too.
+inline int64_t qk_norm_tokens(int64_t per_token, int64_t in_workgroup) {
+  const int64_t counted = INT32_MAX - 256, launched = UINT32_MAX / 256 * in_workgroup;
+  return (counted < launched ? counted : launched) / per_token;
+}
+
 struct ByteRange {
   const void* p;
   int64_t bytes;

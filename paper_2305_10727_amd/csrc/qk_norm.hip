@@ -173,9 +173,12 @@ __global__ void __launch_bounds__(256) qk_norm_rope_kernel(const QkArgs a) {
   }
 }
 
+// vectors of a workgroup: in the cache heads have the lanes of what they are padded to
+int64_t vectors_of_workgroup(int64_t D, bool cached) { return 4 * (64 / (cached ? padded_head((int)D) / 8 : D / 8)); }
+
 template <typename T, int L>
 void launch_lanes(const QkArgs& a, bool interleaved, hipStream_t s) {
-  const unsigned blocks = (unsigned)ceil_div(a.vectors, 4 * (64 / (L != 0 ? L : a.D / 8)));
+  const unsigned blocks = (unsigned)ceil_div(a.vectors, vectors_of_workgroup(a.D, false));
   if (interleaved || a.R == 0)
     qk_norm_rope_kernel<T, L, true, false><<<blocks, 256, 0, s>>>(a);
   else
@@ -183,7 +186,7 @@ void launch_lanes(const QkArgs& a, bool interleaved, hipStream_t s) {
 }
 template <typename T, int L>
 void launch_cached(const QkArgs& a, bool interleaved, hipStream_t s) {
-  const unsigned blocks = (unsigned)ceil_div(a.vectors, 256 / L);
+  const unsigned blocks = (unsigned)ceil_div(a.vectors, vectors_of_workgroup(a.D, true));
   if (interleaved || a.R == 0)
     qk_norm_rope_kernel<T, L, true, true><<<blocks, 256, 0, s>>>(a);
   else
@@ -207,11 +210,11 @@ gpusq_status launch_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_st
                                  const float* q_weight, const float* k_weight, float eps, const float* cos, const float* sin, const int32_t* positions,
                                  int64_t table_rows, int64_t R, int interleaved, void* q_out, void* k_out, void* v_out, void* cache, const int32_t* slots,
                                  int64_t num_pages, hipStream_t s) {
-  const int64_t per_token = heads + kv_heads + (cache != nullptr ? kv_heads : 0), most = (INT32_MAX - 256) / per_token;  // (a last workgroup's count stays in range)
+  const int64_t per_token = heads + kv_heads + (cache != nullptr ? kv_heads : 0), most = qk_norm_tokens(per_token, vectors_of_workgroup(D, cache != nullptr));
   unsigned bits = 1;  // per_token >= 2
   while ((int64_t)1 << bits < per_token) ++bits;
   const unsigned magic = (unsigned)(((uint64_t)1 << (31 + bits)) / per_token + 1);
-  for (int64_t from = 0; from < T; from += most) {  // (vectors are counted in 31 bits)
+  for (int64_t from = 0; from < T; from += most) {
     const int64_t n = T - from < most ? T - from : most;
     const QkArgs a{(const uint8_t*)qkv + from * row_stride * (dt == GPUSQ_F32 ? 4 : 2), row_stride, q_weight, k_weight, cos, sin, positions ? positions + from : nullptr,
                    slots ? slots + from : nullptr, (_Float16*)q_out + from * heads * D, k_out ? (_Float16*)k_out + from * kv_heads * D : nullptr,

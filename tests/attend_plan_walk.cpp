@@ -40,6 +40,27 @@ static const char* keys(int most, int part_tiles, int parts) {
   return next == (most > 0 ? most : 0) ? nullptr : "keys not covered";
 }
 
+// every vector of tokens * per_token in a launch that counts its threads, and vectors in 31 bits
+static const char* norms(int64_t per_token, int64_t in_workgroup) {
+  const int64_t most = qk_norm_tokens(per_token, in_workgroup);
+  if (most < 1) return "no token";
+  const int64_t workgroups = ceil_div(most * per_token, in_workgroup);
+  if (workgroups * 256 > UINT32_MAX || workgroups * in_workgroup > INT32_MAX) return "threads or vectors beyond what is counted";
+  const int64_t more = ceil_div((most + 1) * per_token, in_workgroup);
+  return more * 256 <= UINT32_MAX && (most + 1) * per_token <= INT32_MAX - 256 ? "fewer tokens than a launch takes" : nullptr;
+}
+
+// workgroups that are launched: enough for every block of columns of every unit, and their numbers and columns in 31 bits
+static const char* launches(bool kv4, int DP, int64_t units, int64_t cols, bool reach) {
+  const AttendShape s = attend_shape(kv4, DP, cols, reach);
+  const int64_t col_blocks = ceil_div(cols, s.columns);
+  if (!attend_launchable(units, cols, s)) return units * 1.0 * col_blocks * s.threads > 4.0e9 ? nullptr : "refused";
+  const int64_t workgroups = attend_workgroups(units, col_blocks);
+  if (workgroups < units * col_blocks || workgroups > units * col_blocks + 8 * col_blocks) return "number of workgroups";
+  if (workgroups * s.threads > UINT32_MAX) return "threads beyond what a launch counts";
+  return col_blocks * s.columns > INT32_MAX - 15 ? "columns beyond 31 bits" : nullptr;
+}
+
 int main() {
   // around where products with the number of blocks pass 2^31 and 2^32, and up to what 31 bits of columns allow
   for (const int most : {4, 8, 16})
@@ -62,6 +83,16 @@ int main() {
     const int64_t cols = (int64_t)exp2(std::uniform_real_distribution<double>(0, 24)(rng));
     if (const char* wrong = columns(cols, 4 << (rng() % 3))) return printf("%s: %lld columns\n", wrong, (long long)cols), 1;
   }
+  for (int64_t per_token = 2; per_token <= 3 * 65536; per_token += per_token < 100 ? 1 : 97)
+    for (const int64_t in_workgroup : {8, 12, 32, 64, 256})
+      if (const char* wrong = norms(per_token, in_workgroup)) return printf("%s: %lld vectors a token\n", wrong, (long long)per_token), 1;
+  for (int i = 0; i < 200000; ++i) {
+    const int64_t units = (int64_t)exp2(std::uniform_real_distribution<double>(0, 32)(rng)), cols = (int64_t)exp2(std::uniform_real_distribution<double>(0, 31)(rng));
+    if (const char* wrong = launches(rng() % 2, 64 << (rng() % 3), units, cols, rng() % 4 != 0)) return printf("%s: %lld units, %lld columns\n", wrong, (long long)units, (long long)cols), 1;
+  }
+  for (const int64_t cols : {INT32_MAX, INT32_MAX - 15, INT32_MAX - 127, INT32_MAX - 255, INT32_MAX - 2047})
+    for (int k = 0; k < 12; ++k)
+      if (const char* wrong = launches(k & 1, 64 << (k >> 2), 1, cols, k & 2)) return printf("%s: %lld columns\n", wrong, (long long)cols), 1;
   const int64_t pages = INT32_MAX / 64 - 1;  // of a sequence, at most; a loop is at one's beginning
   if (64 * (pages - 1) + kMostAhead > INT32_MAX) return printf("pages ahead\n"), 1;
   printf("ok\n");

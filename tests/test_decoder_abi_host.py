@@ -166,3 +166,19 @@ def test_a_layer_keeps_its_weights_where_they_are(g, monkeypatch):
     first = dict(layer.packed)
     layer.prepare_weights(weights, None)
     assert set(first) == set(layer.widths) and all(layer.packed[n] is first[n] for n in first)
+
+
+def test_what_no_launch_counts_is_refused(g):
+    """A launch has 2^32 - 1 threads: one more workgroup than that is a shape that is refused, one less meets the next check"""
+    base = dict(q=ODD, cache=P, table=P, lens=P, cu=None, out=P, ws=P, tokens=65535, batch=65535, max_q=1, max_pages=1, pages=300, heads=128, kv_heads=128, head_dim=64, scale=0.0, stream=None)
+    _refuses(g, "gpusq_attention_kv4", base, [(ERR_ALIGN, dict()), (ERR_SHAPE, dict(tokens=65536, batch=65536)),
+                                              (ERR_SHAPE, dict(tokens=2**24, batch=1, cu=P, heads=1, kv_heads=1, max_pages=2000)),  # the join's rows
+                                              (ERR_ALIGN, dict(tokens=2**24 - 1, batch=1, cu=P, heads=1, kv_heads=1, max_pages=2000))])
+    base = dict(q=ODD, k=P, v=P, lens=None, mask=None, out=P, ws=P, batch=65535, q_len=1, kv_len=40, heads=128, kv_heads=128, head_dim=64, qb=8192, qt=8192, qh=64, kb=0, kt=64, kh=64, vb=0,
+                vt=64, vh=64, scale=0.0, stream=None)
+    _refuses(g, "gpusq_cross_attention", base, [(ERR_ALIGN, dict()), (ERR_SHAPE, dict(batch=65536))])
+    base = dict(W=ODD, group=64, codes=P, scales=P, N=2**20 - 1, K=2**15, stream=None)
+    _refuses(g, "gpusq_quantize_groups_int4", base, [(ERR_ALIGN, dict()), (ERR_SHAPE, dict(N=2**20))])
+    base = dict(codes=ODD, scales=P, group=64, packed=P, N=2**20 - 16, K=2**15, stream=None)
+    _refuses(g, "gpusq_pack_int4_groups", base, [(ERR_ALIGN, dict()), (ERR_SHAPE, dict(N=2**20 - 15))])
+    assert g.lib().gpusq_attention_kv4_workspace_bytes(1, 1, 1, 2**25 - 2, 8, 2, 128) > 0 == g.lib().gpusq_attention_kv4_workspace_bytes(1, 1, 1, 2**25 - 1, 8, 2, 128)
