@@ -566,7 +566,8 @@ def qk_norm_rope(qkv, heads, kv_heads, head_dim, q_weight=None, k_weight=None, e
         pages = cache.shape[0]
         if want_cached:
             v = _empty(qkv, f16, T, kv_heads, head_dim)
-    calls.gpusq_qk_norm_rope(qkv, _TORCH_DT[qkv.dtype], qkv.stride(0), T, heads, kv_heads, head_dim, norm, q_weight, k_weight, eps, cos, sin, positions, rows, 2 * R,
+    row = qkv.stride(0) if T > 1 else (heads + 2 * kv_heads) * head_dim  # (torch gives one row any stride)
+    calls.gpusq_qk_norm_rope(qkv, _TORCH_DT[qkv.dtype], row, T, heads, kv_heads, head_dim, norm, q_weight, k_weight, eps, cos, sin, positions, rows, 2 * R,
                              interleaved, q_out, k, v, cache, slots, pages)
     return (q_out, k) if cache is None else (q_out, k, v) if want_cached else q_out
 

@@ -191,3 +191,11 @@ def test_refusals(g):
         g.qk_norm_rope(x, 4, 2, 64, eps=-1.0)
     with pytest.raises(g.GpusqError):
         g.kv4_cache(3, 2, 260)
+
+
+def test_one_token_whose_row_has_no_stride(g):
+    """A column turned over: one contiguous row whose stride from token to token is 1"""
+    c = _Case(1, 4, 2, 64, 64)
+    q, k = g.qk_norm_rope(dev(c.x.reshape(-1, 1)).t(), 4, 2, 64, **c.kwargs(False))
+    q0, k0 = g.qk_norm_rope(dev(c.x), 4, 2, 64, **c.kwargs(False))
+    assert torch.equal(q, q0) and torch.equal(k, k0)
