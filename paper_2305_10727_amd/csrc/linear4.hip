@@ -130,6 +130,9 @@ __device__ __forceinline__ void store_channels(const Linear4Args& a, f4 y, int n
     *(h4*)((_Float16*)a.Y + at) = h4{(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
 }
 
+// the last word of a buffer's descriptor: bytes as they are (data format 32, no swizzle); loads behind its end give 0
+constexpr int kRawBuffer = 4 << 15;
+
 // A few rows: a workgroup takes one tile of 16 channels after another, each wavefront the same S steps of all of them, so that its rows (MT
 // columns of 16) stay in registers.  (A load of 16 bytes a lane takes the first-level cache 16 clocks, whether its lanes ask for the same
 // bytes or not: a step's rows cost four times what its weights do.)  A longer K is taken in chunks of S NW steps, the tiles' sums waiting in LDS.
@@ -147,13 +150,16 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) linear_int4_rows_kernel(const
   };
   auto load = [&](int chunk, int tile, Weights& x) {
     const u4* codes = (const u4*)(a.W + (int64_t)tile * a.kt * 1024) + lane;
-    const h4* scales = (const h4*)(a.W + (int64_t)nt * a.kt * 1024 + (int64_t)tile * a.kt * PER * 32) + g;
+    // (a step beyond the last: the last one's codes again, with rows of zeros; and with scales of zeros, which is what is loaded behind the end of a
+    // buffer: 0 times a scale that is infinite would not be 0)
+    const auto scales = __builtin_amdgcn_make_buffer_rsrc((void*)(a.W + (int64_t)nt * a.kt * 1024 + (int64_t)tile * a.kt * PER * 32), 0, (unsigned)a.kt * (PER * 32), kRawBuffer);
+    const unsigned scales_at = (unsigned)((chunk * NW + wave) * S) * (PER * 32) + 8 * g;
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-      const int at = (chunk * NW + wave) * S + i, step = at < a.kt ? at : a.kt - 1;  // (a step beyond the last: that one again, with rows of zeros)
-      x.w[i] = codes[(int64_t)step * 64];
+      const int at = (chunk * NW + wave) * S + i, step = at < a.kt ? at : a.kt - 1;
 #pragma unroll
-      for (int p = 0; p < PER; ++p) x.s[i][p] = scales[(step * PER + p) * 4];
+      for (int p = 0; p < PER; ++p) x.s[i][p] = __builtin_bit_cast(h4, __builtin_amdgcn_raw_buffer_load_b64(scales, scales_at + (i * PER + p) * 32, 0, 0));
+      x.w[i] = codes[(int64_t)step * 64];
     }
   };
   const _Float16* rows[MT];

@@ -163,3 +163,20 @@ def test_refusals(g):
             g.quantize_groups_int4(X.float(), group)
     with pytest.raises(g.GpusqError):
         g.quantize_groups_int4(torch.zeros((2, 100), device="cuda"), 32)
+
+
+# steps of K that the wavefronts do not deal out evenly: behind the last one some have none
+@pytest.mark.parametrize("M", [1, 20, 40])
+@pytest.mark.parametrize("K", [128, 1152, 2176, 8320])
+def test_an_infinite_scale(g, M, K):
+    """The last group of a channel with a scale that is infinite: its sum, which is not 0, times it, in that channel alone"""
+    N, group = 20, 32
+    codes, scales = _weights(N, K, group, 8)
+    codes[:, -group:] = 1
+    X = np.abs(np.random.default_rng(9).standard_normal((M, K))).astype(np.float16) + np.float16(0.5)
+    clean = host(g.linear_int4(dev(X), g.pack_int4_groups(dev(codes), dev(scales), group), N, group, out_dtype=torch.float32))
+    scales[5, -1], scales[7, -1] = np.inf, -np.inf
+    y = host(g.linear_int4(dev(X), g.pack_int4_groups(dev(codes), dev(scales), group), N, group, out_dtype=torch.float32))
+    assert (y[:, 5] == np.inf).all() and (y[:, 7] == -np.inf).all()
+    others = [n for n in range(N) if n not in (5, 7)]
+    assert np.array_equal(y[:, others], clean[:, others])
