@@ -360,8 +360,8 @@ gpusq_status gpusq_gemm_int8_dense(const int8_t* Xq, const int8_t* Wq, const flo
  *     4 i .. + 3 and k + 2 i + 1 in bits 16 + 4 i .. + 3; then the scales [N / 16][K / 128 * (128 / group)][16 rows].  Rows and columns
  *     beyond the matrix hold zeros.  gpusq_int4_groups_packed_bytes bytes (0 for invalid sizes).
  *   gpusq_linear_int4: Y [M][N] (out_dt GPUSQ_F16 or GPUSQ_F32) = act(X [M][K] fp16 W^T + bias), products exact, sums in fp32, each
- *     group's sum times its scale in fp32; GELU in its exact erf form.  N % 4 == 0 (GPUSQ_ERR_UNSUPPORTED).  Any M; made for up to 64
- *     rows, beyond which the weights are read once for every 64. */
+ *     group's sum times its scale in fp32; GELU in its exact erf form.  N % 4 == 0 (GPUSQ_ERR_UNSUPPORTED), K below 2^31 - 8192 (GPUSQ_ERR_SHAPE).
+ *     Any M; made for up to 64 rows, beyond which the weights are read once for every 64. */
 size_t gpusq_int4_groups_packed_bytes(int64_t N, int64_t K, int group);
 gpusq_status gpusq_quantize_groups_int4(const float* W, int group, int8_t* codes, void* scales, int64_t N, int64_t K, void* stream);
 gpusq_status gpusq_pack_int4_groups(const int8_t* codes, const void* scales, int group, void* packed, int64_t N, int64_t K, void* stream);

@@ -75,7 +75,7 @@ gpusq_status gpusq_linear_int4(const void* X, const void* Wpacked, int group, co
   if (!X || !Wpacked || !Y || ((epilogue & GPUSQ_EPI_BIAS) && !bias)) return GPUSQ_ERR_NULL;
   gpusq_status st = check_groups(N, K, group);
   if (st != GPUSQ_OK) return st;
-  if (!is_size(M) || ceil_div(M, 16) > 65535 || M * N > kMaxElems || M * K > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (!is_size(M) || K > kMostLinear4K || ceil_div(M, 16) > 65535 || M * N > kMaxElems || M * K > kMaxElems) return GPUSQ_ERR_SHAPE;
   if (N % 4 != 0 || (out_dt != GPUSQ_F16 && out_dt != GPUSQ_F32) || (epilogue & ~(GPUSQ_EPI_BIAS | GPUSQ_EPI_GELU))) return GPUSQ_ERR_UNSUPPORTED;
   if (!aligned16(X) || !aligned16(Wpacked) || !aligned16(Y) || (bias && !aligned16(bias))) return GPUSQ_ERR_ALIGN;
   return launch_linear_int4(X, Wpacked, group, bias, Y, out_dt == GPUSQ_F32, M, N, K, epilogue, (hipStream_t)stream);

@@ -12,6 +12,11 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef unsigned u2 __attribute__((ext_vector_type(2)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
+// ---- 4-bit layers ---------------------------------------------------------------------------------------------------------------
+// Steps of 128 k that a workgroup takes at once, at most.  All but one of them may lie behind the end of K, and are found to by comparing their k with
+// it in 31 bits: so K is kMostLinear4K at most.
+constexpr int kLinear4Steps = 64, kMostLinear4K = INT32_MAX - kLinear4Steps * 128;
+
 // ---- the cache ------------------------------------------------------------------------------------------------------------------
 // A page holds 64 tokens of one head, DP = the head's channels padded to 64, 128 or 256:
 //   key codes     [64 tokens][4 g][DP / 32 j] words: channels 32 j + 8 g + 0..7, the even ones in the lower half of the word.  Lane

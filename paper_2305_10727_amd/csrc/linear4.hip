@@ -138,6 +138,7 @@ constexpr int kRawBuffer = 4 << 15;
 // bytes or not: a step's rows cost four times what its weights do.)  A longer K is taken in chunks of S NW steps, the tiles' sums waiting in LDS.
 template <int MT, int NW, int S, bool CHUNKS, int GROUP, bool F32>
 __global__ void __launch_bounds__(64 * NW, NW / 4) linear_int4_rows_kernel(const Linear4Args a) {
+  static_assert(NW * S <= kLinear4Steps, "k behind the end of K");
   constexpr int PER = 128 / GROUP, CH = GROUP / 32;
   extern __shared__ __attribute__((aligned(16))) f4 lds[];  // [2][NW][MT][64], and with chunks [tiles of the workgroup][MT][64]
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;

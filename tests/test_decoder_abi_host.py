@@ -182,3 +182,10 @@ def test_what_no_launch_counts_is_refused(g):
     base = dict(codes=ODD, scales=P, group=64, packed=P, N=2**20 - 16, K=2**15, stream=None)
     _refuses(g, "gpusq_pack_int4_groups", base, [(ERR_ALIGN, dict()), (ERR_SHAPE, dict(N=2**20 - 15))])
     assert g.lib().gpusq_attention_kv4_workspace_bytes(1, 1, 1, 2**25 - 2, 8, 2, 128) > 0 == g.lib().gpusq_attention_kv4_workspace_bytes(1, 1, 1, 2**25 - 1, 8, 2, 128)
+
+
+def test_rows_whose_last_steps_pass_31_bits(g):
+    """The longest rows of a 4-bit layer: a workgroup's 64 steps of 128 behind the last one are still numbers of 31 bits"""
+    base = dict(X=ODD, W=P, group=32, bias=None, Y=P, out_dt=g.F16, M=1, N=4, K=2**31 - 8224, epilogue=0, stream=None)
+    assert -(-base["K"] // 128) * 128 + 63 * 128 + 96 < 2**31
+    _refuses(g, "gpusq_linear_int4", base, [(ERR_ALIGN, dict()), (ERR_SHAPE, dict(K=2**31 - 8192)), (ERR_SHAPE, dict(K=2**31 - 32))])
