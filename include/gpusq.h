@@ -400,7 +400,7 @@ gpusq_status gpusq_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_str
  * queries of a sequence (of one that has more, its first max_q are answered).  cu_q NULL: max_q queries each, tokens = batch * max_q.
  *   scale (0: 1 / sqrt(head_dim)) > 0.  out [tokens][heads][head_dim] fp16; 0 for a query that sees nothing, unspecified for a token that
  *   no sequence has and for queries that are not answered.  Scores, softmax and sums in fp32; the weights of the values are rounded to fp16.
- *   workspace: gpusq_attention_kv4_workspace_bytes, may be NULL where that is 0 (long histories, few sequences: the keys are cut into parts
+ *   workspace: gpusq_attention_kv4_workspace_bytes (0 for sizes that are refused), may be NULL where that is 0 (long histories, few sequences: the keys are cut into parts
  *   that are joined by a second launch); what it held does not matter. */
 size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads,
                                            int64_t head_dim);

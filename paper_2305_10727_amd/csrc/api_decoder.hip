@@ -27,6 +27,15 @@ gpusq_status check_heads(int64_t heads, int64_t kv_heads, int64_t D) {
   return D % 8 == 0 && D <= 256 ? GPUSQ_OK : GPUSQ_ERR_UNSUPPORTED;
 }
 
+// sizes of the attentions, heads checked: products of what passes stay in 64 bits
+bool are_kv4_sizes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t D) {
+  return is_size(tokens) && is_size(batch) && is_size(max_q) && is_size(max_pages) && max_pages <= kMostPages && tokens * heads <= INT32_MAX &&
+         tokens * heads * D <= kMaxElems && max_q <= tokens;
+}
+bool are_cross_sizes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t D) {
+  return is_size(batch) && is_size(q_len) && is_size(kv_len) && kv_len <= kMostStates && batch * q_len <= INT32_MAX / heads && batch * q_len * heads * D <= kMaxElems;
+}
+
 // whether the launches of an attention and of its parts' join count their threads
 bool is_launchable(bool kv4, int64_t batch, int64_t q_len, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t D, const AttendParts& p, bool reach) {
   const int64_t cols = q_len * (heads / kv_heads);
@@ -108,8 +117,7 @@ gpusq_status gpusq_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_str
 }
 
 size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads, int64_t head_dim) {
-  if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !is_size(tokens) || !is_size(batch) || !is_size(max_q) || !is_size(max_pages)) return 0;
-  if (max_pages > kMostPages) return 0;
+  if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !are_kv4_sizes(tokens, batch, max_q, max_pages, heads, head_dim)) return 0;
   return parts_bytes(attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens), tokens, heads, head_dim);
 }
 
@@ -119,9 +127,7 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
   if (!q || !cache || !block_table || !kv_lens || !out) return GPUSQ_ERR_NULL;
   gpusq_status st = check_heads(heads, kv_heads, head_dim);
   if (st != GPUSQ_OK) return st;
-  if (!is_size(tokens) || !is_size(batch) || !is_size(max_q) || !is_size(max_pages) || !is_size(num_pages)) return GPUSQ_ERR_SHAPE;
-  if (max_pages > kMostPages || tokens * heads > INT32_MAX || tokens * heads * head_dim > kMaxElems) return GPUSQ_ERR_SHAPE;
-  if (max_q > tokens || (!cu_q && tokens != batch * max_q)) return GPUSQ_ERR_SHAPE;
+  if (!are_kv4_sizes(tokens, batch, max_q, max_pages, heads, head_dim) || !is_size(num_pages) || (!cu_q && tokens != batch * max_q)) return GPUSQ_ERR_SHAPE;
   AttentionKv4 x{q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim, 0.0f};
   if (!score_scale(scale, head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
   const AttendParts p = attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens);
@@ -133,7 +139,7 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
 }
 
 size_t gpusq_cross_attention_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads, int64_t head_dim) {
-  if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !is_size(batch) || !is_size(q_len) || !is_size(kv_len)) return 0;
+  if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !are_cross_sizes(batch, q_len, kv_len, heads, head_dim)) return 0;
   return parts_bytes(attend_parts(false, batch, q_len, heads, kv_heads, head_dim, kv_len), batch * q_len, heads, head_dim);
 }
 
@@ -144,8 +150,7 @@ gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, 
   if (!q || !k || !v || !out) return GPUSQ_ERR_NULL;
   gpusq_status st = check_heads(heads, kv_heads, head_dim);
   if (st != GPUSQ_OK) return st;
-  if (!is_size(batch) || !is_size(q_len) || !is_size(kv_len) || kv_len > kMostStates) return GPUSQ_ERR_SHAPE;
-  if (batch * q_len > INT32_MAX / heads || batch * q_len * heads * head_dim > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (!are_cross_sizes(batch, q_len, kv_len, heads, head_dim)) return GPUSQ_ERR_SHAPE;
   CrossAttention x{q, k, v, kv_lens, key_mask, out, workspace, batch, q_len, kv_len, heads, kv_heads, head_dim, {q_batch_stride, q_stride, q_head_stride},
                    {k_batch_stride, k_stride, k_head_stride}, {v_batch_stride, v_stride, v_head_stride}, 0.0f};
   for (const int64_t* strides : {x.q_stride, x.k_stride, x.v_stride})

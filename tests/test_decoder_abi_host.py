@@ -3,6 +3,7 @@
 import ctypes
 import os
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -189,3 +190,13 @@ def test_rows_whose_last_steps_pass_31_bits(g):
     base = dict(X=ODD, W=P, group=32, bias=None, Y=P, out_dt=g.F16, M=1, N=4, K=2**31 - 8224, epilogue=0, stream=None)
     assert -(-base["K"] // 128) * 128 + 63 * 128 + 96 < 2**31
     _refuses(g, "gpusq_linear_int4", base, [(ERR_ALIGN, dict()), (ERR_SHAPE, dict(K=2**31 - 8192)), (ERR_SHAPE, dict(K=2**31 - 32))])
+
+
+@pytest.mark.parametrize("name,sizes", [("attention_kv4", (1, 2**30, 2**30, 2000, 65536, 1, 64)), ("attention_kv4", (2**31 - 1, 1, 1, 2**20, 65536, 32768, 256)),
+                                        ("attention_kv4", (1, 1, 2, 2000, 8, 2, 64)), ("cross_attention", (2**30, 2**30, 5000, 65536, 1, 64)),
+                                        ("cross_attention", (1, 1, 2**31 - 1, 8, 2, 64))])
+def test_workspaces_of_sizes_that_are_refused(g, name, sizes):
+    """0 for what the call would refuse, without a product that passes 64 bits (a divisor that wrapped to 0 would end the process: asked in one of its own)"""
+    ask = "import sys; sys.path.insert(0, %r)\nfrom paper_2305_10727_amd import gpusq\nprint(gpusq.lib().gpusq_%s_workspace_bytes%r)" % (ROOT, name, sizes)
+    run = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and run.stdout == "0\n", run
