@@ -239,8 +239,27 @@ PyObject* is_tensor(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// strides(t): t.stride() with 0 for dimensions of size 1, whose strides no address is formed with and torch gives any value
+PyObject* strides(PyObject*, PyObject* o) {
+  HANDLE_TH_ERRORS
+  if (!THPVariable_Check(o)) {
+    PyErr_SetString(PyExc_TypeError, "strides(t): a tensor");
+    return nullptr;
+  }
+  const at::Tensor& t = THPVariable_Unpack(o);
+  PyObject* all = PyTuple_New(t.dim());
+  for (int64_t i = 0; all && i < t.dim(); ++i) {
+    PyObject* n = PyLong_FromLongLong(t.size(i) == 1 ? 0 : t.stride(i));
+    if (!n) Py_CLEAR(all);
+    else PyTuple_SET_ITEM(all, i, n);
+  }
+  return all;
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef g_methods[] = {{"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, "empty(like, dtype, *sizes)"},
                            {"is_tensor", (PyCFunction)(void (*)(void))is_tensor, METH_FASTCALL, "is_tensor(t, dtype, *sizes)"},
+                           {"strides", (PyCFunction)strides, METH_O, "strides(t)"},
                            {"setup", setup, METH_VARARGS, "setup(get_device, get_stream, on_error)"}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_fastcall", "C functions as cheap Python callables", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -482,6 +482,14 @@ def _is(t, dtype, *sizes):
     return _is(t, dtype, *sizes)
 
 
+def _strides(t):
+    """t.stride(), 0 for dimensions of size 1; the extension module, loaded on first use, takes its place"""
+    global _strides
+    from . import _fastcall
+    _strides = _fastcall.strides
+    return _strides(t)
+
+
 def _want(ok, what):
     if not ok:
         raise ValueError(what)
@@ -611,10 +619,8 @@ def cross_attention(q, k, v, kv_lens=None, key_mask=None, scale=None, out=None, 
     _want(_is(k, f16, B, -1, -1, D), "k: [batch, kv_len, kv_heads, head_dim] float16 on the GPU, of q's batch and head_dim")
     _, S, G, _ = k.shape
     _want(_is(v, f16, B, S, G, D), "v: as k")
-    qs, ks, vs = q.stride(), k.stride(), v.stride()
+    qs, ks, vs = _strides(q), _strides(k), _strides(v)
     _want(qs[3] == ks[3] == vs[3] == 1, "q, k, v: the last dimension contiguous")
-    if 1 in (B, Tq, S, H, G):  # (torch gives a dimension of one any stride; it is not used)
-        qs, ks, vs = ([0 if n == 1 else s for n, s in zip(t.shape, t.stride())] for t in (q, k, v))
     _want(kv_lens is None or _is(kv_lens, torch.int32, B), "kv_lens: [batch] int32 on the GPU")
     _want(key_mask is None or _is(key_mask, torch.uint8, B, S) or _is(key_mask, torch.bool, B, S), "key_mask: [batch, kv_len] uint8 or bool on the GPU")
     if out is None:

@@ -200,3 +200,11 @@ def test_workspaces_of_sizes_that_are_refused(g, name, sizes):
     ask = "import sys; sys.path.insert(0, %r)\nfrom paper_2305_10727_amd import gpusq\nprint(gpusq.lib().gpusq_%s_workspace_bytes%r)" % (ROOT, name, sizes)
     run = subprocess.run([sys.executable, "-c", ask], capture_output=True, text=True, timeout=300)
     assert run.returncode == 0 and run.stdout == "0\n", run
+
+
+def test_strides_of_dimensions_of_one(g):
+    torch = pytest.importorskip("torch")
+    t = torch.zeros(64).as_strided((1, 3, 1, 8), (5, 16, 7, 1))
+    assert g._strides(t) == (0, 16, 0, 1) and g._strides(torch.zeros(())) == ()
+    with pytest.raises(TypeError):
+        g._strides(3)
