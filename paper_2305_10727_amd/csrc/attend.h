@@ -133,6 +133,13 @@ struct Columns {
       const _Float16* p = a.q + span.q_base + tok * a.q_token + head * a.q_head;
 #pragma unroll
       for (int j = 0; j < J; ++j) q[i][j] = in && 32 * j + 8 * g < a.D ? *(const h8*)(p + 32 * j + 8 * g) : h8(0);
+    }
+    clear();
+  }
+  // no key seen
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
       m[i] = limit_s[i] = -__builtin_inff();
       off[i] = kShift;
       l[i] = f4(0);

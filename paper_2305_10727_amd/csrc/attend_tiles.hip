@@ -46,13 +46,14 @@ struct States {
   const uint8_t* mask;
   uint8_t byte[COPIES];
   float* begin;  // [buffer][key of a tile]
+  unsigned seen;  // whether this lane copied of any key
   bool first;    // of a row's lanes
 
   __device__ __forceinline__ States(const AttendArgs& a, const Work& w, int len_, int wave, int lane, uint8_t* tiles, float* begin_, int first_key)
       : kp((const uint8_t*)(a.k + w.b * a.k_batch + w.kh * a.k_head + first_key * a.k_token)),
         vp((const uint8_t*)(a.v + w.b * a.v_batch + w.kh * a.v_head + first_key * a.v_token)), k_row(2 * a.k_token), v_row(2 * a.v_token),
         lds(lds_address(tiles) + wave * COPIES * 1024), len(len_), D2(2 * a.D),
-        mask(MASKED ? a.mask + (int64_t)w.b * a.kv_len : nullptr), begin(begin_), first(lane % PIECES == 0) {
+        mask(MASKED ? a.mask + (int64_t)w.b * a.kv_len : nullptr), begin(begin_), seen(0), first(lane % PIECES == 0) {
 #pragma unroll
     for (int i = 0; i < COPIES; ++i) {
       row[i] = (wave * COPIES + i) * ROWS + lane / PIECES;
@@ -74,6 +75,7 @@ struct States {
     if constexpr (MASKED) {
 #pragma unroll
       for (int i = 0; i < COPIES; ++i) sees = row[i] <= last && byte[i] != 0 ? sees : sees & ~(1u << i);
+      seen |= sees & ((1u << COPIES) - 1);
       asm volatile("" : "+v"(sees));  // (all of the bytes, before a copy: the compiler, which does not count these, would wait for them as well)
     }
 #pragma unroll
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
   static_assert(NB * KT <= kMostAhead, "key0 + NB * KT");
   constexpr int J = DP / 32, CH = DP / 16, NT = 64 * NW, kTile = KT * kRow<DP>;
   __shared__ __attribute__((aligned(16))) uint8_t lds[NB * 2 * kTile];  // [buffer][keys, values]
-  __shared__ __attribute__((aligned(16))) float begin[MASKED ? NB * KT : 4];
+  __shared__ __attribute__((aligned(16))) float begin[MASKED ? NB * KT + 4 : 4];
   __shared__ int pages[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
   Work w;
@@ -203,6 +205,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
   Stage stage(a, w, span.len, wave, lane, lds, begin, first_key);
   if (!KV4 && (MASKED || a.D < DP)) {  // the pieces beyond the head, and rows that are not copied: zeros, once
     for (int i = threadIdx.x; i < NB * 2 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
+    if (MASKED && threadIdx.x == 0) begin[NB * KT] = 0.0f;
     __syncthreads();
   }
   if constexpr (KV4) {
@@ -316,6 +319,12 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
     run(std::integral_constant<int, 1>());
   else
     run(std::integral_constant<int, 0>());
+  // Columns that see nothing have nothing, also where a query is no number: -inf, which the scores of hidden keys begin at, and NaN are NaN.
+  if constexpr (MASKED) {
+    if (stage.seen != 0) begin[NB * KT] = 1.0f;  // (whoever writes it: the same)
+    __syncthreads();
+    if (begin[NB * KT] == 0.0f) x.clear();
+  }
   if (count > 0) x.store(a, w.part, g);
 }
 

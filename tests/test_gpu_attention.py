@@ -464,3 +464,18 @@ def test_strides_of_dimensions_of_one(g):
     odd = lambda x: dev(x).as_strided(x.shape, tuple(3 if n == 1 else s for n, s in zip(x.shape, dev(x).stride())))  # noqa: E731
     assert odd(k).stride() == (3, D, 3, 1)
     assert torch.equal(g.cross_attention(odd(q), odd(k), odd(v)), g.cross_attention(dev(q), dev(k), dev(v)))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("Tq,S", [(3, 100), (50, 100), (50, 1500)])
+def test_a_query_that_sees_nothing_and_is_no_number(g, Tq, S, D):
+    """0, as for any query that sees nothing, where a mask or a length hides all keys, which hold anything, one piece or parts"""
+    B = 3
+    q, k, v = _normal(91, B, Tq, 2, D), _normal(92, B, S, 1, D), _normal(93, B, S, 1, D)
+    seen = np.ones((B, S), bool)
+    seen[1] = False
+    q[:, 1, 0, 3], q[:, 2, 1, 4], k[1], v[1] = np.nan, np.inf, np.nan, np.nan
+    for hide in (dict(key_mask=dev(seen)), dict(kv_lens=dev(np.array([S, 0, S], np.int32))), dict(key_mask=dev(seen), kv_lens=dev(np.array([S, 5, S], np.int32)))):
+        y = host(g.cross_attention(dev(q), dev(k), dev(v), **hide))
+        assert not y[1].any()
+        assert np.isnan(y[[0, 2], 1, 0]).all() and np.isfinite(y[[0, 2], 0]).all()
