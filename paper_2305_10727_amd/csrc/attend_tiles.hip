@@ -2,7 +2,7 @@
 // arithmetic.  A workgroup's wavefronts have columns of their own and share the keys: keys and values go through LDS a tile at a time, in rows
 // as they lie in memory, with the 16-byte pieces of a row in places that differ from row to row (place()), so that neither the 16 rows of a
 // key operand nor the transposed reads of a value operand meet in a bank.  While one buffer is multiplied the others are filled.
-// Prompts of 1000 queries, 32 heads of 128 over 8, to up to 2313 states: 122-128 us, 0.9 PFLOP/s, the matrix units busy half of the time; for 34
+// Prompts of 1000 queries, 32 heads of 128 over 8, to up to 2313 states: 124-129 us, 0.9 PFLOP/s, the matrix units busy half of the time; for 34
 // matrix instructions (32 keys, 32 columns) there are 16 exponentials and some 70 other vector ones, of which a SIMD does little side by side.
 // ViT-B's attention at batch 128: 41 us for 155 MB, 3.7 TB/s where a large copy has 5.0.
 //   fp16 states go from memory to LDS directly; the cache's codes become fp16 numbers on the way, once for all the workgroup's columns.
@@ -169,8 +169,7 @@ struct Codes {
 };
 
 // The cache: 8 wavefronts on tiles of 64 keys, one workgroup a CU, as the codes are unpacked once for all of them (chunks of 300 tokens behind
-// 6000, 32 heads of 128 over 8: 89 us; with 4 wavefronts on tiles of 32 and three workgroups a CU 117.  Heads of 64: 63 us, two workgroups a CU
-// with a register or two in memory 68).
+// 6000, 32 heads of 128 over 8: 87 us; with 4 wavefronts on tiles of 32 and three workgroups a CU 129.  Heads of 64: 63 us, and 70).
 // States: tiles of 32, as many workgroups a CU as registers allow.  Heads of 64 need more loads on their way than two buffers hold: four (ViT-B's
 // attention, batch 128: 42.8 us with two, 41.5 with four); heads of 128, whose tile takes twice as long to multiply, gain nothing (prompts of 1000
 // over 2313 states: 126 us with two, 129 with three).

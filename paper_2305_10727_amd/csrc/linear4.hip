@@ -9,8 +9,8 @@
 //   - codes are turned into fp16 integers, exact, and the products of a group summed in 32 bits before its scale, in 32 bits too,
 //     multiplies the sum: nothing is rounded before the output, whatever the scales;
 //   - a workgroup's wavefronts share its channels and deal out the steps of K; their sums meet in LDS once, at the end.
-// 5120 -> 13824 with GELU for one row (36.6 MB): 10.5 us, 3.5 TB/s; 8192 -> 24576 for 13 rows (109 MB): 26 us, 4.2 TB/s; a large copy has 5.0.
-// 1024 -> 1024 for one row: 3.1 us, a launch and three trips to memory.
+// Replayed from a graph: 5120 -> 13824 with GELU for one row (36.6 MB) 11 us, 3.4 TB/s; 8192 -> 24576 for 13 rows (109 MB) 27 us, 4.0 TB/s, for 50
+// rows 60 us; 13824 -> 5120 for one row 13 us; a large copy has 5.0.  1024 -> 1024 for one row: 3.0 us, a launch and three trips to memory.
 #include "epilogue.h"
 #include "kv4.h"
 
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(256) pack_int4_groups_kernel(const int8_t* __r
 
 // GELU of four values, x Phi(x) = max(x, 0) - t Phi(-t), t = |x|.  For fp32 output by erfc; for fp16 output Phi(-t) = 2^P(t), P of degree 9
 // fitted to log2 Phi(-t) on 0 .. 6.5 (the result within 9e-8 of the exact one, and 2^-18 of it down to 2^-14; held at 9, where t Phi(-t) is 1e-18):
-// a tenth of erfc's instructions, which one wavefront has for all of a tile.  (5120 -> 13824 for one row 11.9 us with erfc, 10.8 with this.)
+// a tenth of erfc's instructions, which one wavefront has for all of a tile.  (5120 -> 13824 for one row 11.4 us with erfc, 10.8 with this.)
 template <bool F32>
 __device__ __forceinline__ f4 gelu4(f4 x) {
   constexpr float P[10] = {-0.999999463558197f,    -1.1511276960372925f,    -0.459060937166214f,     -0.05285963416099548f,   0.007497080136090517f,
@@ -273,7 +273,8 @@ gpusq_status launch_linear_int4(const void* X, const void* W, int group, const f
                                 hipStream_t s) {
   const Linear4Args a{(const _Float16*)X, (const uint8_t*)W, bias, Y, (int)M, (int)N, (int)K, (int)ceil_div(K, 128), epilogue};
   // The fewest steps a wavefront that K needs: registers for rows, and wavefronts for as much of the weights in flight as there are
-  // (8 wavefronts rather than 16 up to K = 2048: 1024 -> 1024 for one row 2.7 us, 3.4 with 16; 5120 -> 13824 10.9 with 8, 10.2 with 16).
+  // (8 wavefronts rather than 16 up to K = 2048: 1024 -> 1024 for one row 2.7 us, 3.4 with 16; 8 with twice the steps are within 2 % of 16 up to
+  // K = 5120: 4096 -> 16384 11.3 and 11.1, 5120 -> 13824 10.7 and 10.8).
   if (M <= 16)
     a.kt <= 8    ? launch_rows<1, 8, 1, false>(a, group, f32, s)
     : a.kt <= 16 ? launch_rows<1, 8, 2, false>(a, group, f32, s)

@@ -211,8 +211,8 @@ class EncoderBlockLinears:
     without one proj writes fc1's codes beside its fp16 output, which is a launch less, and up to 512 channels proj, fc1 and fc2 are one launch where that
     is ahead (gpusq_block_mlp_int8), two less again.  qkv, and fc1 behind a norm, quantise their fp16 input on the way in where their sizes favour it: a launch
     less for each.
-    Attention and the normalisation are not part of the library: `attention(qkv_int8 [M,3D], out_int8 [M,D])` and
-    `norm(proj_fp16 [M,D]) -> fp16 [M,D]` are the caller's (stubs in the tests and the report).  capture() records the
+    Attention from int8 to int8 and the normalisation are not part of the library: `attention(qkv_int8 [M,3D], out_int8 [M,D])` and
+    `norm(proj_fp16 [M,D]) -> fp16 [M,D]` are the caller's (stubs in the tests and the report); gpusq.cross_attention is attention from fp16 to fp16.  capture() records the
     whole sequence into a HIP graph, which takes the host out of the loop.
 
     scales: dict of 1-element fp32 device tensors: x (block input), qkv (qkv output), attn (attention output),
