@@ -400,6 +400,7 @@ gpusq_status gpusq_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_str
  * queries of a sequence (of one that has more, its first max_q are answered).  cu_q NULL: max_q queries each, tokens = batch * max_q.
  *   scale (0: 1 / sqrt(head_dim)) > 0.  out [tokens][heads][head_dim] fp16; 0 for a query that sees nothing, unspecified for a token that
  *   no sequence has and for queries that are not answered.  Scores, softmax and sums in fp32; the weights of the values are rounded to fp16.
+ *   Scores scale * q . k are below 2^22 in magnitude: beyond that, where 32 bits do not hold a weight to a factor of two, a row may be NaN.
  *   workspace: gpusq_attention_kv4_workspace_bytes (0 for sizes that are refused), may be NULL where that is 0 (long histories, few sequences: the keys are cut into parts
  *   that are joined by a second launch); what it held does not matter. */
 size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads,
@@ -413,7 +414,7 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
  * GPUSQ_ERR_ALIGN; not negative), so that heads may lie in a packed projection or apart.
  *   kv_len: at most 2^31 - 129.  kv_lens (or NULL): keys of batch b beyond kv_lens[b] are not seen; key_mask (or NULL) [batch][kv_len] bytes: keys of a 0 are not seen.
  *   What is not seen may hold anything, NaN included; a channel with an infinity among the values seen is infinite or NaN.
- *   scale, out [batch][q_len][heads][head_dim] and workspace as above. */
+ *   scale and the scores' range, out [batch][q_len][heads][head_dim] and workspace as above. */
 size_t gpusq_cross_attention_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads, int64_t head_dim);
 gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, const int32_t* kv_lens, const uint8_t* key_mask, void* out,
                                    void* workspace, int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads,

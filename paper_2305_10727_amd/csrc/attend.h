@@ -10,6 +10,8 @@
 //
 // The maximum moves only when a score passes it by 2^8 (kSlack): p = 2^(s - m + 6) then lies in fp16 up to 2^14, and down to 2^-24,
 // that is to 2^-30 of the largest where it has not moved.  Most tiles need neither the maximum across lanes nor a rescaled sum.
+// The exponent is formed of a score in one fused step from the maximum in log2 units, which is held to less than 1 up to 2^23, so that p stays in fp16 for scores
+// up to 2^22.  (Larger ones would need the maximum taken off before they are scaled: 1 to 3 % of a call, for scores that 32 bits hold to a factor of two.)
 // P is rounded to fp16 for the matrix instruction (the one rounding between the scores and the output); its sum is that of the rounded
 // values, in 32 bits, one matrix instruction with a first operand of ones instead of 8 additions a lane.
 #pragma once

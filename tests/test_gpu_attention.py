@@ -479,3 +479,53 @@ def test_a_query_that_sees_nothing_and_is_no_number(g, Tq, S, D):
         y = host(g.cross_attention(dev(q), dev(k), dev(v), **hide))
         assert not y[1].any()
         assert np.isnan(y[[0, 2], 1, 0]).all() and np.isfinite(y[[0, 2], 0]).all()
+
+
+# scores up to millions, of either sign; one piece and parts, few queries and many
+@pytest.mark.parametrize("size", [30.0, 300.0])
+@pytest.mark.parametrize("Tq,S,D", [(3, 70, 64), (40, 70, 128), (40, 1600, 64), (2, 3000, 256), (1, 9000, 64)])
+def test_large_scores(g, Tq, S, D, size):
+    """Keys that are multiples of one vector, so that the scores of a query are as far apart as the multiples: the largest takes all (the next one is
+    32-bit roundings of a sum away many times over)"""
+    r = np.random.default_rng(D + S)
+    u = np.where(r.random(D) < 0.5, 1.0, 0.5)
+    some = np.sort(r.choice(S, min(S, 60), replace=False))
+    a = np.full(S, -1.0)
+    a[some] = r.permutation(np.linspace(0.25, 1, len(some)))  # (the others: far below or, for queries of the other sign, far above in one place)
+    a[some[0] if some[0] != S - 1 else 0] = -2.0
+    k = (np.float16(size) * a[:, None] * u)[None, :, None].astype(np.float16)
+    sign = np.where(np.arange(Tq) % 2 == 0, 1.0, -1.0)
+    q = (size * sign[:, None] * np.ones(D))[None, :, None].astype(np.float16)
+    v = r.standard_normal((1, S, 1, D)).astype(np.float16)
+    scores = (q[0, :, 0].astype(np.float64) @ k[0, :, 0].astype(np.float64).T) * D ** -0.5
+    order = np.sort(scores, 1)
+    exp, off = _cross_expected(q, k, v, np.ones((1, S), bool), D ** -0.5)
+    near = (order[:, -1] - order[:, -2]) > np.maximum(40, 4 * D * 2.0 ** -24 * np.abs(order).max(1))
+    assert size < 300 or near.all()
+    y = host(g.cross_attention(dev(q), dev(k), dev(v))).astype(np.float64)
+    assert np.isfinite(y).all()
+    best = v[0, scores.argmax(1), 0].astype(np.float64)
+    assert (np.abs(y[0, near, 0] - best[near]) <= 2.0 ** -10 * np.abs(best[near]) + 2.0 ** -24).all()
+    assert (np.abs(y - exp) <= off)[:, ~near].all()
+
+
+@pytest.mark.parametrize("Tq,S", [(1, 200), (40, 200), (1, 9000), (40, 2100)])
+def test_large_scores_over_the_cache(g, Tq, S):
+    """The same where the keys are the cache's largest, 7 times 896"""
+    D = 64
+    c = _Cache([S], 1, D, seed=95)
+    best = S // 3
+    k = np.full((S, 1, D), -896.0 * 7, np.float32)
+    k[best] = 896.0 * 7  # seen by the last queries; the ones in front of it have only keys that are alike
+    (ck, sk), (cv, sv) = ref.cache_codes(k), ref.cache_codes(np.random.default_rng(3).standard_normal((S, 1, D)).astype(np.float32))
+    n = -(-S // 64)
+    pages = [np.concatenate([x, np.zeros((n * 64 - S,) + x.shape[1:], x.dtype)]).reshape(n, 64, 1, -1).transpose(0, 2, 1, 3) for x in (ck, sk, cv, sv)]
+    c.pages, c.table = ref.write_pages(*pages, D), np.arange(n, dtype=np.int32)[None]
+    V = cv * sv.astype(np.float64).repeat(32, -1)
+    q = np.full((Tq, 1, D), 64.0, np.float16)  # scores of 3.2 million
+    y = host(g.attention_kv4(dev(q), dev(c.pages), dev(c.table), dev(np.array([S], np.int32)), max_q=Tq)).astype(np.float64)
+    assert (np.abs(y[:, 0] - V[best, 0]) <= 2.0 ** -10 * np.abs(V[best, 0]) + 2.0 ** -24).all()
+    y = host(g.attention_kv4(dev(-q), dev(c.pages), dev(c.table), dev(np.array([S], np.int32)), max_q=Tq)).astype(np.float64)
+    for i in range(Tq):  # all but one alike: their mean, the weights' roundings at most 2^-11 of each
+        seen = np.delete(np.arange(S - Tq + 1 + i), best)
+        assert (np.abs(y[i, 0] - V[seen, 0].mean(0)) <= 2.0 ** -10 * np.abs(V[seen, 0]).mean(0) + 2.0 ** -24).all()
