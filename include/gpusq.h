@@ -409,6 +409,14 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
                                  void* out, void* workspace, int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages,
                                  int64_t num_pages, int64_t heads, int64_t kv_heads, int64_t head_dim, float scale, void* stream);
 
+/* The same for a tree of drafted tokens: a sequence's new tokens (its last ones in the cache) see every token in front of them, and of each other
+ * those that bits of tree [tokens][tree_words] say: bit j % 32 of word j / 32 of a token's row stands for the j-th new token of its sequence (itself
+ * is one of them; bits of tokens that it has not are not read).  tree_words * 32 >= max_q (GPUSQ_ERR_SHAPE), at most 2^30 tokens.  A token that sees
+ * nothing gives 0.  Workspace: gpusq_attention_kv4_workspace_bytes. */
+gpusq_status gpusq_attention_tree_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* kv_lens, const int32_t* cu_q,
+                                      const int32_t* tree, int64_t tree_words, void* out, void* workspace, int64_t tokens, int64_t batch, int64_t max_q,
+                                      int64_t max_pages, int64_t num_pages, int64_t heads, int64_t kv_heads, int64_t head_dim, float scale, void* stream);
+
 /* Attention of q_len queries to kv_len keys and values of another source, or of the same one, without a causal mask: q [batch][q_len][heads],
  * k, v [batch][kv_len][kv_heads], vectors of head_dim fp16 values, each dimension with a stride of its own in values (a multiple of 8,
  * GPUSQ_ERR_ALIGN; not negative), so that heads may lie in a packed projection or apart.
@@ -421,6 +429,51 @@ gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, 
                                    int64_t head_dim, int64_t q_batch_stride, int64_t q_stride, int64_t q_head_stride,
                                    int64_t k_batch_stride, int64_t k_stride, int64_t k_head_stride, int64_t v_batch_stride,
                                    int64_t v_stride, int64_t v_head_stride, float scale, void* stream);
+
+/* ---- answers with drafted tokens.  A step runs, for each sequence, the token that was answered last (node 0) and the tokens that something drafted
+ * behind it, a tree: node i is its i-th new token, parents[i] the number, in its sequence, of the node that it follows, one in front of it; any
+ * other number: none.  kv_lens counts all of them, cu_q and max_q (at most 512: GPUSQ_ERR_UNSUPPORTED) are as in attention over the cache.  Tokens
+ * that no sequence has, and nodes beyond max_q, are not written.
+ *
+ * gpusq_draft_tree, before the step: tree [tokens][ceil(max_q / 32)] with the bits of a node and of all that it follows; positions (or NULL) [tokens]:
+ *   tokens in front of the new ones, and the nodes that it follows; slots (or NULL) [tokens]: where the cache keeps it, through block_table
+ *   [batch][max_pages]; -1 where the table, or a page number that is negative or 2^25 and more, has no place. */
+gpusq_status gpusq_draft_tree(const int32_t* parents, const int32_t* kv_lens, const int32_t* cu_q, const int32_t* block_table, int32_t* tree, int32_t* positions,
+                              int32_t* slots, int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, void* stream);
+
+/* gpusq_accept_drafts, behind it: sampled [tokens] are the tokens drawn behind each node, drafted [tokens] the nodes' own.  Node 0 is kept; of the nodes
+ * that follow the last kept one the first (with a greater number) whose draft is what was drawn behind that is kept too, and so on; a negative
+ * drawn token is no node's draft.
+ *   path [batch][max_q]: the kept nodes, then -1; accepted [batch]: how many; answers [batch]: the token drawn behind the last (a sequence without
+ *   new tokens: 0 and -1); new_lens [batch]: tokens of the sequence with the kept ones (at least 0).
+ *   caches: a host array of `layers` (0 to 1024) device pointers to caches of the same sizes, none overlapping another (GPUSQ_ERR_UNSUPPORTED).  In each
+ *   the i-th kept node's place becomes the i-th new token's; kept tokens without a place in table or cache are not moved. */
+gpusq_status gpusq_accept_drafts(const int32_t* drafted, const int32_t* sampled, const int32_t* parents, const int32_t* kv_lens, const int32_t* cu_q,
+                                 const int32_t* block_table, void* const* caches, int64_t layers, int32_t* path, int32_t* accepted, int32_t* answers,
+                                 int32_t* new_lens, int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t num_pages, int64_t kv_heads,
+                                 int64_t head_dim, void* stream);
+
+/* Linear layers in 8-bit integers with a scale for each token and channel (a prompt's layers, the vocabulary's):
+ *   s_m = max|X[m]| / 127 (1 where that is 0), q = clamp(rint(X / s_m), -127, 127) with fp32 division, half to even, NaN 0: what gpusq_quantize_int8 gives
+ *   row by row;  Y [M][N] (out_dt GPUSQ_F16 or GPUSQ_F32) = act(fma(sum_k q[m][k] Wq[n][k] * s_m, w_scale[n], bias[n])), the sum exact, the rest in fp32;
+ *   GELU in its exact erf form.  X [M][K] fp16 or fp32 (dt), Wq [N][K] int8 with w_scale [N], from gpusq_quantize_int8 (GPUSQ_PER_ROW) or elsewhere.
+ *   K % 16 == 0, N % 4 == 0 (GPUSQ_ERR_UNSUPPORTED); K at most 132096, M at most 64 * 65535 (GPUSQ_ERR_SHAPE).  A token with an infinity gives NaN.
+ *   workspace: gpusq_linear_int8_tokens_workspace_bytes (0 for sizes that are refused); what it held does not matter. */
+size_t gpusq_linear_int8_tokens_workspace_bytes(int64_t M, int64_t K);
+gpusq_status gpusq_linear_int8_tokens(const void* X, gpusq_dtype dt, const int8_t* Wq, const float* w_scale, const float* bias, void* Y, gpusq_dtype out_dt,
+                                      void* workspace, int64_t M, int64_t N, int64_t K, int epilogue, void* stream);
+
+/* Tokens drawn from logits [rows][vocabulary] (dt GPUSQ_F16 or GPUSQ_F32, row_stride values from row to row, aligned to a value; at most 2^18 tokens,
+ * GPUSQ_ERR_SHAPE) with given random numbers, one in [0, 1) a row.  temperature, top_k, top_p, min_p: [rows] each, or NULL (1, and no cut).
+ *   A token's weight is exp((x - max) / temperature) in 64 bits, 0 below 2^-40; 1 where x is the greatest, also where that is infinite.  Tokens are
+ *   ordered by their logits, ties by their index, the lower first; -infinity and NaN are never drawn.  Kept are the first top_k (0 or less: all);
+ *   of those as many as it takes for top_p of their weight, one at least (1 and more: all); of those the ones of a weight of min_p or more (of the
+ *   first one's, which is 1; at most 1 is asked).
+ *   Drawn is the first token, in the vocabulary's order, at which the sum of the kept weights up to it passes random times their sum.  A temperature
+ *   that is not above 0: the first in the order.
+ *   tokens [rows]: its index, -1 where all logits are -infinity or NaN; probs [rows]: its share of the kept weight (there 0). */
+gpusq_status gpusq_sample_tokens(const void* logits, gpusq_dtype dt, int64_t row_stride, const float* random, const float* temperature, const int32_t* top_k,
+                                 const float* top_p, const float* min_p, int32_t* tokens, float* probs, int64_t rows, int64_t vocabulary, void* stream);
 
 #ifdef __cplusplus
 }

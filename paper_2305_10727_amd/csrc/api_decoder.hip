@@ -2,12 +2,19 @@
 #include <math.h>
 
 #include "attend_plan.h"
+#include "drafts_plan.h"
 #include "kv4.h"
 
 using namespace gpusq;
 
 namespace {
 constexpr int64_t kMaxElems = (int64_t)1 << 40;
+
+// sums of products of codes, -128 the least of a weight's, stay in 32 bits
+constexpr int64_t kMostTokens8K = INT32_MAX / (127 * 128) / 64 * 64;
+// a row's weights as whole numbers: together in 62 bits, the least (2^-40) 16 or more
+constexpr int64_t kMostVocabulary = (int64_t)1 << 18;
+double sample_one(int64_t) { return 0x1p44; }
 
 constexpr int64_t kMostPages = INT32_MAX / kPageTokens - 1;  // of a sequence: tokens are counted in 31 bits, a page beyond the last too
 
@@ -48,6 +55,32 @@ bool score_scale(float given, int64_t D, float* scale) {
   *scale = given == 0.0f ? 1.0f / sqrtf((float)D) : given;
   return *scale > 0.0f && *scale <= 3.4e38f;
 }
+
+// attention over the cache, causal or of a tree: sizes, workspace and pointers
+gpusq_status attend_kv4(AttentionKv4 x, hipStream_t s) {
+  if (!x.q || !x.cache || !x.block_table || !x.kv_lens || !x.out) return GPUSQ_ERR_NULL;
+  gpusq_status st = check_heads(x.heads, x.kv_heads, x.head_dim);
+  if (st != GPUSQ_OK) return st;
+  if (!are_kv4_sizes(x.tokens, x.batch, x.max_q, x.max_pages, x.heads, x.head_dim) || !is_size(x.num_pages) || (!x.cu_q && x.tokens != x.batch * x.max_q))
+    return GPUSQ_ERR_SHAPE;
+  if (!score_scale(x.scale, x.head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
+  const AttendParts p = attend_parts(true, x.batch, x.max_q, x.heads, x.kv_heads, x.head_dim, x.max_pages * kPageTokens);
+  if (!is_launchable(true, x.batch, x.max_q, x.tokens, x.heads, x.kv_heads, x.head_dim, p, true)) return GPUSQ_ERR_SHAPE;
+  if (p.parts > 1 && !x.workspace) return GPUSQ_ERR_NULL;
+  if (!aligned16(x.q) || !aligned16(x.cache) || !aligned16(x.out) || !aligned16(x.workspace) || !aligned4(x.block_table) || !aligned4(x.kv_lens) || !aligned4(x.cu_q))
+    return GPUSQ_ERR_ALIGN;
+  return launch_attention_kv4(x, s);
+}
+
+// the new tokens of sequences, with a tree of at most kMostDrafts each
+gpusq_status check_drafts(int64_t tokens, int64_t batch, int64_t max_q, const int32_t* cu_q) {
+  if (!is_size(tokens) || !is_size(batch) || !is_size(max_q) || max_q > tokens || (!cu_q && tokens != batch * max_q) || !launchable(batch, 256)) return GPUSQ_ERR_SHAPE;
+  return max_q <= kMostDrafts ? GPUSQ_OK : GPUSQ_ERR_UNSUPPORTED;
+}
+
+// codes of M tokens of K values in the workspace, rows of whole steps of 64; their scales behind them
+bool are_tokens8(int64_t M, int64_t K) { return is_size(M) && is_size(K) && K <= kMostTokens8K && ceil_div(M, 64) <= 65535 && M * K <= kMaxElems; }
+size_t tokens8_scales_at(int64_t M, int64_t K) { return (size_t)M * ceil_div(K, 64) * 64; }
 
 size_t parts_bytes(const AttendParts& p, int64_t tokens, int64_t heads, int64_t D) {
   return p.parts > 1 ? (size_t)p.parts * tokens * heads * (D + 2) * 4 : 0;
@@ -124,18 +157,19 @@ size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_
 gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* kv_lens, const int32_t* cu_q, void* out,
                                  void* workspace, int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t num_pages, int64_t heads,
                                  int64_t kv_heads, int64_t head_dim, float scale, void* stream) {
-  if (!q || !cache || !block_table || !kv_lens || !out) return GPUSQ_ERR_NULL;
-  gpusq_status st = check_heads(heads, kv_heads, head_dim);
-  if (st != GPUSQ_OK) return st;
-  if (!are_kv4_sizes(tokens, batch, max_q, max_pages, heads, head_dim) || !is_size(num_pages) || (!cu_q && tokens != batch * max_q)) return GPUSQ_ERR_SHAPE;
-  AttentionKv4 x{q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim, 0.0f};
-  if (!score_scale(scale, head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
-  const AttendParts p = attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens);
-  if (!is_launchable(true, batch, max_q, tokens, heads, kv_heads, head_dim, p, true)) return GPUSQ_ERR_SHAPE;
-  if (p.parts > 1 && !workspace) return GPUSQ_ERR_NULL;
-  if (!aligned16(q) || !aligned16(cache) || !aligned16(out) || !aligned16(workspace) || !aligned4(block_table) || !aligned4(kv_lens) || !aligned4(cu_q))
-    return GPUSQ_ERR_ALIGN;
-  return launch_attention_kv4(x, (hipStream_t)stream);
+  return attend_kv4(AttentionKv4{q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim, scale},
+                    (hipStream_t)stream);
+}
+
+gpusq_status gpusq_attention_tree_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* kv_lens, const int32_t* cu_q,
+                                      const int32_t* tree, int64_t tree_words, void* out, void* workspace, int64_t tokens, int64_t batch, int64_t max_q,
+                                      int64_t max_pages, int64_t num_pages, int64_t heads, int64_t kv_heads, int64_t head_dim, float scale, void* stream) {
+  if (!tree) return GPUSQ_ERR_NULL;
+  if (!is_size(max_q) || !is_size(tree_words) || tree_words < ceil_div(max_q, 32) || tokens > INT32_MAX / 2) return GPUSQ_ERR_SHAPE;
+  if (!aligned4(tree)) return GPUSQ_ERR_ALIGN;
+  return attend_kv4(AttentionKv4{q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim, scale,
+                                 tree, tree_words},
+                    (hipStream_t)stream);
 }
 
 size_t gpusq_cross_attention_workspace_bytes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads, int64_t kv_heads, int64_t head_dim) {
@@ -164,6 +198,79 @@ gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, 
   if (p.parts > 1 && !workspace) return GPUSQ_ERR_NULL;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(workspace) || !aligned4(kv_lens)) return GPUSQ_ERR_ALIGN;
   return launch_cross_attention(x, (hipStream_t)stream);
+}
+
+gpusq_status gpusq_draft_tree(const int32_t* parents, const int32_t* kv_lens, const int32_t* cu_q, const int32_t* block_table, int32_t* tree, int32_t* positions,
+                              int32_t* slots, int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, void* stream) {
+  if (!parents || !kv_lens || !tree || (slots && !block_table)) return GPUSQ_ERR_NULL;
+  gpusq_status st = check_drafts(tokens, batch, max_q, cu_q);
+  if (st != GPUSQ_OK) return st;
+  if (slots && (!is_size(max_pages) || max_pages > kMostPages)) return GPUSQ_ERR_SHAPE;
+  if (!aligned4(parents) || !aligned4(kv_lens) || !aligned4(cu_q) || !aligned4(block_table) || !aligned4(tree) || !aligned4(positions) || !aligned4(slots))
+    return GPUSQ_ERR_ALIGN;
+  return launch_draft_tree(DraftArgs{kv_lens, cu_q, (int)tokens, (int)batch, (int)max_q}, parents, block_table, max_pages, tree, ceil_div(max_q, 32), positions, slots,
+                           (hipStream_t)stream);
+}
+
+gpusq_status gpusq_accept_drafts(const int32_t* drafted, const int32_t* sampled, const int32_t* parents, const int32_t* kv_lens, const int32_t* cu_q,
+                                 const int32_t* block_table, void* const* caches, int64_t layers, int32_t* path, int32_t* accepted, int32_t* answers,
+                                 int32_t* new_lens, int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t num_pages, int64_t kv_heads,
+                                 int64_t head_dim, void* stream) {
+  if (!drafted || !sampled || !parents || !kv_lens || !path || !accepted || !answers || !new_lens) return GPUSQ_ERR_NULL;
+  if (layers != 0 && (!caches || !block_table)) return GPUSQ_ERR_NULL;
+  gpusq_status st = check_drafts(tokens, batch, max_q, cu_q);
+  if (st != GPUSQ_OK) return st;
+  if (layers < 0 || layers > 1024 || batch * max_q > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (layers != 0) {
+    st = check_heads(kv_heads, kv_heads, head_dim);
+    if (st != GPUSQ_OK) return st;
+    if (!is_size(max_pages) || max_pages > kMostPages || !is_size(num_pages) || num_pages > INT32_MAX / kPageTokens || caches_of_launch(batch, kv_heads) < 1)
+      return GPUSQ_ERR_SHAPE;
+    const int64_t bytes = num_pages * kv_heads * page_bytes(padded_head((int)head_dim));
+    for (int64_t i = 0; i < layers; ++i) {
+      if (!caches[i]) return GPUSQ_ERR_NULL;
+      if (!aligned16(caches[i])) return GPUSQ_ERR_ALIGN;
+      for (int64_t j = 0; j < i; ++j)  // (the same tokens moved twice)
+        if (overlap(ByteRange{caches[i], bytes}, ByteRange{caches[j], bytes})) return GPUSQ_ERR_UNSUPPORTED;
+    }
+  }
+  if (!aligned4(drafted) || !aligned4(sampled) || !aligned4(parents) || !aligned4(kv_lens) || !aligned4(cu_q) || !aligned4(block_table) || !aligned4(path) ||
+      !aligned4(accepted) || !aligned4(answers) || !aligned4(new_lens))
+    return GPUSQ_ERR_ALIGN;
+  return launch_accept_drafts(DraftArgs{kv_lens, cu_q, (int)tokens, (int)batch, (int)max_q}, drafted, sampled, parents, block_table, max_pages, path, accepted, answers,
+                              new_lens, caches, layers, num_pages, layers != 0 ? kv_heads : 1, layers != 0 ? head_dim : 64, (hipStream_t)stream);
+}
+
+size_t gpusq_linear_int8_tokens_workspace_bytes(int64_t M, int64_t K) {
+  if (!are_tokens8(M, K)) return 0;
+  return tokens8_scales_at(M, K) + (size_t)ceil_div(M, 4) * 16;
+}
+
+gpusq_status gpusq_linear_int8_tokens(const void* X, gpusq_dtype dt, const int8_t* Wq, const float* w_scale, const float* bias, void* Y, gpusq_dtype out_dt,
+                                      void* workspace, int64_t M, int64_t N, int64_t K, int epilogue, void* stream) {
+  if (!X || !Wq || !w_scale || !Y || !workspace || ((epilogue & GPUSQ_EPI_BIAS) && !bias)) return GPUSQ_ERR_NULL;
+  if (!are_tokens8(M, K) || !is_size(N) || M * N > kMaxElems || N * K > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (K % 16 != 0 || N % 4 != 0 || (dt != GPUSQ_F16 && dt != GPUSQ_F32) || (out_dt != GPUSQ_F16 && out_dt != GPUSQ_F32) ||
+      (epilogue & ~(GPUSQ_EPI_BIAS | GPUSQ_EPI_GELU)))
+    return GPUSQ_ERR_UNSUPPORTED;
+  if (!aligned16(X) || !aligned16(Wq) || !aligned16(w_scale) || !aligned16(bias) || !aligned16(Y) || !aligned16(workspace)) return GPUSQ_ERR_ALIGN;
+  Linear8Args a{X, dt == GPUSQ_F32, Wq, w_scale, bias, Y, out_dt == GPUSQ_F32, epilogue, (int)M, (int)N, (int)K, (int8_t*)workspace,
+                (float*)((uint8_t*)workspace + tokens8_scales_at(M, K)), ceil_div(K, 64) * 64};
+  return launch_linear_int8_tokens(a, (hipStream_t)stream);
+}
+
+gpusq_status gpusq_sample_tokens(const void* logits, gpusq_dtype dt, int64_t row_stride, const float* random, const float* temperature, const int32_t* top_k,
+                                 const float* top_p, const float* min_p, int32_t* tokens, float* probs, int64_t rows, int64_t vocabulary, void* stream) {
+  if (!logits || !random || !tokens || !probs) return GPUSQ_ERR_NULL;
+  if (!is_size(rows) || !is_size(vocabulary) || vocabulary > kMostVocabulary || row_stride < vocabulary || row_stride > INT32_MAX || rows * row_stride > kMaxElems ||
+      !launchable(rows, 1024))
+    return GPUSQ_ERR_SHAPE;
+  if (dt != GPUSQ_F16 && dt != GPUSQ_F32) return GPUSQ_ERR_UNSUPPORTED;
+  if (((uintptr_t)logits & (dt == GPUSQ_F32 ? 3u : 1u)) != 0 || !aligned4(random) || !aligned4(temperature) || !aligned4(top_k) || !aligned4(top_p) || !aligned4(min_p) ||
+      !aligned4(tokens) || !aligned4(probs))
+    return GPUSQ_ERR_ALIGN;
+  const SampleArgs a{logits, row_stride, random, temperature, top_p, min_p, top_k, tokens, probs, (int)vocabulary, sample_one(vocabulary)};
+  return launch_sample_tokens(a, dt == GPUSQ_F32, rows, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -33,6 +33,8 @@ struct AttendArgs {
   const uint8_t* cache;
   const int32_t *table, *cu_q;
   int max_pages, num_pages, tokens;
+  const int32_t* tree;  // [token][tree_words]: which of its sequence's new tokens a token sees (NULL: those up to itself)
+  int tree_words;
   // over fp16 states
   const _Float16 *k, *v;
   int64_t k_batch, k_token, k_head, v_batch, v_token, v_head;
@@ -109,6 +111,16 @@ struct Span {
     return limit < len ? limit : len;
   }
 };
+
+// A tree of drafted tokens: which of the 32 keys from key0 on (all in the cache: len) the column with the words `row` sees, a bit each.  Keys in front of
+// the new tokens are seen by all.  Words beyond a row's last are none.
+__device__ __forceinline__ unsigned tree_keys(const int32_t* row, int words, int before, int len, int key0) {
+  const int node = key0 - before, at = node >> 5;
+  auto word = [&](int i) { return i < 0 ? ~0u : i < words ? (unsigned)row[i] : 0u; };
+  const unsigned seen = __builtin_amdgcn_alignbit(word(at + 1), word(at), node & 31);
+  const int left = len - key0;
+  return left >= 32 ? seen : left > 0 ? seen & ((1u << left) - 1) : 0u;
+}
 
 // (One instruction.  A NaN is passed on, which fmaxf would leave out, with another instruction for each operand to see to it: a column with a
 // NaN among its scores has no other value.)

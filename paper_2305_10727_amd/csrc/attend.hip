@@ -43,7 +43,8 @@ struct Values4 {
 constexpr int waves_per_simd(bool kv4, int DP, int QT) { return DP > 128 ? 1 : QT == 1 ? (kv4 || DP == 64 ? 4 : 3) : 2; }
 
 // KV4: over the cache, else fp16 states.  QT: blocks of 16 columns, the same ones for each of WK wavefronts, which deal out the keys and join
-// their sums in LDS.
+// their sums in LDS.  MASKED: over the cache a tree of new tokens, whose words are looked at for the last tiles only, those that reach behind the
+// history; over states a mask of bytes.
 template <bool KV4, int DP, int QT, int WK, bool MASKED>
 __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_few_kernel(const AttendArgs a) {
   constexpr int J = DP / 32, CH = DP / 16;
@@ -55,8 +56,17 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
   if (col0 >= cols) return;  // the whole workgroup, like above
   Columns<KV4, DP, QT> x;
   x.load(a, span, w.kh, g, r, [&](int i) { return col0 + 16 * i; });
-  const int least = span.sees(col0 / a.rep);  // every column sees the keys in front of it, none those from `most` on
-  const int most = span.sees((col0 + 16 * QT < cols ? col0 + 16 * QT - 1 : cols - 1) / a.rep);
+  constexpr bool TREE = KV4 && MASKED;
+  const int least = TREE ? span.before : span.sees(col0 / a.rep);  // every column sees the keys in front of it, none those from `most` on
+  const int most = TREE ? len : span.sees((col0 + 16 * QT < cols ? col0 + 16 * QT - 1 : cols - 1) / a.rep);
+  const int32_t* words[TREE ? QT : 1];
+  if constexpr (TREE) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const int col = col0 + 16 * i + r < cols ? col0 + 16 * i + r : cols - 1;
+      words[i] = a.tree + (int64_t)(span.t0 + (a.rep == 1 ? col : col / a.rep)) * a.tree_words;
+    }
+  }
   const int tiles = most > 0 ? (most + 31) >> 5 : 0;
   const int begin = w.part * a.part_tiles, end = begin + a.part_tiles < tiles ? begin + a.part_tiles : tiles;
   // The first keys, values and the queries are waited for together, in front of the loop: left to itself the compiler waits at its top, for
@@ -102,7 +112,16 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       next = page_of(after(ahead));
       const bool check = key0 + 32 > least || !there;
       h8 p[QT];
-      if (check) x.hide(s, [&](int i, int t, int e) { return key0 + 16 * t + 4 * g + e >= (there ? x.limit[i] : 0); });
+      if constexpr (TREE) {
+        if (check) {
+          unsigned seen[QT];
+#pragma unroll
+          for (int i = 0; i < QT; ++i) seen[i] = there ? tree_keys(words[i], a.tree_words, least, len, key0) >> (4 * g) : 0u;
+          x.hide(s, [&](int i, int t, int e) { return (seen[i] >> (16 * t + e) & 1) == 0; });
+        }
+      } else if (check) {
+        x.hide(s, [&](int i, int t, int e) { return key0 + 16 * t + 4 * g + e >= (there ? x.limit[i] : 0); });
+      }
       x.follow(s, a);
       x.weights(s, a.c, p);
       x.sum(p);
@@ -344,11 +363,9 @@ template <bool KV4, int DP, int QT, int WK>
 void launch_shape(AttendArgs a, hipStream_t s) {
   a.col_blocks = (int)ceil_div((int64_t)a.q_len * a.rep, 16 * QT);
   const unsigned blocks = Work::workgroups(a);
-  if constexpr (!KV4) {
-    if (a.mask != nullptr) {
-      attend_few_kernel<KV4, DP, QT, WK, true><<<blocks, 64 * WK, 0, s>>>(a);
-      return;
-    }
+  if (KV4 ? a.tree != nullptr : a.mask != nullptr) {
+    attend_few_kernel<KV4, DP, QT, WK, true><<<blocks, 64 * WK, 0, s>>>(a);
+    return;
   }
   attend_few_kernel<KV4, DP, QT, WK, false><<<blocks, 64 * WK, 0, s>>>(a);
 }
@@ -425,6 +442,8 @@ gpusq_status launch_attention_kv4(const AttentionKv4& x, hipStream_t s) {
   a.cache = (const uint8_t*)x.cache;
   a.table = x.block_table;
   a.cu_q = x.cu_q;
+  a.tree = x.tree;
+  a.tree_words = (int)x.tree_words;
   a.max_pages = (int)x.max_pages;
   a.num_pages = (int)x.num_pages;
   a.tokens = (int)x.tokens;

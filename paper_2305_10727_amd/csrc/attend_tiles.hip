@@ -177,14 +177,15 @@ constexpr int tile_waves_per_simd(bool kv4, int DP, bool masked) { return kv4 ||
 constexpr int state_buffers(int DP) { return DP == 64 ? 4 : 2; }  // (a mask's bytes come one tile ahead of two buffers)
 
 template <bool KV4, int DP, int QT, int NW, int KT, int NB, bool MASKED>
-__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED)) attend_tiles_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED && !KV4)) attend_tiles_kernel(const AttendArgs a) {
   static_assert(NB == 2 || (NB == 4 && !KV4), "the waits for copies");
-  static_assert(!MASKED || NB == 2, "bytes of one tile");
+  constexpr bool BYTES = MASKED && !KV4, TREE = MASKED && KV4;
+  static_assert(!BYTES || NB == 2, "bytes of one tile");
   static_assert(QT <= 2, "count below QT is 1 or 0");
   static_assert(NB * KT <= kMostAhead, "key0 + NB * KT");
   constexpr int J = DP / 32, CH = DP / 16, NT = 64 * NW, kTile = KT * kRow<DP>;
   __shared__ __attribute__((aligned(16))) uint8_t lds[NB * 2 * kTile];  // [buffer][keys, values]
-  __shared__ __attribute__((aligned(16))) float begin[MASKED ? NB * KT + 4 : 4];
+  __shared__ __attribute__((aligned(16))) float begin[BYTES ? NB * KT + 4 : 4];
   __shared__ int pages[2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
   Work w;
@@ -195,30 +196,38 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
   if (w.block >= groups) return;
   const ColumnShare share = column_share(col_tiles, groups, w.block);
   const int tile0 = share.first, tile1 = share.last;
-  const int least = span.sees(16 * (tile0 + wave) / a.rep);
+  const int least = TREE ? span.before : span.sees(16 * (tile0 + wave) / a.rep);
   const int last = 16 * tile1 < cols ? 16 * tile1 - 1 : cols - 1;
-  const int most = span.sees(last / a.rep);
+  const int most = TREE ? span.len : span.sees(last / a.rep);
   const KeyRange keys = keys_of_part(w.part, a.part_tiles, most);
   const int first_key = keys.begin, end_key = keys.end;
-  typedef typename std::conditional<KV4, Codes<DP, KT, NW>, States<DP, KT, NW, MASKED>>::type Stage;
+  typedef typename std::conditional<KV4, Codes<DP, KT, NW>, States<DP, KT, NW, BYTES>>::type Stage;
   Stage stage(a, w, span.len, wave, lane, lds, begin, first_key);
-  if (!KV4 && (MASKED || a.D < DP)) {  // the pieces beyond the head, and rows that are not copied: zeros, once
+  if (!KV4 && (BYTES || a.D < DP)) {  // the pieces beyond the head, and rows that are not copied: zeros, once
     for (int i = threadIdx.x; i < NB * 2 * kTile / 16; i += NT) ((u4*)lds)[i] = u4(0);
-    if (MASKED && threadIdx.x == 0) begin[NB * KT] = 0.0f;
+    if (BYTES && threadIdx.x == 0) begin[NB * KT] = 0.0f;
     __syncthreads();
   }
   if constexpr (KV4) {
     if (first_key < end_key) stage.load(0, first_key);
   } else {
-    if (MASKED && first_key < end_key) stage.look(first_key);
+    if (BYTES && first_key < end_key) stage.look(first_key);
 #pragma unroll
     for (int i = 0; i < NB - 1; ++i)
       if (first_key + i * KT < end_key) stage.load(i, first_key + i * KT);
-    if (MASKED && first_key + KT < end_key) stage.look(first_key + KT);
+    if (BYTES && first_key + KT < end_key) stage.look(first_key + KT);
   }
   Columns<KV4, DP, QT> x;
   // (block i of a wavefront beyond the workgroup's last: columns that are no columns)
   x.load(a, span, w.kh, g, r, [&](int i) { return tile0 + wave + NW * i < tile1 ? 16 * (tile0 + wave + NW * i) : cols; });
+  const int32_t* words[TREE ? QT : 1];
+  if constexpr (TREE) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const int col = 16 * (tile0 + wave + NW * i) + r < cols ? 16 * (tile0 + wave + NW * i) + r : cols - 1;
+      words[i] = a.tree + (int64_t)(span.t0 + col / a.rep) * a.tree_words;
+    }
+  }
   // The queries are waited for here: their first use is inside the loop, where the compiler, which does not know of the copies to LDS, would
   // wait for all of these as well, in every turn.
   __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
@@ -241,7 +250,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
       f4 s[N][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const f4 begins = MASKED ? *(const f4*)&begin[buf * KT + 32 * half + 16 * t + 4 * g] : f4(0);
+        const f4 begins = BYTES ? *(const f4*)&begin[buf * KT + 32 * half + 16 * t + 4 * g] : f4(0);
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i][t] = begins;
 #pragma unroll
@@ -253,7 +262,16 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
       }
       h8 p[N];
       const int at = key0 + 32 * half + 4 * g;
-      if (!MASKED && (!there || key0 + 32 * half + 32 > least)) x.hide(s, [&](int i, int t, int e) { return at + 16 * t + e >= (there ? x.limit[i] : 0); });
+      if constexpr (TREE) {
+        if (!there || key0 + 32 * half + 32 > least) {
+          unsigned seen[N];
+#pragma unroll
+          for (int i = 0; i < N; ++i) seen[i] = there ? tree_keys(words[i], a.tree_words, least, span.len, key0 + 32 * half) >> (4 * g) : 0u;
+          x.hide(s, [&](int i, int t, int e) { return (seen[i] >> (16 * t + e) & 1) == 0; });
+        }
+      } else if (!BYTES && (!there || key0 + 32 * half + 32 > least)) {
+        x.hide(s, [&](int i, int t, int e) { return at + 16 * t + e >= (there ? x.limit[i] : 0); });
+      }
       x.follow(s, a);
       x.weights(s, a.c, p);
       x.sum(p);
@@ -303,7 +321,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
           asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (key0 + (NB - 1) * KT < end_key) {
           stage.load(buf == 0 ? NB - 1 : buf - 1, key0 + (NB - 1) * KT);
-          if (MASKED && key0 + NB * KT < end_key) stage.look(key0 + NB * KT);
+          if (BYTES && key0 + NB * KT < end_key) stage.look(key0 + NB * KT);
         }
         if constexpr (decltype(blocks)::value > 0) multiply(blocks, buf, key0, true);
         buf = buf + 1 < NB ? buf + 1 : 0;
@@ -319,7 +337,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED))
   else
     run(std::integral_constant<int, 0>());
   // Columns that see nothing have nothing, also where a query is no number: -inf, which the scores of hidden keys begin at, and NaN are NaN.
-  if constexpr (MASKED) {
+  if constexpr (BYTES) {
     if (stage.seen != 0) begin[NB * KT] = 1.0f;  // (whoever writes it: the same)
     __syncthreads();
     if (begin[NB * KT] == 0.0f) x.clear();
@@ -332,11 +350,9 @@ void launch_shape(AttendArgs a, hipStream_t s) {
   static_assert(16 * QT * NW == tiles_columns(KV4, DP) && 64 * NW == tiles_threads(KV4), "as the host counts workgroups");
   a.col_blocks = (int)ceil_div((int64_t)a.q_len * a.rep, 16 * QT * NW);
   const unsigned blocks = Work::workgroups(a);
-  if constexpr (!KV4) {
-    if (a.mask != nullptr) {
-      attend_tiles_kernel<KV4, DP, QT, NW, KT, 2, true><<<blocks, 64 * NW, 0, s>>>(a);
-      return;
-    }
+  if (KV4 ? a.tree != nullptr : a.mask != nullptr) {
+    attend_tiles_kernel<KV4, DP, QT, NW, KT, 2, true><<<blocks, 64 * NW, 0, s>>>(a);
+    return;
   }
   attend_tiles_kernel<KV4, DP, QT, NW, KT, NB, false><<<blocks, 64 * NW, 0, s>>>(a);
 }

@@ -512,6 +512,8 @@ struct AttentionKv4 {
   void *out, *workspace;
   int64_t tokens, batch, max_q, max_pages, num_pages, heads, kv_heads, head_dim;
   float scale;
+  const int32_t* tree = nullptr;  // [tokens][tree_words] or NULL: causal
+  int64_t tree_words = 0;
 };
 struct CrossAttention {
   const void *q, *k, *v;
@@ -528,6 +530,38 @@ struct AttendParts {
 AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys);
 gpusq_status launch_attention_kv4(const AttentionKv4& x, hipStream_t s);
 gpusq_status launch_cross_attention(const CrossAttention& x, hipStream_t s);
+
+// answers with drafted tokens (drafts.hip, linear8.hip, sample.hip)
+struct DraftArgs;
+gpusq_status launch_draft_tree(const DraftArgs& a, const int32_t* parents, const int32_t* table, int64_t max_pages, int32_t* tree, int64_t words, int32_t* positions,
+                               int32_t* slots, hipStream_t s);
+gpusq_status launch_accept_drafts(const DraftArgs& a, const int32_t* drafted, const int32_t* sampled, const int32_t* parents, const int32_t* table, int64_t max_pages,
+                                  int32_t* path, int32_t* accepted, int32_t* answers, int32_t* new_lens, void* const* caches, int64_t layers, int64_t num_pages,
+                                  int64_t kv_heads, int64_t D, hipStream_t s);
+struct SampleArgs {
+  const void* logits;
+  int64_t row_stride;
+  const float *random, *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+  int32_t* tokens;
+  float* probs;
+  int V;
+  double one;  // what a weight of 1 is as a whole number
+};
+gpusq_status launch_sample_tokens(const SampleArgs& a, bool f32, int64_t rows, hipStream_t s);
+struct Linear8Args {
+  const void* X;
+  int x_f32;
+  const int8_t* W;
+  const float *w_scale, *bias;
+  void* Y;
+  int out_f32, epilogue;
+  int M, N, K;
+  int8_t* Xq;       // [M][pitch], zeros behind K
+  float* x_scale;   // [M]
+  int64_t pitch;
+};
+gpusq_status launch_linear_int8_tokens(const Linear8Args& a, hipStream_t s);
 
 inline gpusq_status check_launch() {
   hipError_t e = hipGetLastError();

@@ -7,6 +7,8 @@
 // Signature, one letter per C parameter:
 //   p  tensor, integer address or None (NULL)
 //   t  tensor on the GPU and contiguous (else ValueError), or None
+//   u  like t, on the current device (whose stream the call is made on)
+//   v  like u, of any strides
 //   i  integer (int, int64_t, an enum)
 //   f  float, up to two
 //   s  torch's current stream; takes no argument
@@ -40,7 +42,7 @@ struct FastCall {
   char sig[kMaxArgs + 1];
 };
 
-PyObject *s_data_ptr, *s_is_cuda, *s_is_contiguous;
+PyObject *s_data_ptr, *s_is_cuda, *s_is_contiguous, *s_get_device;
 PyObject *g_get_device, *g_get_stream, *g_raise;  // set by setup()
 
 bool address_of(PyObject* o, bool check, long* out) {
@@ -95,6 +97,35 @@ bool address_of(PyObject* o, bool check, long* out) {
   return !PyErr_Occurred();
 }
 
+// ... of a tensor on the GPU that calls are made on now (*device, asked once a call)
+bool address_on(PyObject* o, bool contiguous, long* device, long* out) {
+  if (o != Py_None) {
+    if (*device < 0) {
+      PyObject* dev = PyObject_CallNoArgs(g_get_device);
+      if (!dev) return false;
+      *device = PyLong_AsLong(dev);
+      Py_DECREF(dev);
+      if (PyErr_Occurred()) return false;
+    }
+    long of = -1;
+    if (THPVariable_CheckExact(o)) {
+      const at::Tensor& t = THPVariable_Unpack(o);
+      if (t.is_cuda()) of = t.get_device();
+    } else {
+      PyObject* n = PyObject_CallMethodNoArgs(o, s_get_device);  // (-1 of the host's)
+      if (!n) return false;
+      of = PyLong_AsLong(n);
+      Py_DECREF(n);
+      if (PyErr_Occurred()) return false;
+    }
+    if (of != *device) {
+      PyErr_SetString(PyExc_ValueError, of < 0 ? "gpusq works on device tensors only" : "gpusq works on tensors of the current device");
+      return false;
+    }
+  }
+  return address_of(o, contiguous, out);
+}
+
 bool current_stream(long* out) {
   PyObject* dev = PyObject_CallNoArgs(g_get_device);
   if (!dev) return false;
@@ -114,6 +145,7 @@ PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyObject* k
   long a[kMaxArgs] = {0};
   float x[kMaxFloats] = {0};
   int at = 0, to = 0, floats = 0;
+  long device = -1;
   for (int i = 0; i < f->n; ++i) {
     switch (f->sig[i]) {
       case 's':
@@ -126,6 +158,10 @@ PyObject* call(PyObject* self, PyObject* const* args, size_t nargsf, PyObject* k
       case 'f':
         x[floats] = (float)PyFloat_AsDouble(args[at++]);
         if (x[floats++] == -1.0f && PyErr_Occurred()) return nullptr;
+        break;
+      case 'u':
+      case 'v':
+        if (!address_on(args[at++], f->sig[i] == 'u', &device, &a[to++])) return nullptr;
         break;
       default:
         if (!address_of(args[at++], f->sig[i] == 't', &a[to++])) return nullptr;
@@ -161,8 +197,8 @@ PyObject* make(PyTypeObject* type, PyObject* args, PyObject*) {
   const size_t n = strlen(sig);
   int floats = 0;
   for (size_t i = 0; i < n; ++i) floats += sig[i] == 'f';
-  if (n > kMaxArgs || floats > kMaxFloats || strspn(sig, "ptifs") != n) {
-    PyErr_SetString(PyExc_ValueError, "signature: up to 24 of p, t, i, f, s, two of them f");
+  if (n > kMaxArgs || floats > kMaxFloats || strspn(sig, "ptuvifs") != n) {
+    PyErr_SetString(PyExc_ValueError, "signature: up to 24 of p, t, u, v, i, f, s, two of them f");
     return nullptr;
   }
   FastCall* f = (FastCall*)type->tp_alloc(type, 0);
@@ -277,6 +313,7 @@ PyMODINIT_FUNC PyInit__fastcall(void) {
   s_data_ptr = PyUnicode_InternFromString("data_ptr");
   s_is_cuda = PyUnicode_InternFromString("is_cuda");
   s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+  s_get_device = PyUnicode_InternFromString("get_device");
   PyObject* m = PyModule_Create(&g_module);
   if (!m || !s_data_ptr || !s_is_cuda || !s_is_contiguous) return nullptr;
   Py_INCREF(&g_type);

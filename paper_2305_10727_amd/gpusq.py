@@ -35,6 +35,7 @@ EXPORTS = [
     "gpusq_block_mlp_int8", "gpusq_block_mlp_int8_launches",
     "gpusq_int4_groups_packed_bytes", "gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_kv4_page_bytes",
     "gpusq_qk_norm_rope", "gpusq_attention_kv4_workspace_bytes", "gpusq_attention_kv4", "gpusq_cross_attention_workspace_bytes", "gpusq_cross_attention",
+    "gpusq_attention_tree_kv4", "gpusq_draft_tree", "gpusq_accept_drafts", "gpusq_linear_int8_tokens_workspace_bytes", "gpusq_linear_int8_tokens", "gpusq_sample_tokens",
 ]
 
 
@@ -47,7 +48,8 @@ class GpusqError(RuntimeError):
         super().__init__("%s: %s" % (where, msg))
 
 
-# C parameters of the calls that launch kernels (fastcall.cpp: p pointer, t checked tensor, i integer, f float, s the stream)
+# C parameters of the calls that launch kernels (fastcall.cpp: p pointer, t checked tensor, u one on the current device, v one with any strides, i integer,
+# f float, s the stream)
 _SIGNATURES = {
     "gpusq_prune_2to4": "tttiiis", "gpusq_cast_f16": "ttis", "gpusq_quantize_int8": "tittiiiits",
     "gpusq_quantize_tensor_int8_noalloc": "tittiiis", "gpusq_compress": "ttttiiis", "gpusq_check_2to4": "titiis",
@@ -64,7 +66,12 @@ _SIGNATURES = {
     "gpusq_int4_to_sparse_int8": "tttttiis", "gpusq_prune_n_of_m": "ttiiiis",
     "gpusq_quantize_groups_int4": "tittiis", "gpusq_pack_int4_groups": "ttitiis", "gpusq_linear_int4": "ttittiiiiis",
     "gpusq_qk_norm_rope": "piiiiiiittftttiiitttttis", "gpusq_attention_kv4": "tttttttiiiiiiiifs", "gpusq_cross_attention": "pppttttiiiiiiiiiiiiiiifs",
+    "gpusq_attention_tree_kv4": "uuuuuuiuuiiiiiiiifs", "gpusq_draft_tree": "uuuuuuuiiiis", "gpusq_accept_drafts": "uuuuuupiuuuuiiiiiiis",
+    "gpusq_linear_int8_tokens": "uiuuuuiuiiiis", "gpusq_sample_tokens": "viiuuuuuuuiis",
 }
+
+
+_UNCHECKED = str.maketrans("tuv", "ppp")
 
 
 class _Calls:
@@ -84,7 +91,7 @@ class _Calls:
         for n, sig in _SIGNATURES.items():
             assert len(sig) == len(getattr(L, n).argtypes), n
             address = ctypes.cast(getattr(L, n), ctypes.c_void_p).value
-            setattr(self, n, _fastcall.FastCall(n, address, sig if self._check else sig.replace("t", "p"), n == "gpusq_check_2to4"))
+            setattr(self, n, _fastcall.FastCall(n, address, sig if self._check else sig.translate(_UNCHECKED), n == "gpusq_check_2to4"))
         return self.__dict__[name]
 
 
@@ -194,7 +201,16 @@ def lib():
         L.gpusq_attention_kv4.argtypes = [vp] * 7 + [i64] * 8 + [cf, vp]
         L.gpusq_cross_attention_workspace_bytes.argtypes = [i64] * 6
         L.gpusq_cross_attention.argtypes = [vp] * 7 + [i64] * 15 + [cf, vp]
-        for name in ("gpusq_int4_groups_packed_bytes", "gpusq_kv4_page_bytes", "gpusq_attention_kv4_workspace_bytes", "gpusq_cross_attention_workspace_bytes"):
+        L.gpusq_attention_tree_kv4.argtypes = [vp] * 6 + [i64] + [vp] * 2 + [i64] * 8 + [cf, vp]
+        L.gpusq_draft_tree.argtypes = [vp] * 7 + [i64] * 4 + [vp]
+        L.gpusq_accept_drafts.argtypes = [vp] * 7 + [i64] + [vp] * 4 + [i64] * 7 + [vp]
+        L.gpusq_linear_int8_tokens_workspace_bytes.argtypes = [i64] * 2
+        L.gpusq_linear_int8_tokens.argtypes = [vp, ci] + [vp] * 4 + [ci, vp] + [i64] * 3 + [ci, vp]
+        L.gpusq_sample_tokens.argtypes = [vp, ci, i64] + [vp] * 7 + [i64] * 2 + [vp]
+        for name in ("gpusq_attention_tree_kv4", "gpusq_draft_tree", "gpusq_accept_drafts", "gpusq_linear_int8_tokens", "gpusq_sample_tokens"):
+            getattr(L, name).restype = ci
+        for name in ("gpusq_int4_groups_packed_bytes", "gpusq_kv4_page_bytes", "gpusq_attention_kv4_workspace_bytes", "gpusq_cross_attention_workspace_bytes",
+                     "gpusq_linear_int8_tokens_workspace_bytes"):
             getattr(L, name).restype = sz
         for name in ("gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_qk_norm_rope", "gpusq_attention_kv4", "gpusq_cross_attention"):
             getattr(L, name).restype = ci
@@ -587,10 +603,11 @@ def _workspace(like, given, nbytes):
     return given
 
 
-def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=None, scale=None, out=None, workspace=None):
+def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=None, scale=None, out=None, workspace=None, tree=None):
     """gpusq_attention_kv4: q [tokens,heads,head_dim] fp16, cache [pages,kv_heads,bytes], block_table [batch,max_pages] int32, kv_lens [batch] int32,
     cu_q [batch + 1] int32 (None: max_q queries each) -> [tokens,heads,head_dim] fp16.  max_q: the most queries of a sequence; by default 1 without
-    cu_q, and with it as many as there are tokens: every query is answered, at the cost of workgroups for that many of each sequence."""
+    cu_q, and with it as many as there are tokens: every query is answered, at the cost of workgroups for that many of each sequence.
+    tree [tokens, words] int32 (draft_tree): gpusq_attention_tree_kv4, new tokens see those of each other that their bits say instead of those in front."""
     _want(_is(q, torch.float16, -1, -1, -1), "q: [tokens, heads, head_dim] float16 on the GPU")
     tokens, heads, D = q.shape
     if max_q is None:
@@ -606,7 +623,13 @@ def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=None, scale=N
     else:
         _want(_is(out, torch.float16, tokens, heads, D), "out: [tokens, heads, head_dim] float16 on the GPU")
     workspace = _workspace(q, workspace, _size("gpusq_attention_kv4_workspace_bytes", tokens, batch, max_q, max_pages, heads, kv_heads, D))
-    calls.gpusq_attention_kv4(q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, pages, heads, kv_heads, D, 0.0 if scale is None else scale)
+    s = 0.0 if scale is None else scale
+    if tree is None:
+        calls.gpusq_attention_kv4(q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, pages, heads, kv_heads, D, s)
+    else:
+        _want(_is(tree, torch.int32, tokens, -1), "tree: [tokens, words] int32 on the GPU")
+        calls.gpusq_attention_tree_kv4(q, cache, block_table, kv_lens, cu_q, tree, tree.shape[1], out, workspace, tokens, batch, max_q, max_pages, pages, heads,
+                                       kv_heads, D, s)
     return out
 
 
@@ -631,3 +654,90 @@ def cross_attention(q, k, v, kv_lens=None, key_mask=None, scale=None, out=None, 
     calls.gpusq_cross_attention(q, k, v, kv_lens, key_mask, out, workspace, B, Tq, S, H, G, D, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
                                 0.0 if scale is None else scale)
     return out
+
+
+# ---- answers with drafted tokens
+def _drafts(parents, kv_lens, cu_q, max_q):
+    """tokens, batch and the most nodes of a sequence"""
+    i32 = torch.int32
+    _want(_is(parents, i32, -1), "parents: [tokens] int32 on the GPU")
+    _want(_is(kv_lens, i32, -1), "kv_lens: [batch] int32 on the GPU")
+    tokens, batch = parents.shape[0], kv_lens.shape[0]
+    _want(cu_q is None or _is(cu_q, i32, batch + 1), "cu_q: [batch + 1] int32 on the GPU")
+    if max_q is None:
+        max_q = tokens if cu_q is not None else tokens // max(batch, 1)
+    return tokens, batch, max_q
+
+
+def draft_tree(parents, kv_lens, block_table, cu_q=None, max_q=None):
+    """gpusq_draft_tree: parents [tokens] int32 (the number, in its sequence, of the node that each new token follows, or -1), kv_lens [batch] int32 with the new
+    tokens, block_table [batch,max_pages] int32, cu_q [batch + 1] int32 (None: max_q tokens each) -> (tree [tokens, ceil(max_q / 32)], positions [tokens],
+    slots [tokens]) int32: what attention_kv4, a table of positions and qk_norm_rope take.  max_q: the most new tokens of a sequence, 512 at most."""
+    i32 = torch.int32
+    tokens, batch, max_q = _drafts(parents, kv_lens, cu_q, max_q)
+    _want(_is(block_table, i32, batch, -1), "block_table: [batch, max_pages] int32 on the GPU")
+    tree, positions, slots = _empty(parents, i32, tokens, max(1, (max_q + 31) // 32)), _empty(parents, i32, tokens), _empty(parents, i32, tokens)
+    calls.gpusq_draft_tree(parents, kv_lens, cu_q, block_table, tree, positions, slots, tokens, batch, max_q, block_table.shape[1])
+    return tree, positions, slots
+
+
+def accept_drafts(drafted, sampled, parents, kv_lens, cu_q=None, max_q=None, caches=(), block_table=None):
+    """gpusq_accept_drafts: drafted, sampled, parents [tokens] int32 (a node's own token, the one drawn behind it, the node that it follows), kv_lens, cu_q and
+    max_q as in draft_tree -> (path [batch,max_q], accepted [batch], answers [batch], new lengths [batch]) int32.  In caches (kv4_cache tensors of one
+    size, a layer each) the kept tokens are moved together, through block_table."""
+    i32 = torch.int32
+    tokens, batch, max_q = _drafts(parents, kv_lens, cu_q, max_q)
+    _want(_is(drafted, i32, tokens) and _is(sampled, i32, tokens), "drafted, sampled: [tokens] int32 on the GPU")
+    layers = len(caches)
+    max_pages = pages = kv_heads = head_dim = 0
+    addresses = None
+    if layers:
+        _want(_is(block_table, i32, batch, -1), "block_table: [batch, max_pages] int32 on the GPU")
+        max_pages = block_table.shape[1]
+        _want(_is(caches[0], torch.uint8, -1, -1, -1), "caches: pages of kv4_cache")
+        pages, kv_heads, nbytes = caches[0].shape
+        head_dim = nbytes // 72  # (of the padded one: the places are the same)
+        _want(nbytes == _size("gpusq_kv4_page_bytes", 1, head_dim), "caches: pages of kv4_cache")
+        device = caches[0].get_device()
+        for c in caches:
+            _want(_is(c, torch.uint8, pages, kv_heads, nbytes) and c.is_contiguous() and c.get_device() == device, "caches: contiguous, of one size, on one GPU")
+        _want(device == torch.cuda.current_device(), "caches: on the current device")
+        addresses = (ctypes.c_void_p * layers)(*[c.data_ptr() for c in caches])
+    path = _empty(parents, i32, batch, max(1, max_q))
+    accepted, answers, new_lens = _empty(parents, i32, batch), _empty(parents, i32, batch), _empty(parents, i32, batch)
+    calls.gpusq_accept_drafts(drafted, sampled, parents, kv_lens, cu_q, block_table, None if addresses is None else ctypes.addressof(addresses), layers, path, accepted,
+                              answers, new_lens, tokens, batch, max_q, max_pages, pages, kv_heads, head_dim)
+    return path, accepted, answers, new_lens
+
+
+def linear_int8_tokens(X, Wq, w_scale, bias=None, gelu=False, out_dtype=torch.float16, out=None, workspace=None):
+    """gpusq_linear_int8_tokens: X [M,K] fp16 or fp32, Wq [N,K] int8 with w_scale [N] (quantize_int8 by rows) -> act(X W^T + bias) [M,N] fp16 or fp32, X in
+    8 bits with a scale for each row"""
+    f32 = torch.float32
+    _want(_is(X, torch.float16, -1, -1) or _is(X, f32, -1, -1), "X: [M, K] float16 or float32 on the GPU")
+    M, K = X.shape
+    _want(_is(Wq, torch.int8, -1, K), "Wq: [N, K] int8 on the GPU")
+    N = Wq.shape[0]
+    _want(_is(w_scale, f32, N) and (bias is None or _is(bias, f32, N)), "w_scale, bias: [N] float32 on the GPU")
+    if out is None:
+        out = _empty(X, out_dtype, M, N)
+    else:
+        _want(_is(out, out_dtype, M, N), "out: [M, N] of out_dtype on the GPU")
+    workspace = _workspace(X, workspace, max(_size("gpusq_linear_int8_tokens_workspace_bytes", M, K), 16))
+    calls.gpusq_linear_int8_tokens(X, _TORCH_DT[X.dtype], Wq, w_scale, bias, out, _TORCH_DT[out_dtype], workspace, M, N, K, _epi(bias, gelu))
+    return out
+
+
+def sample_tokens(logits, random, temperature=None, top_k=None, top_p=None, min_p=None):
+    """gpusq_sample_tokens: logits [rows,vocabulary] fp16 or fp32 (rows contiguous, any stride between them), random [rows] fp32 in [0, 1), temperature, top_p,
+    min_p [rows] fp32, top_k [rows] int32 (None: 1, no cut) -> (tokens [rows] int32, their shares of what was kept [rows] fp32)"""
+    f32, i32 = torch.float32, torch.int32
+    _want((_is(logits, torch.float16, -1, -1) or _is(logits, f32, -1, -1)) and (logits.stride(1) == 1 or logits.shape[1] == 1),
+          "logits: [rows, vocabulary] float16 or float32 on the GPU, rows contiguous")
+    R, V = logits.shape
+    _want(_is(random, f32, R), "random: [rows] float32 on the GPU")
+    for t, dt, name in ((temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"), (min_p, f32, "min_p")):
+        _want(t is None or _is(t, dt, R), "%s: [rows] %s on the GPU" % (name, "int32" if dt is i32 else "float32"))
+    tokens, probs = _empty(logits, i32, R), _empty(logits, f32, R)
+    calls.gpusq_sample_tokens(logits, _TORCH_DT[logits.dtype], logits.stride(0) if R > 1 else V, random, temperature, top_k, top_p, min_p, tokens, probs, R, V)
+    return tokens, probs
