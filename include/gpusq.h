@@ -457,7 +457,7 @@ gpusq_status gpusq_accept_drafts(const int32_t* drafted, const int32_t* sampled,
  *   s_m = max|X[m]| / 127 (1 where that is 0), q = clamp(rint(X / s_m), -127, 127) with fp32 division, half to even, NaN 0: what gpusq_quantize_int8 gives
  *   row by row;  Y [M][N] (out_dt GPUSQ_F16 or GPUSQ_F32) = act(fma(sum_k q[m][k] Wq[n][k] * s_m, w_scale[n], bias[n])), the sum exact, the rest in fp32;
  *   GELU in its exact erf form.  X [M][K] fp16 or fp32 (dt), Wq [N][K] int8 with w_scale [N], from gpusq_quantize_int8 (GPUSQ_PER_ROW) or elsewhere.
- *   K % 16 == 0, N % 4 == 0 (GPUSQ_ERR_UNSUPPORTED); K at most 132096, M at most 64 * 65535 (GPUSQ_ERR_SHAPE).  A token with an infinity gives NaN.
+ *   K % 16 == 0, N % 4 == 0 (GPUSQ_ERR_UNSUPPORTED); K at most 132096, N 2^24, M 64 * 65535 (GPUSQ_ERR_SHAPE).  A token with an infinity gives NaN.
  *   workspace: gpusq_linear_int8_tokens_workspace_bytes (0 for sizes that are refused); what it held does not matter. */
 size_t gpusq_linear_int8_tokens_workspace_bytes(int64_t M, int64_t K);
 gpusq_status gpusq_linear_int8_tokens(const void* X, gpusq_dtype dt, const int8_t* Wq, const float* w_scale, const float* bias, void* Y, gpusq_dtype out_dt,

@@ -49,7 +49,7 @@ def test_linear_int8_tokens(g):
     base = dict(X=P, dt=g.F16, Wq=P, w_scale=P, bias=P, Y=P, out_dt=g.F16, ws=P, M=3, N=64, K=128, epilogue=g.EPI_BIAS, stream=None)
     _refuses(g, "gpusq_linear_int8_tokens", base, [
         (ERR_NULL, dict(X=None)), (ERR_NULL, dict(Wq=None)), (ERR_NULL, dict(w_scale=None)), (ERR_NULL, dict(bias=None)), (ERR_NULL, dict(Y=None)), (ERR_NULL, dict(ws=None)), (ERR_SHAPE, dict(M=0)),
-        (ERR_SHAPE, dict(N=0)), (ERR_SHAPE, dict(K=0)), (ERR_SHAPE, dict(K=132112)), (ERR_SHAPE, dict(M=64 * 65535 + 1)), (ERR_SHAPE, dict(N=2**31)), (ERR_SHAPE, dict(M=2**21, N=2**20)),
+        (ERR_SHAPE, dict(N=0)), (ERR_SHAPE, dict(K=0)), (ERR_SHAPE, dict(K=132112)), (ERR_SHAPE, dict(M=64 * 65535 + 1)), (ERR_SHAPE, dict(N=2**24 + 4)), (ERR_SHAPE, dict(M=2**21, N=2**20)),
         (ERR_UNSUPPORTED, dict(K=120)), (ERR_UNSUPPORTED, dict(N=62)), (ERR_UNSUPPORTED, dict(dt=g.I8)), (ERR_UNSUPPORTED, dict(out_dt=g.I32)), (ERR_UNSUPPORTED, dict(epilogue=4)),
         (ERR_ALIGN, dict(X=ODD)), (ERR_ALIGN, dict(Wq=ODD)), (ERR_ALIGN, dict(w_scale=ODD)), (ERR_ALIGN, dict(bias=ODD)), (ERR_ALIGN, dict(Y=ODD)), (ERR_ALIGN, dict(ws=ODD))])
     size = g.lib().gpusq_linear_int8_tokens_workspace_bytes
