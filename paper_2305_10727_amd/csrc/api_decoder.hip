@@ -250,7 +250,7 @@ size_t gpusq_linear_int8_tokens_workspace_bytes(int64_t M, int64_t K) {
 gpusq_status gpusq_linear_int8_tokens(const void* X, gpusq_dtype dt, const int8_t* Wq, const float* w_scale, const float* bias, void* Y, gpusq_dtype out_dt,
                                       void* workspace, int64_t M, int64_t N, int64_t K, int epilogue, void* stream) {
   if (!X || !Wq || !w_scale || !Y || !workspace || ((epilogue & GPUSQ_EPI_BIAS) && !bias)) return GPUSQ_ERR_NULL;
-  if (!are_tokens8(M, K) || !is_size(N) || N > kMostTokens8N || M * N > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (!are_tokens8(M, K) || !is_size(N) || N > kMostTokens8N || !tokens8_countable(M, N) || M * N > kMaxElems) return GPUSQ_ERR_SHAPE;
   if (K % 16 != 0 || N % 4 != 0 || (dt != GPUSQ_F16 && dt != GPUSQ_F32) || (out_dt != GPUSQ_F16 && out_dt != GPUSQ_F32) ||
       (epilogue & ~(GPUSQ_EPI_BIAS | GPUSQ_EPI_GELU)))
     return GPUSQ_ERR_UNSUPPORTED;

@@ -1,5 +1,5 @@
 // Linear layers in 8-bit integers with a scale for each token and each channel: Y = act(s_m w_n (q_m . c_n) + b_n), s_m = max|x_m| / 127,
-// q_m = clamp(rint(x_m / s_m)).  This file: the codes of the tokens, the kernel for few of them, the choice; linear8_tiles.hip: many tokens.
+// q_m = clamp(rint(x_m / s_m)).  This file: the codes of the tokens, the kernel for few of them, the choice; linear8_tiles.h: many tokens.
 //
 // Few tokens are bound by the bytes of the weights, one each; every other choice follows from reading them once, with much in flight:
 //   - the weights stay as they are, rows of K bytes: a wavefront reads 64 consecutive bytes of 16 rows with an instruction, and the next 64 with the next;
@@ -12,7 +12,10 @@
 
 namespace gpusq {
 
-void launch_linear8_tiles(const Linear8Args& a, const EvenPlan& plan, hipStream_t s);
+// linear8_tiles.h by the channels of a tile
+void launch_linear8_tiles8(const Linear8Args& a, const Tokens8Plan& plan, hipStream_t s);
+void launch_linear8_tiles4(const Linear8Args& a, const Tokens8Plan& plan, hipStream_t s);
+void launch_linear8_tiles2(const Linear8Args& a, const Tokens8Plan& plan, hipStream_t s);
 
 namespace {
 
@@ -20,7 +23,25 @@ typedef int i4v __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float token_scale(float most) { return most == 0.0f ? 1.0f : __fdiv_rn(most, 127.0f); }
 
-// 16 consecutive values in fp32
+// 16 consecutive values as they are
+template <typename T>
+struct Raw16 {
+  typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
+  vec v[sizeof(T)];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) v[i] = *(const vec*)(p + i * (16 / (int)sizeof(T)));
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) v[i] = vec(0);
+  }
+  __device__ __forceinline__ void values(float (&x)[16]) const {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = (float)v[e * sizeof(T) / 16][e % (16 / sizeof(T))];
+  }
+};
+// ... in fp32
 template <typename T>
 __device__ __forceinline__ void load16(const T* p, float (&x)[16]) {
   if constexpr (sizeof(T) == 4) {
@@ -123,11 +144,9 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) linear8_rows_kernel(const Lin
   const int nt = (a.N + 15) >> 4, steps = (a.K + 63) >> 6, chunks = CHUNKS ? (steps + NW * S - 1) / (NW * S) : 1;
   const int groups = (nt + NT - 1) / NT, m0 = blockIdx.y * 16 * MT;
   i4v* totals = lds + 2 * NW * NT * MT * 64;
-  struct Weights {
-    i4v w[NT][S];
-  };
+  i4v w[NT][S];
   // (a chunk behind the end of a row: the row's last, met by codes of 0; a row behind the last channel: that one, not stored)
-  auto load = [&](int chunk, int group, Weights& x) {
+  auto load = [&](int chunk, int group) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int n = (group * NT + t) * 16 + r;
@@ -135,26 +154,45 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) linear8_rows_kernel(const Lin
 #pragma unroll
       for (int i = 0; i < S; ++i) {
         const int k = ((chunk * NW + wave) * S + i) * 64 + 16 * g;
-        x.w[t][i] = *(const i4v*)(row + (k < a.K ? k : a.K - 16));
+        w[t][i] = *(const i4v*)(row + (k < a.K ? k : a.K - 16));
       }
     }
   };
-  Weights next;
-  load(0, blockIdx.x, next);
+  // the tokens that are quantised here, in registers from the range to the codes where they fit (asked for in front of the weights, which take longer)
+  constexpr bool HELD = HERE && !CHUNKS && S * sizeof(T) <= 12;
+  Raw16<T> raw[HELD ? S : 1];
+  const T* x = (const T*)a.X + (int64_t)(r < a.M ? r : a.M - 1) * a.K;  // (a column beyond the last token: zeros)
+  if constexpr (HELD) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      const int k = (wave * S + i) * 64 + 16 * g;
+      raw[i].zero();
+      if (r < a.M && k < a.K) raw[i].load(x + k);
+    }
+  }
+  load(0, blockIdx.x);
   float s_row = 1.0f, rs_row = 1.0f;
   if constexpr (HERE) {  // the tokens' ranges: a lane has token r, 16 values in 64
-    const T* x = (const T*)a.X + (int64_t)(r < a.M ? r : a.M - 1) * a.K;
     float most = 0.0f;
-    for (int chunk = 0; chunk < chunks; ++chunk)
+    if constexpr (HELD) {
 #pragma unroll
       for (int i = 0; i < S; ++i) {
-        const int k = ((chunk * NW + wave) * S + i) * 64 + 16 * g;
-        if (k < a.K) {
-          float v[16];
-          load16(x + k, v);
-          most = fmaxf(most, most_of(v));
-        }
+        float v[16];
+        raw[i].values(v);
+        most = fmaxf(most, most_of(v));
       }
+    } else {
+      for (int chunk = 0; chunk < chunks; ++chunk)
+#pragma unroll 2
+        for (int i = 0; i < S; ++i) {
+          const int k = ((chunk * NW + wave) * S + i) * 64 + 16 * g;
+          if (r < a.M && k < a.K) {
+            float v[16];
+            load16(x + k, v);
+            most = fmaxf(most, most_of(v));
+          }
+        }
+    }
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
     if (g == 0) ranges[wave][r] = most;
@@ -165,6 +203,15 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) linear8_rows_kernel(const Lin
     s_row = token_scale(most);
     rs_row = scale_reciprocal(s_row);
     if (threadIdx.x < 16) scales[r] = s_row;
+    // (what the range was taken of is not kept in 32 bits for the codes: these begin with the values, or with memory, again)
+    if constexpr (HELD) {
+#pragma unroll
+      for (int i = 0; i < S; ++i)
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T); ++j) asm volatile("" : "+v"(raw[i].v[j]));
+    } else {
+      asm volatile("" : "+v"(x));
+    }
   }
   int buf = 0, turn = 0;
   for (int chunk = 0; chunk < chunks; ++chunk) {
@@ -175,14 +222,19 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) linear8_rows_kernel(const Lin
       for (int i = 0; i < S; ++i) {
         const int k = ((chunk * NW + wave) * S + i) * 64 + 16 * g;
         if constexpr (HERE) {
-          b[m][i] = i4v(0);
-          if (k < a.K) {
-            float v[16];
-            unsigned c[4];
-            load16((const T*)a.X + (int64_t)(r < a.M ? r : a.M - 1) * a.K + k, v);
-            quantize_words<16>(v, s_row, rs_row, c, 127.0f);
-            b[m][i] = i4v{(int)c[0], (int)c[1], (int)c[2], (int)c[3]};
+          float v[16];
+          unsigned c[4];
+          if constexpr (HELD) {
+            raw[i].values(v);
+          } else {
+            Raw16<T> now;
+            now.zero();
+            if (r < a.M && k < a.K) now.load(x + k);
+            now.values(v);
           }
+          quantize_words<16>(v, s_row, rs_row, c, 127.0f);
+          b[m][i] = i4v{(int)c[0], (int)c[1], (int)c[2], (int)c[3]};
+          if (HELD || (i & 1)) __builtin_amdgcn_sched_barrier(0);  // (one after the other, or two: all of them side by side do not fit the registers)
         } else {
           const int row = m0 + 16 * m + r < a.M ? m0 + 16 * m + r : a.M - 1;  // (columns beyond the last token repeat it and are not stored)
           b[m][i] = k < (int)a.pitch ? *(const i4v*)(a.Xq + (int64_t)row * a.pitch + k) : i4v(0);
@@ -190,22 +242,28 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) linear8_rows_kernel(const Lin
       }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): else the loop waits for the tokens again, and with them for the next tile's weights
     for (int group = blockIdx.x, n = 0; group < groups; group += gridDim.x, ++n) {
-      const Weights now = next;
-      const int ahead = group + gridDim.x;
-      if constexpr (CHUNKS)
-        load(ahead < groups || chunk + 1 == chunks ? chunk : chunk + 1, ahead < groups ? ahead : chunk + 1 == chunks ? group : blockIdx.x, next);
-      else
-        load(0, ahead < groups ? ahead : group, next);  // (behind the last one: that one again)
-      i4v* part = lds + buf * NW * NT * MT * 64;
+      i4v acc[NT][MT];
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          i4v acc = i4v(0);
+          acc[t][m] = i4v(0);
 #pragma unroll
-          for (int i = 0; i < S; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(now.w[t][i], b[m][i], acc, 0, 0, 0);
-          part[((wave * NT + t) * MT + m) * 64 + lane] = acc;
+          for (int i = 0; i < S; ++i) acc[t][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[t][i], b[m][i], acc[t][m], 0, 0, 0);
         }
+      // the next weights, into the registers that have just been read
+      __builtin_amdgcn_sched_barrier(0);
+      const int ahead = group + gridDim.x;
+      if constexpr (CHUNKS)
+        load(ahead < groups || chunk + 1 == chunks ? chunk : chunk + 1, ahead < groups ? ahead : chunk + 1 == chunks ? group : blockIdx.x);
+      else
+        load(0, ahead < groups ? ahead : group);  // (behind the last one: that one again)
+      __builtin_amdgcn_sched_barrier(0);
+      i4v* part = lds + buf * NW * NT * MT * 64;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) part[((wave * NT + t) * MT + m) * 64 + lane] = acc[t][m];
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // (the next weights stay in flight)
       // NT MT wavefronts add up, others from turn to turn
       constexpr int JOBS = NT * MT;
@@ -213,8 +271,8 @@ __global__ void __launch_bounds__(64 * NW, NW / 4) linear8_rows_kernel(const Lin
       const int job = wave >= turn ? wave - turn : wave - turn + NW;
       if (job < JOBS) {
         i4v y = part[job * 64 + lane];
-#pragma unroll
-        for (int w = 1; w < NW; ++w) y += part[(w * JOBS + job) * 64 + lane];
+#pragma unroll 3
+        for (int v = 1; v < NW; ++v) y += part[(v * JOBS + job) * 64 + lane];  // (all at once they would take the registers of the weights)
         i4v* total = totals + (n * JOBS + job) * 64 + lane;
         if (CHUNKS && chunk > 0) y += *total;
         if (CHUNKS && chunk + 1 < chunks) {
@@ -244,42 +302,47 @@ void launch_rows(const Linear8Args& a, hipStream_t s) {
   else
     linear8_rows_kernel<T, MT, NW, S, NT, CHUNKS, false><<<grid, 64 * NW, lds, s>>>(a);
 }
-// up to 16 tokens: the fewest steps a wavefront that K needs
+// The fewest steps a wavefront that K needs, up to 64 steps.
 template <typename T>
-void launch_16(const Linear8Args& a, hipStream_t s) {
-  const int steps = (int)ceil_div(a.K, 64);
-  steps <= 16   ? launch_rows<T, 1, 1, 4, false>(a, s)
-  : steps <= 32 ? launch_rows<T, 1, 2, 2, false>(a, s)
-  : steps <= 64 ? launch_rows<T, 1, 4, 1, false>(a, s)
-                : launch_rows<T, 1, 4, 1, true>(a, s);
+void launch_16(const Linear8Args& a, int steps, hipStream_t s) {
+  steps <= 16 ? launch_rows<T, 1, 1, 4, false>(a, s) : steps <= 32 ? launch_rows<T, 1, 2, 2, false>(a, s) : launch_rows<T, 1, 4, 1, false>(a, s);
+}
+template <typename T>
+void launch_quantiser(const Linear8Args& a, hipStream_t s) {
+  const T* x = (const T*)a.X;
+  if (a.K <= 4096)
+    quantize_tokens_kernel<T, 1><<<(unsigned)a.M, 256, 0, s>>>(x, a.Xq, a.x_scale, a.K, (int)a.pitch);
+  else
+    quantize_tokens_kernel<T, 2><<<(unsigned)a.M, 256, 0, s>>>(x, a.Xq, a.x_scale, a.K, (int)a.pitch);
 }
 
 }  // namespace
 
 gpusq_status launch_linear_int8_tokens(const Linear8Args& a, hipStream_t s) {
-  if (a.M <= 16) {
-    a.x_f32 ? launch_16<float>(a, s) : launch_16<_Float16>(a, s);
+  const int steps = (int)ceil_div(a.K, 64);
+  // Tokens quantised by the product's own workgroups: a launch less, but each of them reads them all (4096 -> 4096: 8 tokens 12.7 us so, 12.4 with the
+  // quantiser's launch in front, 16 tokens 18.1 and 12.6), and up to K = 4096 they fit the registers beside the weights.
+  if (a.M <= 16 && steps <= 64 && (int64_t)a.M * a.K <= 32768) {
+    a.x_f32 ? launch_16<float>(a, steps, s) : launch_16<_Float16>(a, steps, s);
     return check_launch();
   }
-  const unsigned rows = (unsigned)a.M;
-  if (a.x_f32)
-    a.K <= 4096 ? quantize_tokens_kernel<float, 1><<<rows, 256, 0, s>>>((const float*)a.X, a.Xq, a.x_scale, a.K, (int)a.pitch)
-                : quantize_tokens_kernel<float, 2><<<rows, 256, 0, s>>>((const float*)a.X, a.Xq, a.x_scale, a.K, (int)a.pitch);
-  else
-    a.K <= 4096 ? quantize_tokens_kernel<_Float16, 1><<<rows, 256, 0, s>>>((const _Float16*)a.X, a.Xq, a.x_scale, a.K, (int)a.pitch)
-                : quantize_tokens_kernel<_Float16, 2><<<rows, 256, 0, s>>>((const _Float16*)a.X, a.Xq, a.x_scale, a.K, (int)a.pitch);
+  a.x_f32 ? launch_quantiser<float>(a, s) : launch_quantiser<_Float16>(a, s);
   gpusq_status st = check_launch();
   if (st != GPUSQ_OK) return st;
-  const int steps = (int)ceil_div(a.K, 64);
-  if (a.M <= 32)
+  if (a.M <= 16)
+    steps <= 64 ? launch_16<int8_t>(a, steps, s) : steps <= 96 ? launch_rows<int8_t, 1, 6, 1, false>(a, s) : steps <= 128 ? launch_rows<int8_t, 1, 8, 1, false>(a, s) : launch_rows<int8_t, 1, 8, 1, true>(a, s);
+  else if (a.M <= 32)
     steps <= 16   ? launch_rows<int8_t, 2, 1, 2, false>(a, s)
     : steps <= 32 ? launch_rows<int8_t, 2, 2, 1, false>(a, s)
     : steps <= 64 ? launch_rows<int8_t, 2, 4, 1, false>(a, s)
+    : steps <= 96 ? launch_rows<int8_t, 2, 6, 1, false>(a, s)
                   : launch_rows<int8_t, 2, 4, 1, true>(a, s);
-  else if (a.M <= 64)
-    steps <= 32 ? launch_rows<int8_t, 4, 2, 1, false>(a, s) : steps <= 64 ? launch_rows<int8_t, 4, 4, 1, false>(a, s) : launch_rows<int8_t, 4, 4, 1, true>(a, s);
-  else
-    launch_linear8_tiles(a, tokens8_plan(a.M, a.N, a.K, num_cus()).even, s);
+  else if (a.M <= 64 && steps <= 64 && a.N < 32768)
+    steps <= 32 ? launch_rows<int8_t, 4, 2, 1, false>(a, s) : launch_rows<int8_t, 4, 4, 1, false>(a, s);
+  else {
+    const Tokens8Plan plan = tokens8_plan(a.M, a.N, a.K, num_cus());
+    plan.tn == 8 ? launch_linear8_tiles8(a, plan, s) : plan.tn == 4 ? launch_linear8_tiles4(a, plan, s) : launch_linear8_tiles2(a, plan, s);
+  }
   return check_launch();
 }
 

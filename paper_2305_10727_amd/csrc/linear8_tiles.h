@@ -12,6 +12,7 @@
 // instructions of its first half: by then a wavefront has its last read of the step's stage, and its own copies of step g + 1 have landed.  Behind
 // it stage g + 1 is whole and is read ahead, and stage g is free for the copies of step g + R.
 // K that is no whole number of steps: the rows of codes have zeros behind their end, and the chunks of weights there are the step's first once more.
+#pragma once
 #include <type_traits>
 
 #include "gelu4.h"
@@ -22,12 +23,13 @@ namespace gpusq {
 
 namespace {
 
-template <int NX>
+// A stage: the tile's blocks of weights, then those of its rows.  A wavefront copies block `wave` and every eighth behind it: kCopies, or one less (the
+// waits count them).
+template <int TN, int NX>
 struct Ring8 {
-  static constexpr int kX = NX * 4096, kStage = kX + 16384;
-  static constexpr int kStages = NX == 4 ? 4 : NX == 3 ? 5 : 6;
-  static constexpr int kCopiesX = (NX + 1) / 2, kCopies = kCopiesX + 2;  // of a wavefront and step
-  static_assert(kStages * kStage + 6144 <= 160 * 1024, "LDS");
+  static constexpr int kW = 2 * TN, kBlocks = kW + 4 * NX, kStage = kBlocks * 1024, kCopies = (kBlocks + 7) / 8;
+  static constexpr int kStages = 148 * 1024 / kStage < 10 ? 148 * 1024 / kStage : 10;
+  static_assert(kStages >= 4 && kStages * kStage + 6144 <= 160 * 1024, "LDS");
 };
 
 template <int N>
@@ -51,10 +53,10 @@ __device__ __forceinline__ void values8(const v4i& a0, const v4i& a1, float s, c
   }
 }
 
-// The wavefront's 128 channels x 16 MT rows to Y.  Whole lines (see store_line_pair): fp16 pairs two batches of 32 channels, fp32 a batch's halves.
+// The wavefront's 16 TN channels x 16 MT rows to Y.  Whole lines (see store_line_pair): fp16 pairs two batches of 32 channels, fp32 a batch's halves.
 // p: 128 channel scales, 128 biases; rows: the wavefront's token scales.  CHECKED: some of it lies outside Y.
-template <bool F32, bool GELU, bool CHECKED, int NX, int MT>
-__device__ __forceinline__ void lines8(const Linear8Args& a, const v4i (&acc)[kTileTN][NX], const float* p, const float* rows, int n_wave, int64_t m_wave, int lane, int mine) {
+template <bool F32, bool GELU, bool CHECKED, int TN, int NX, int MT>
+__device__ __forceinline__ void lines8(const Linear8Args& a, const v4i (&acc)[TN][NX], const float* p, const float* rows, int n_wave, int64_t m_wave, int lane, int mine) {
   asm volatile("" : "+v"(lane));  // (computed here, per tile: nothing lane-dependent is carried across the K loop)
   const int c = lane & 15, q = lane >> 4, up = c >> 3;
   constexpr int OB = F32 ? 4 : 2;
@@ -75,7 +77,7 @@ __device__ __forceinline__ void lines8(const Linear8Args& a, const v4i (&acc)[kT
   for (int mt = 0; mt < MT; ++mt) s[mt] = rows[16 * mt + c];
   if constexpr (F32) {
 #pragma unroll
-    for (int g = 0; g < kTileTN / 2; ++g) {
+    for (int g = 0; g < TN / 2; ++g) {
       const int nb = (g >> 1) * kRowBlock + (g & 1) * 32 + q * 8 + up * 4;  // the 4 channels that this lane stores
       const bool n_ok = n_wave + nb < a.N;
       float c8[8], b8[8];
@@ -92,7 +94,7 @@ __device__ __forceinline__ void lines8(const Linear8Args& a, const v4i (&acc)[kT
     }
   } else {
 #pragma unroll
-    for (int gp = 0; gp < kTileTN / 4; ++gp) {
+    for (int gp = 0; gp < TN / 4; ++gp) {
       const bool n_ok = n_wave + gp * kRowBlock + up * 32 + q * 8 < a.N;
       float c8[2][8], b8[2][8];
       constants(2 * gp, c8[0], b8[0]);
@@ -116,13 +118,15 @@ __device__ __forceinline__ void lines8(const Linear8Args& a, const v4i (&acc)[kT
   }
 }
 
-// fp16 output where N % 8 == 4: rows begin at odd multiples of 8 bytes, four channels a store
-template <bool GELU, int NX>
-__device__ __forceinline__ void quads8(const Linear8Args& a, const v4i (&acc)[kTileTN][NX], const float* p, const float* rows, int n_wave, int64_t m_wave, int lane, int mine) {
+// fp16 output by batches of 32 channels, a lane's 8 channels of a row at a time: of wavefronts with one batch, or where N % 8 == 4 and rows begin at odd
+// multiples of 8 bytes (halves then)
+template <bool GELU, int TN, int NX>
+__device__ __forceinline__ void batches8(const Linear8Args& a, const v4i (&acc)[TN][NX], const float* p, const float* rows, int n_wave, int64_t m_wave, int lane, int mine) {
   asm volatile("" : "+v"(lane));
   const int c = lane & 15, q = lane >> 4;
+  const bool whole = (a.N & 7) == 0;
 #pragma unroll
-  for (int g = 0; g < kTileTN / 2; ++g) {
+  for (int g = 0; g < TN / 2; ++g) {
     const int nl = (g >> 1) * kRowBlock + (g & 1) * 32 + q * 8;
     float c8[8], b8[8];
 #pragma unroll
@@ -136,19 +140,25 @@ __device__ __forceinline__ void quads8(const Linear8Args& a, const v4i (&acc)[kT
       const int64_t m = m_wave + 16 * mt + c;
       f4 y[2];
       values8<false, GELU>(acc[2 * g][mt], acc[2 * g + 1][mt], rows[16 * mt + c], c8, b8, y);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (m < a.M && n_wave + nl + 4 * h < a.N)
-          *(h4*)((_Float16*)a.Y + m * a.N + n_wave + nl + 4 * h) = h4{(_Float16)y[h][0], (_Float16)y[h][1], (_Float16)y[h][2], (_Float16)y[h][3]};
+      const h8 h = {(_Float16)y[0][0], (_Float16)y[0][1], (_Float16)y[0][2], (_Float16)y[0][3], (_Float16)y[1][0], (_Float16)y[1][1], (_Float16)y[1][2], (_Float16)y[1][3]};
+      _Float16* out = (_Float16*)a.Y + m * a.N + n_wave + nl;
+      if (m >= a.M || n_wave + nl >= a.N) continue;
+      if (whole) {
+        *(h8*)out = h;
+      } else {
+        *(h4*)out = h4{h[0], h[1], h[2], h[3]};
+        if (n_wave + nl + 4 < a.N) *(h4*)(out + 4) = h4{h[4], h[5], h[6], h[7]};
+      }
     }
   }
 }
 
 // NX: slabs of 16 rows that a wavefront has at most
-template <int NX, bool F32, bool GELU>
-__global__ void __launch_bounds__(512, 1) linear8_tiles_kernel(const Linear8Args a, const EvenPlan plan) {
-  typedef Ring8<NX> R;
-  constexpr int kStores = (F32 ? 8 : 4) * (NX > 1 ? NX - 1 : 1);  // the fewest that a wavefront inside Y issues for a tile
+template <int TN, int NX, bool F32, bool GELU>
+__global__ void __launch_bounds__(512, 1) linear8_tiles_kernel(const Linear8Args a, const Tokens8Plan plan) {
+  typedef Ring8<TN, NX> R;
+  constexpr bool LINES = F32 || TN > 2;  // whole lines of fp16 take 64 channels
+  constexpr int kStores = (F32 ? TN : TN / 2) * (NX > 1 ? NX - 1 : 1);  // the fewest that a wavefront inside Y issues for a tile in lines
   __shared__ __attribute__((aligned(1024))) uint8_t ring[R::kStages * R::kStage];
   __shared__ __attribute__((aligned(1024))) float prm[2][2][256];     // by parity of the tile and half of its channels: 128 scales, 128 biases
   __shared__ __attribute__((aligned(1024))) float row_scales[2][256];  // by parity of the tile
@@ -159,7 +169,7 @@ __global__ void __launch_bounds__(512, 1) linear8_tiles_kernel(const Linear8Args
   const int place = (int)(blockIdx.x & 7) * plan.grid8 + (int)(blockIdx.x >> 3);
   const int my_items = plan.rounds + (place < plan.last_round ? 1 : 0);
   if (my_items == 0) return;  // the whole workgroup, in front of any barrier
-  auto tile_of = [&](int i) { return even_tile(plan, i * 8 * plan.grid8 + place); };
+  auto tile_of = [&](int i) { return tokens8_tile(plan, i * 8 * plan.grid8 + place); };
   const bool has_bias = (a.epilogue & GPUSQ_EPI_BIAS) != 0;
   if (!has_bias && wm == 0) {
 #pragma unroll
@@ -176,8 +186,8 @@ __global__ void __launch_bounds__(512, 1) linear8_tiles_kernel(const Linear8Args
     if (wm == 0) {
       const uint32_t dst = prm_lds + (uint32_t)parity * (uint32_t)sizeof(prm[0]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        int n = n0 + wn * 128 + i * 64 + l;
+      for (int i = 0; i < (TN + 3) / 4; ++i) {
+        int n = n0 + wn * (16 * TN) + i * 64 + l;
         n = n < a.N ? n : a.N - 1;  // (channels past the end are not stored)
         copy4_to_lds(a.w_scale, (uint32_t)n * 4u, dst + (uint32_t)i * 256u);
         if (has_bias) copy4_to_lds(a.bias, (uint32_t)n * 4u, dst + 512u + (uint32_t)i * 256u);
@@ -191,92 +201,82 @@ __global__ void __launch_bounds__(512, 1) linear8_tiles_kernel(const Linear8Args
       }
     }
   };
-  const uint32_t a_off = (uint32_t)(R::kX + wn * kTileTN * 1024 + (lane & 15) * 64 + (((lane >> 4) ^ ((lane & 15) >> 2)) * 16));
+  const uint32_t a_off = (uint32_t)(wn * TN * 1024 + (lane & 15) * 64 + (((lane >> 4) ^ ((lane & 15) >> 2)) * 16));
 
   // cursor of the copies: the next step to request, as (tile, step); at the end of the sequence it stays on the last step
-  const uint32_t wave_lds = (uint32_t)wave * 1024u;
+  // (A copy's block is the wavefront's for the whole launch; its source is a base in scalar registers for a tile and a lane's offset that moves by
+  // 64 a step, its place the stage's and the block's: four instructions a copy.)
   int pf_item = 0, pf_ks = 0;
-  const uint8_t *pf_x = (const uint8_t*)a.Xq, *pf_w = (const uint8_t*)a.W;
-  uint32_t pf_xoff[R::kCopiesX], pf_woff[2];
+  const uint8_t* pf_base[R::kCopies];
+  uint32_t pf_off[R::kCopies];
+  auto block_of = [&](int i) { return wave + 8 * i; };
+  const bool all_copies = block_of(R::kCopies - 1) < R::kW + 2 * tokens8_units(plan);  // (no block that no tile has)
   auto clip_tail = [&]() {  // chunks of weights behind the end of a row
     if (tail != 0 && pf_ks + 1 == ksteps) {
       int l = lane;
       asm volatile("" : "+v"(l));
-      const uint32_t at = (uint32_t)((l & 3) ^ (l >> 4)) * 16u;
-      pf_woff[0] -= at >= (uint32_t)tail ? at : 0u;
-      pf_woff[1] -= at >= (uint32_t)tail ? at : 0u;
+      const uint32_t at = (uint32_t)((l & 3) ^ (l >> 4)) * 16u, back = at >= (uint32_t)tail ? at : 0u;
+#pragma unroll
+      for (int i = 0; i < R::kCopies; ++i) pf_off[i] -= block_of(i) < R::kW ? back : 0u;
     }
   };
   auto seek = [&](int item) {
     pf_item = item;
     pf_ks = 0;
-    const EvenTile t = tile_of(item);
+    const Tokens8Tile t = tile_of(item);
     int l = lane;
     asm volatile("" : "+v"(l));
-    const int r = l >> 2, c = (l & 3) ^ (l >> 4);
+    const int r = l >> 2, c = (l & 3) ^ (l >> 4), n0 = t.n_blk * (32 * TN);
     int64_t last = (int64_t)a.M - 1 - t.m0;
     last = last < 16 * t.slabs - 1 ? last : 16 * t.slabs - 1;  // a lower tile draws no rows that it does not use
 #pragma unroll
-    for (int i = 0; i < R::kCopiesX; ++i) {
-      int block = wave + 8 * i;
-      if (block >= 4 * NX) block -= 4 * NX;  // (copied twice: every wavefront has as many copies)
-      const int64_t row = 16 * block + r;
-      pf_xoff[i] = (uint32_t)((row < last ? row : last) * a.pitch + c * 16);
+    for (int i = 0; i < R::kCopies; ++i) {
+      const int f = block_of(i);
+      pf_base[i] = f < R::kW ? (const uint8_t*)a.W + (int64_t)n0 * a.K : (const uint8_t*)a.Xq + t.m0 * a.pitch;
+      if (f < R::kW) {
+        int ch = 64 * (f >> 2) + packed_row_to_channel(f & 3, r);
+        ch = n0 + ch < a.N ? ch : a.N - 1 - n0;
+        pf_off[i] = (uint32_t)ch * (uint32_t)a.K + c * 16;
+      } else {
+        const int64_t row = 16 * (f - R::kW) + r;
+        pf_off[i] = (uint32_t)((row < last ? row : last) * a.pitch + c * 16);
+      }
     }
-    const int n0 = t.n_blk * kTileBN;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int f = wave + 8 * i;
-      int ch = 64 * (f >> 2) + packed_row_to_channel(f & 3, r);
-      ch = n0 + ch < a.N ? ch : a.N - 1 - n0;
-      pf_woff[i] = (uint32_t)ch * (uint32_t)a.K + c * 16;
-    }
-    pf_x = (const uint8_t*)a.Xq + t.m0 * a.pitch;
-    pf_w = (const uint8_t*)a.W + (int64_t)n0 * a.K;
     clip_tail();
   };
   auto advance = [&]() {
     if (pf_ks + 1 < ksteps) {
       ++pf_ks;
-      pf_x += 64;
-      pf_w += 64;
+#pragma unroll
+      for (int i = 0; i < R::kCopies; ++i) pf_off[i] += 64;
       clip_tail();
     } else if (pf_item + 1 < my_items) {
       seek(pf_item + 1);
     }
   };
-  auto request_copy = [&](auto i, uint32_t stage_lds) {
-    constexpr int I = decltype(i)::value;
-    const uint32_t base = stage_lds + wave_lds;
-    if constexpr (I == 0) {
-      copy16_to_lds(pf_x, pf_xoff[0], 4 * NX < 8 && wave >= 4 * NX ? base - 4096u * NX : base);
-    } else if constexpr (I < R::kCopiesX) {
-      copy16_to_lds(pf_x, pf_xoff[I < R::kCopiesX ? I : 0], wave + 8 * I >= 4 * NX ? base + 8192u * I - 4096u * NX : base + 8192u * I);
-    } else if constexpr (I < R::kCopies) {
-      copy16_to_lds_at<R::kX + (I - R::kCopiesX) * 8192>(pf_w, pf_woff[I - R::kCopiesX < 2 ? I - R::kCopiesX : 0], base);
-    }
+  auto request_copy = [&](int i, uint32_t stage_lds) {
+    if (i == R::kCopies - 1 && !all_copies) return;
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(stage_lds), "s"((uint32_t)block_of(i) * 1024u), "v"(pf_off[i]), "s"(pf_base[i])
+                 : "memory", "m0", "scc");
   };
-  typedef std::integral_constant<int, 0> C0;
-  typedef std::integral_constant<int, 1> C1;
-  typedef std::integral_constant<int, 2> C2;
-  typedef std::integral_constant<int, 3> C3;
 
-  v4i acc[kTileTN][NX], b[NX], av[kTileTN];
+  v4i acc[TN][NX], b[NX], av[TN];
   {
-    const EvenTile t = tile_of(0);
-    request_constants(t.n_blk * kTileBN, t.m0, 0);
+    const Tokens8Tile t = tile_of(0);
+    request_constants(t.n_blk * (32 * TN), t.m0, 0);
   }
   seek(0);
 #pragma nounroll
   for (int g = 0; g < R::kStages; ++g) {
     const uint32_t stage = ring_lds + (uint32_t)g * R::kStage;
-    request_copy(C0{}, stage);
-    request_copy(C1{}, stage);
-    request_copy(C2{}, stage);
-    request_copy(C3{}, stage);
+#pragma unroll
+    for (int i = 0; i < R::kCopies; ++i) request_copy(i, stage);
     advance();
   }
-  wait_copies<(R::kStages - 1) * R::kCopies>();  // the constants and step 0
+  if (all_copies)  // the constants and step 0
+    wait_copies<(R::kStages - 1) * R::kCopies>();
+  else
+    wait_copies<(R::kStages - 1) * (R::kCopies - 1)>();
   __builtin_amdgcn_sched_barrier(0);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -285,69 +285,87 @@ __global__ void __launch_bounds__(512, 1) linear8_tiles_kernel(const Linear8Args
   bool stores_behind = false;
 #pragma nounroll
   for (int item = 0; item < my_items; ++item) {
-    const EvenTile t = tile_of(item);
+    const Tokens8Tile t = tile_of(item);
     // this wavefront's slabs: a quarter of the tile's, the first t.slabs % 4 (0 or 2) wavefronts along m one more
     const int quarter = t.slabs >> 2, extra = t.slabs & 3;
     const int mine = quarter + (wm < extra ? 1 : 0), row0 = 16 * (wm * quarter + (wm < extra ? wm : extra));
     int l = lane;
     asm volatile("" : "+v"(l));
-    const uint32_t b_off = (uint32_t)(row0 * 64 + (l & 15) * 64 + (((l >> 4) ^ ((l & 15) >> 2)) * 16));
+    const uint32_t b_off = (uint32_t)(R::kW * 1024 + row0 * 64 + (l & 15) * 64 + (((l >> 4) ^ ((l & 15) >> 2)) * 16));
     const bool more = item + 1 < my_items;
-    const EvenTile after = tile_of(more ? item + 1 : item);
+    const Tokens8Tile after = tile_of(more ? item + 1 : item);
 #pragma unroll
-    for (int i = 0; i < kTileTN; ++i)
+    for (int i = 0; i < TN; ++i)
 #pragma unroll
       for (int j = 0; j < NX; ++j) acc[i][j] = v4i{0, 0, 0, 0};
     auto k_loop = [&](auto tma) {
-      constexpr int TMA = decltype(tma)::value, H = 4 * TMA, kBarrierSlot = TMA > 2 ? H - 2 : H;
-      constexpr int kBehind = (R::kStages - 2) * R::kCopies;
+      constexpr int TMA = decltype(tma)::value, F = TN / 2, H = F * TMA, kBarrierSlot = TMA > 2 && F > 1 ? H - 2 : H;
+      constexpr int kBehind = (R::kStages - 2) * R::kCopies, kBehindLess = (R::kStages - 2) * (R::kCopies - 1);
 #pragma unroll
-      for (int f = 0; f < 4; ++f) av[f] = *(const v4i*)(ring + slot_off + a_off + f * 1024);
+      for (int f = 0; f < F; ++f) av[f] = *(const v4i*)(ring + slot_off + a_off + f * 1024);
 #pragma unroll
       for (int mt = 0; mt + 1 < TMA; ++mt) b[mt] = *(const v4i*)(ring + slot_off + b_off + mt * 1024);
-#pragma nounroll
-      for (int ks = 0; ks < ksteps; ++ks) {
+      // A step.  EDGE: of a tile's first, beside the output of the one before, or its last, from which on the copies are the next tile's.  Between them a
+      // step has nothing to decide: a wavefront issues an instruction every five clocks or so, and sixty scalar ones a step took a quarter of its time.
+      auto step = [&](auto edge, int ks) {
+        constexpr bool EDGE = decltype(edge)::value;
         const int next_off = slot_off + R::kStage == R::kStages * R::kStage ? 0 : slot_off + R::kStage;
         const uint8_t *stage = ring + slot_off, *next = ring + next_off;
         const uint32_t stage_lds = ring_lds + (uint32_t)slot_off;
 #pragma unroll
         for (int slot = 0; slot < 2 * H; ++slot) {
-          const int mt = (slot % H) >> 2, f = (slot & 3) + (slot < H ? 0 : 4);
+          const int mt = slot % H / F, f = slot % F + (slot < H ? 0 : F);
           if (slot == kBarrierSlot) {
             __builtin_amdgcn_sched_barrier(0);
             // (with fewer steps to a tile than stages the constants asked for in the last one's would not be waited for)
-            if (ksteps < R::kStages)
+            if (EDGE && ksteps < R::kStages)
               wait_copies<0>();
-            else if (stores_behind && ks < R::kStages - 1)
-              wait_copies<kBehind + kStores>();
+            else if (EDGE && stores_behind && ks < R::kStages - 1)
+              all_copies ? wait_copies<kBehind + kStores>() : wait_copies<kBehindLess + kStores>();
             else
-              wait_copies<kBehind>();
+              all_copies ? wait_copies<kBehind>() : wait_copies<kBehindLess>();
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (ks + 1 == ksteps && more) request_constants(after.n_blk * kTileBN, after.m0, (item + 1) & 1);
+            if (EDGE && ks + 1 == ksteps && more) request_constants(after.n_blk * (32 * TN), after.m0, (item + 1) & 1);
           }
           if (slot < H) {
-            auto at = [&](int i) { return slot == (H >= 12 ? i : i * (H / 4) / 4); };
+            // (in front of the barrier, all of them)
+            auto at = [&](int i) { return slot == (H >= 3 * F ? i : i * (H / F) / 4); };
             if (at(0)) b[TMA - 1] = *(const v4i*)(stage + b_off + (TMA - 1) * 1024);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (at(1 + j)) av[4 + j] = *(const v4i*)(stage + a_off + (4 + j) * 1024);
+            for (int j = 0; j < F; ++j)
+              if (at(1 + j)) av[F + j] = *(const v4i*)(stage + a_off + (F + j) * 1024);
           } else {
             const int s = slot - H;
-            if (s < 4) av[s] = *(const v4i*)(next + a_off + s * 1024);
-            // slab mt is free once its four instructions of this half are issued
-            if (s >= 4 && (s & 3) == 0 && (s >> 2) - 1 < TMA - 1) b[(s >> 2) - 1] = *(const v4i*)(next + b_off + ((s >> 2) - 1) * 1024);
-            if (s == 0) request_copy(C0{}, stage_lds);
-            if (s == H / 4) request_copy(C1{}, stage_lds);
-            if (s == 2 * H / 4) request_copy(C2{}, stage_lds);
-            if (s == 3 * H / 4) request_copy(C3{}, stage_lds);
+            if (s < F) av[s] = *(const v4i*)(next + a_off + s * 1024);
+            // slab mt is free once its instructions of this half are issued
+            if (s >= F && s % F == 0 && s / F - 1 < TMA - 1) b[s / F - 1] = *(const v4i*)(next + b_off + (s / F - 1) * 1024);
+#pragma unroll
+            for (int i = 0; i < R::kCopies; ++i)
+              if (s == i * H / R::kCopies) request_copy(i, stage_lds);
           }
           __builtin_amdgcn_sched_barrier(0);
           acc[f][mt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[f], b[mt], acc[f][mt], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        advance();
+        if constexpr (EDGE) {
+          advance();
+        } else {
+#pragma unroll
+          for (int i = 0; i < R::kCopies; ++i) pf_off[i] += 64;
+        }
         slot_off = next_off;
+      };
+      const int plain = ksteps - R::kStages - 2;  // up to here the cursor stays in front of the tile's last step
+#pragma nounroll
+      for (int ks = 0; ks < ksteps; ++ks) {
+        if (ks == (stores_behind ? R::kStages - 1 : 0) && ks < plain) {
+          pf_ks += plain - ks;
+#pragma nounroll
+          do step(std::false_type(), ks);
+          while (++ks < plain);
+        }
+        step(std::true_type(), ks);
       }
     };
     if constexpr (NX > 1) {
@@ -358,42 +376,45 @@ __global__ void __launch_bounds__(512, 1) linear8_tiles_kernel(const Linear8Args
     } else {
       k_loop(std::integral_constant<int, 1>{});
     }
-    const int n_wave = t.n_blk * kTileBN + wn * (kTileTN * 16);
+    const int n_wave = t.n_blk * (32 * TN) + wn * (TN * 16);
     const int64_t m_wave = t.m0 + row0, rows = (int64_t)a.M - m_wave;
-    const bool lines = F32 || (a.N & 7) == 0, inside = lines && rows >= mine * 16 && a.N - n_wave >= kTileTN * 16;
+    const bool lines = F32 || (LINES && (a.N & 7) == 0), inside = lines && rows >= mine * 16 && a.N - n_wave >= TN * 16;
     const float *p = prm[item & 1][wn], *rs = row_scales[item & 1] + row0;
-    if (inside && mine == NX)
-      lines8<F32, GELU, false, NX, NX>(a, acc, p, rs, n_wave, m_wave, lane, NX);
-    else if (inside && NX > 1)
-      lines8<F32, GELU, false, NX, (NX > 1 ? NX - 1 : 1)>(a, acc, p, rs, n_wave, m_wave, lane, NX - 1);
-    else if (lines)
-      lines8<F32, GELU, true, NX, NX>(a, acc, p, rs, n_wave, m_wave, lane, mine);
-    else if constexpr (!F32)
-      quads8<GELU, NX>(a, acc, p, rs, n_wave, m_wave, lane, mine);
+    if constexpr (LINES) {
+      if (inside && mine == NX)
+        lines8<F32, GELU, false, TN, NX, NX>(a, acc, p, rs, n_wave, m_wave, lane, NX);
+      else if (inside && NX > 1)
+        lines8<F32, GELU, false, TN, NX, (NX > 1 ? NX - 1 : 1)>(a, acc, p, rs, n_wave, m_wave, lane, NX - 1);
+      else if (lines)
+        lines8<F32, GELU, true, TN, NX, NX>(a, acc, p, rs, n_wave, m_wave, lane, mine);
+    }
+    if constexpr (!F32) {
+      if (!lines) batches8<GELU, TN, NX>(a, acc, p, rs, n_wave, m_wave, lane, mine);
+    }
     stores_behind = inside && mine > 0 && ksteps >= R::kStages;
   }
   wait_copies<0>();  // those asked for past the end of the sequence land before the LDS is given up
 }
 
-template <int NX>
-void launch_nx(const Linear8Args& a, const EvenPlan& plan, unsigned grid, hipStream_t s) {
+template <int TN, int NX>
+void launch_nx(const Linear8Args& a, const Tokens8Plan& plan, hipStream_t s) {
   const bool gelu = (a.epilogue & GPUSQ_EPI_GELU) != 0;
+  const unsigned grid = (unsigned)plan.grid8 * 8;
   if (a.out_f32)
-    gelu ? linear8_tiles_kernel<NX, true, true><<<grid, 512, 0, s>>>(a, plan) : linear8_tiles_kernel<NX, true, false><<<grid, 512, 0, s>>>(a, plan);
+    gelu ? linear8_tiles_kernel<TN, NX, true, true><<<grid, 512, 0, s>>>(a, plan) : linear8_tiles_kernel<TN, NX, true, false><<<grid, 512, 0, s>>>(a, plan);
   else
-    gelu ? linear8_tiles_kernel<NX, false, true><<<grid, 512, 0, s>>>(a, plan) : linear8_tiles_kernel<NX, false, false><<<grid, 512, 0, s>>>(a, plan);
+    gelu ? linear8_tiles_kernel<TN, NX, false, true><<<grid, 512, 0, s>>>(a, plan) : linear8_tiles_kernel<TN, NX, false, false><<<grid, 512, 0, s>>>(a, plan);
 }
 
 }  // namespace
 
-void launch_linear8_tiles(const Linear8Args& a, const EvenPlan& plan, hipStream_t s) {
-  const unsigned grid = (unsigned)plan.grid8 * 8;
-  switch ((even_units(plan) + 1) / 2) {
-    case 1: return launch_nx<1>(a, plan, grid, s);
-    case 2: return launch_nx<2>(a, plan, grid, s);
-    case 3: return launch_nx<3>(a, plan, grid, s);
-    default: return launch_nx<4>(a, plan, grid, s);
+template <int TN>
+void launch_linear8_tiles_of(const Linear8Args& a, const Tokens8Plan& plan, hipStream_t s) {
+  switch ((tokens8_units(plan) + 1) / 2) {
+    case 1: return launch_nx<TN, 1>(a, plan, s);
+    case 2: return launch_nx<TN, 2>(a, plan, s);
+    case 3: return launch_nx<TN, 3>(a, plan, s);
+    default: return launch_nx<TN, 4>(a, plan, s);
   }
 }
-
 }  // namespace gpusq
