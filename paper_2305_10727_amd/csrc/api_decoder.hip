@@ -13,9 +13,8 @@ constexpr int64_t kMaxElems = (int64_t)1 << 40;
 
 // sums of products of codes, -128 the least of a weight's, stay in 32 bits
 constexpr int64_t kMostTokens8K = INT32_MAX / (127 * 128) / 64 * 64;
-// a row's weights as whole numbers: together in 62 bits, the least (2^-40) 16 or more
+// a row's weights, whole numbers up to 2^44, are together below 2^63
 constexpr int64_t kMostVocabulary = (int64_t)1 << 18;
-double sample_one(int64_t) { return 0x1p44; }
 
 constexpr int64_t kMostPages = INT32_MAX / kPageTokens - 1;  // of a sequence: tokens are counted in 31 bits, a page beyond the last too
 
@@ -270,7 +269,7 @@ gpusq_status gpusq_sample_tokens(const void* logits, gpusq_dtype dt, int64_t row
   if (((uintptr_t)logits & (dt == GPUSQ_F32 ? 3u : 1u)) != 0 || !aligned4(random) || !aligned4(temperature) || !aligned4(top_k) || !aligned4(top_p) || !aligned4(min_p) ||
       !aligned4(tokens) || !aligned4(probs))
     return GPUSQ_ERR_ALIGN;
-  const SampleArgs a{logits, row_stride, random, temperature, top_p, min_p, top_k, tokens, probs, (int)vocabulary, sample_one(vocabulary)};
+  const SampleArgs a{logits, row_stride, random, temperature, top_p, min_p, top_k, tokens, probs, (int)vocabulary};
   return launch_sample_tokens(a, dt == GPUSQ_F32, rows, (hipStream_t)stream);
 }
 

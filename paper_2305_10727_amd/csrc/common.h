@@ -546,7 +546,6 @@ struct SampleArgs {
   int32_t* tokens;
   float* probs;
   int V;
-  double one;  // what a weight of 1 is as a whole number
 };
 gpusq_status launch_sample_tokens(const SampleArgs& a, bool f32, int64_t rows, hipStream_t s);
 struct Linear8Args {
