@@ -465,15 +465,19 @@ gpusq_status gpusq_linear_int8_tokens(const void* X, gpusq_dtype dt, const int8_
 
 /* Tokens drawn from logits [rows][vocabulary] (dt GPUSQ_F16 or GPUSQ_F32, row_stride values from row to row, aligned to a value; at most 2^18 tokens,
  * GPUSQ_ERR_SHAPE) with given random numbers, one in [0, 1) a row.  temperature, top_k, top_p, min_p: [rows] each, or NULL (1, and no cut).
- *   A token's weight is exp((x - max) / temperature) in 64 bits, 0 below 2^-40; 1 where x is the greatest, also where that is infinite.  Tokens are
+ *   A token's weight is exp((x - max) / temperature), to 2^-30 of it, 0 below 2^-40; 1 where x is the greatest, also where that is infinite.  Tokens are
  *   ordered by their logits, ties by their index, the lower first; -infinity and NaN are never drawn.  Kept are the first top_k (0 or less: all);
  *   of those as many as it takes for top_p of their weight, one at least (1 and more: all); of those the ones of a weight of min_p or more (of the
  *   first one's, which is 1; at most 1 is asked).
  *   Drawn is the first token, in the vocabulary's order, at which the sum of the kept weights up to it passes random times their sum.  A temperature
- *   that is not above 0: the first in the order.
- *   tokens [rows]: its index, -1 where all logits are -infinity or NaN; probs [rows]: its share of the kept weight (there 0). */
+ *   that is not above 0: the first in the order; one below 2^-100 counts as that.
+ *   tokens [rows]: its index, -1 where all logits are -infinity or NaN; probs [rows]: its share of the kept weight (there 0).
+ *   workspace: gpusq_sample_tokens_workspace_bytes (0 for sizes that are refused), may be NULL where that is 0 (few long rows: several workgroups have a row); what it held
+ *   does not matter. */
+size_t gpusq_sample_tokens_workspace_bytes(int64_t rows, int64_t vocabulary);
 gpusq_status gpusq_sample_tokens(const void* logits, gpusq_dtype dt, int64_t row_stride, const float* random, const float* temperature, const int32_t* top_k,
-                                 const float* top_p, const float* min_p, int32_t* tokens, float* probs, int64_t rows, int64_t vocabulary, void* stream);
+                                 const float* top_p, const float* min_p, int32_t* tokens, float* probs, void* workspace, int64_t rows, int64_t vocabulary,
+                                 void* stream);
 
 #ifdef __cplusplus
 }

@@ -4,6 +4,7 @@
 #include "attend_plan.h"
 #include "drafts_plan.h"
 #include "linear8_plan.h"
+#include "sample_plan.h"
 #include "kv4.h"
 
 using namespace gpusq;
@@ -77,6 +78,8 @@ gpusq_status check_drafts(int64_t tokens, int64_t batch, int64_t max_q, const in
   if (!is_size(tokens) || !is_size(batch) || !is_size(max_q) || max_q > tokens || (!cu_q && tokens != batch * max_q) || !launchable(batch, 256)) return GPUSQ_ERR_SHAPE;
   return max_q <= kMostDrafts ? GPUSQ_OK : GPUSQ_ERR_UNSUPPORTED;
 }
+
+bool are_samples(int64_t rows, int64_t vocabulary) { return is_size(rows) && is_size(vocabulary) && vocabulary <= kMostVocabulary && launchable(rows, kSampleThreads); }
 
 // codes of M tokens of K values in the workspace, rows of whole steps of 64; their scales behind them
 bool are_tokens8(int64_t M, int64_t K) { return is_size(M) && is_size(K) && K <= kMostTokens8K && ceil_div(M, 64) <= 65535 && M * K <= kMaxElems; }
@@ -259,18 +262,24 @@ gpusq_status gpusq_linear_int8_tokens(const void* X, gpusq_dtype dt, const int8_
   return launch_linear_int8_tokens(a, (hipStream_t)stream);
 }
 
+size_t gpusq_sample_tokens_workspace_bytes(int64_t rows, int64_t vocabulary) {
+  if (!are_samples(rows, vocabulary)) return 0;
+  const int parts = sample_parts(rows, vocabulary);
+  return parts > 1 ? (size_t)(rows * sample_space(parts).bytes) : 0;
+}
+
 gpusq_status gpusq_sample_tokens(const void* logits, gpusq_dtype dt, int64_t row_stride, const float* random, const float* temperature, const int32_t* top_k,
-                                 const float* top_p, const float* min_p, int32_t* tokens, float* probs, int64_t rows, int64_t vocabulary, void* stream) {
+                                 const float* top_p, const float* min_p, int32_t* tokens, float* probs, void* workspace, int64_t rows, int64_t vocabulary,
+                                 void* stream) {
   if (!logits || !random || !tokens || !probs) return GPUSQ_ERR_NULL;
-  if (!is_size(rows) || !is_size(vocabulary) || vocabulary > kMostVocabulary || row_stride < vocabulary || row_stride > INT32_MAX || rows * row_stride > kMaxElems ||
-      !launchable(rows, 1024))
-    return GPUSQ_ERR_SHAPE;
+  if (!are_samples(rows, vocabulary) || row_stride < vocabulary || row_stride > INT32_MAX || rows * row_stride > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (sample_parts(rows, vocabulary) > 1 && !workspace) return GPUSQ_ERR_NULL;
   if (dt != GPUSQ_F16 && dt != GPUSQ_F32) return GPUSQ_ERR_UNSUPPORTED;
   if (((uintptr_t)logits & (dt == GPUSQ_F32 ? 3u : 1u)) != 0 || !aligned4(random) || !aligned4(temperature) || !aligned4(top_k) || !aligned4(top_p) || !aligned4(min_p) ||
-      !aligned4(tokens) || !aligned4(probs))
+      !aligned4(tokens) || !aligned4(probs) || !aligned16(workspace))
     return GPUSQ_ERR_ALIGN;
   const SampleArgs a{logits, row_stride, random, temperature, top_p, min_p, top_k, tokens, probs, (int)vocabulary};
-  return launch_sample_tokens(a, dt == GPUSQ_F32, rows, (hipStream_t)stream);
+  return launch_sample_tokens(a, dt == GPUSQ_F32, rows, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

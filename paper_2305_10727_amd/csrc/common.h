@@ -547,7 +547,7 @@ struct SampleArgs {
   float* probs;
   int V;
 };
-gpusq_status launch_sample_tokens(const SampleArgs& a, bool f32, int64_t rows, hipStream_t s);
+gpusq_status launch_sample_tokens(const SampleArgs& a, bool f32, int64_t rows, void* workspace, hipStream_t s);
 struct Linear8Args {
   const void* X;
   int x_f32;

@@ -4,16 +4,24 @@
 //   first whose weights reach p of the first k's, and in front of the first whose weight is below min_p;  drawn is the first token, in the
 //   vocabulary's order, up to which the kept weights pass u of their sum.
 //
-// Where two tokens' shares meet is closer to a neighbour's than 32 bits tell apart, so weights are formed in 64 bits and summed as whole numbers, of
-// which no order changes the sum.  A token's place in the order is one number, its logit's bits made monotone and its index counted down: a cut is the
-// least such number that is kept.
+// Where two tokens' shares meet is closer to a neighbour's than 32 bits tell apart, so weights are formed to 2^-31 of themselves and summed as whole
+// numbers of 2^-44, of which no order changes the sum.  A token's place in the order is one number, its logit's bits made monotone and its index
+// counted down: a cut is the least such number that is kept.
+//
+// A row is read three times: for its greatest logit; for a histogram of the logits' distances from it, in 2048 bins of 28 / 2048 of the temperature, from
+// which the bin of the k-th token and the bins between which the p-th share ends are known; for the sums, and the tokens of those bins, which are sorted
+// and decide.  A wavefront sums a stretch of the vocabulary; the token lies in the stretch that passes the random share, which is looked at once more.
+// What bounds it is the instructions of the weights, some thirty a token and pass, and of the histogram's atomics in LDS.  So few rows are cut into parts,
+// a workgroup each, in a launch for each reading and one that decides.
 #include "common.h"
+#include "sample_plan.h"
 
 namespace gpusq {
 
 namespace {
 
-constexpr int kThreads = 1024, kBins = 2048;
+constexpr int kThreads = kSampleThreads, kWaves = kSampleWaves, kBins = kSampleBins, kListed = kSampleListed;
+constexpr float kBinsOfUnit = kBins / 28.0f;  // (2^-40 is 27.73 below the greatest)
 typedef unsigned long long u64;
 
 // The logits' order: greater numbers first; -0 is 0, what is no number is -infinity
@@ -24,72 +32,139 @@ __device__ __forceinline__ unsigned key_of(float x) {
 }
 __device__ __forceinline__ float value_of(unsigned key) { return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key); }
 __device__ __forceinline__ u64 place_of(float x, int i) { return (u64)key_of(x) << 32 | (unsigned)~i; }
+__device__ __forceinline__ int index_of(u64 place) { return (int)~(unsigned)place; }
+__device__ __forceinline__ float logit_of(u64 place) { return value_of((unsigned)(place >> 32)); }
 
-// Weights as whole numbers of 2^-44.  exp(y) is 2^(j / 64) 2^e (1 + r + r^2 / 2 + r^3 / 6 + r^4 / 24) with |r| at most ln 2 / 128, off by 4e-14 of
-// itself: a dozen operations in 64 bits, a third of the library's exp.
-struct Weights {
-  float top;            // the greatest logit
-  double steps;         // 64 / (T ln 2)
-  const double* table;  // 2^(j / 64)
-  __device__ __forceinline__ double exact(float x) const {
-    // (x equal to an infinite greatest one: 1; of -infinity and of what is no number 2^-42)
-    const double d = x == top ? 0.0 : (double)x - (double)top, t = fmax(d * steps, -2700.0);
-    const double shifted = t + 0x1.8p52, whole = shifted - 0x1.8p52, r = (t - whole) * 0x1.62e42fefa39efp-7;
-    const int k = (int)(unsigned)__double_as_longlong(shifted);
-    const double c = table[k & 63], p = r * __builtin_fma(r, __builtin_fma(r, __builtin_fma(r, 1.0 / 24, 1.0 / 6), 0.5), 1.0);
-    return __longlong_as_double(__double_as_longlong(__builtin_fma(c, p, c)) + ((long long)(k >> 6) << 52));
-  }
-  static __device__ __forceinline__ u64 whole(double w) {  // 0 below 2^-40
-    return w >= 0x1p-40 ? (u64)(__double_as_longlong(w + 256.0) - __double_as_longlong(256.0)) : 0;
-  }
-  __device__ __forceinline__ u64 operator()(float x) const { return whole(exact(x)); }
-};
+// A step of a scan over the wavefront's lanes: the value of the lane that CTRL names, 0 where there is none or ROWS leaves the lane out
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 from_lane(u64 v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)(unsigned)v, CTRL, ROWS, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xF, false);
+  return (u64)(unsigned)hi << 32 | (unsigned)lo;
+}
+// Of the lanes up to this one; op of 0 changes nothing.  (row_shr 1, 2, 4, 8, then the rows' last lanes: a fifth of the time of ds_bpermute's trips)
+template <class Op>
+__device__ __forceinline__ u64 scan(u64 v, Op op) {
+  v = op(v, from_lane<0x111, 0xF>(v));
+  v = op(v, from_lane<0x112, 0xF>(v));
+  v = op(v, from_lane<0x114, 0xF>(v));
+  v = op(v, from_lane<0x118, 0xF>(v));
+  v = op(v, from_lane<0x142, 0xA>(v));
+  return op(v, from_lane<0x143, 0xC>(v));
+}
+__device__ __forceinline__ u64 last_lane(u64 v) {
+  return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, 63);
+}
+__device__ __forceinline__ u64 sum_of(u64 a, u64 b) { return a + b; }
+__device__ __forceinline__ u64 max_of(u64 a, u64 b) { return a > b ? a : b; }
 
 struct Block {
-  u64 part[kThreads / 64];
+  u64 part[kWaves];
   template <class Op>
   __device__ __forceinline__ u64 all(u64 v, Op op) {  // of all threads, to all threads
+    v = last_lane(scan(v, op));
     __syncthreads();
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = op(v, (u64)__shfl_xor(v, d));
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
     v = part[0];
 #pragma unroll
-    for (int i = 1; i < kThreads / 64; ++i) v = op(v, part[i]);
+    for (int i = 1; i < kWaves; ++i) v = op(v, part[i]);
     return v;
   }
-  // sum of the threads in front of this one
-  __device__ __forceinline__ u64 before(u64 v) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u64 upto = v;
+  // sum of the threads in front of this one, and of all
+  __device__ __forceinline__ u64 before(u64 v, u64* total = nullptr) {
+    const int wave = threadIdx.x >> 6;
+    const u64 upto = scan(v, sum_of);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) part[wave] = upto;
+    __syncthreads();
+    u64 sum = upto - v, whole = 0;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const u64 o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
+    for (int i = 0; i < kWaves; ++i) {
+      const u64 p = part[i];
+      sum += i < wave ? p : 0;
+      whole += p;
     }
-    __syncthreads();
-    if (lane == 63) part[wave] = upto;
-    __syncthreads();
-    u64 sum = upto - v;
-    for (int i = 0; i < wave; ++i) sum += part[i];
+    if (total != nullptr) *total = whole;
     return sum;
   }
+  // how many of the threads' two answers are true
+  __device__ __forceinline__ int count(bool a, bool b) {
+    const int n = __popcll(__builtin_amdgcn_ballot_w64(a)) + __popcll(__builtin_amdgcn_ballot_w64(b));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) sum += (int)part[i];
+    return sum;
+  }
+  // the first thread for which it is so, or where none is the last for which `otherwise` is; -1: none
+  __device__ __forceinline__ int first(bool is, bool otherwise) {
+    const u64 yes = __builtin_amdgcn_ballot_w64(is), other = __builtin_amdgcn_ballot_w64(otherwise);
+    const unsigned wave = threadIdx.x >> 6, lowest = yes != 0 ? 64 * wave + __builtin_ctzll(yes) : 0xFFFFu, highest = other != 0 ? 64 * wave + 64 - __builtin_clzll(other) : 0;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[wave] = lowest << 16 | highest;
+    __syncthreads();
+    unsigned lo = 0xFFFFu, hi = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const unsigned p = (unsigned)part[i];
+      lo = lo < p >> 16 ? lo : p >> 16;
+      hi = hi > (p & 0xFFFFu) ? hi : p & 0xFFFFu;
+    }
+    return lo != 0xFFFFu ? (int)lo : (int)hi - 1;
+  }
 };
-__device__ __forceinline__ u64 sum_of(u64 a, u64 b) { return a + b; }
-__device__ __forceinline__ u64 max_of(u64 a, u64 b) { return a > b ? a : b; }
 
-// A row of logits by vectors of 16 bytes, wherever it begins: a wavefront has a stretch of the vocabulary, its lanes a vector each at a time.  each(value,
-// index) is called of a lane's values one after the other, unrolled.
+struct Shared {
+  Block block;
+  double table[64];  // 2^(j / 64)
+  u64 masses[kBins];
+  unsigned counts[kBins];
+  u64 list[kListed];
+  u64 sums[kSampleParts * kWaves], found[2];
+  unsigned listed, of_k_bin;
+};
+
+// exp(y) is 2^(k / 64), from a table, times 2^(f / 64), |f| at most 1/2: k and f of 64 (x - max) / (T ln 2) in 64 bits, 2^(f / 64) - 1, at most
+// 0.0055, by a polynomial in 32 bits: off by 2^-31 of the weight.
+struct Weights {
+  float top, limit, scale;  // the greatest logit; the distance of 2^-40 from it; bins of a distance
+  double steps;             // 64 / (T ln 2)
+  const double* table;
+  __device__ __forceinline__ Weights(float top_, float temperature, const double* table_)
+      : top(top_), limit(fminf(27.725887f * temperature, 3.4028235e38f)), scale(kBinsOfUnit / temperature), steps(92.332482616893657 / (double)temperature), table(table_) {}
+  // (not so for what is no number, or -infinity)
+  __device__ __forceinline__ bool has(float x) const { return top - x <= limit; }
+  // of a logit that has one: whole numbers of 2^-44
+  __device__ __forceinline__ u64 of(float x) const {
+    const double t = ((double)x - (double)top) * steps, shifted = t + 0x1.8p52;
+    const float f = (float)(t - (shifted - 0x1.8p52));
+    const float q = f * __builtin_fmaf(f, __builtin_fmaf(f, 0x1.c6b08ep-23f, 0x1.ebfbep-15f), 0x1.62e430p-7f);
+    const int k = (int)(unsigned)__double_as_longlong(shifted);
+    const double c = table[k & 63], w = __builtin_fma(c, (double)q, c);
+    const double scaled = __hiloint2double(__double2hiint(w) + (int)((unsigned)(k & ~63) << 14), __double2loint(w));  // times 2^(k / 64 whole)
+    const double sum = scaled + 256.0;  // the last place is 2^-44
+    return (u64)(unsigned)(__double2hiint(sum) - 0x40700000) << 32 | (unsigned)__double2loint(sum);
+  }
+  __device__ __forceinline__ u64 operator()(float x) const { return has(x) ? of(x) : 0; }
+  // ... a logit's bin, in the logits' order
+  __device__ __forceinline__ float distance(float x) const { return (top - x) * scale; }
+};
+
+// A row of logits by vectors of 16 bytes, wherever it begins; of a part of it a wavefront has a stretch, its lanes a vector each at a time.
+// each(value, index) is called of a lane's values one after the other, unrolled; indices in front of the row and behind it have -infinity.
 template <typename T>
 struct Row {
-  static constexpr int VEC = 16 / (int)sizeof(T), WAVES = kThreads / 64, AHEAD = 4;
+  static constexpr int VEC = 16 / (int)sizeof(T), AHEAD = 4;
   typedef T vec __attribute__((ext_vector_type(VEC)));
   const T* x;
-  int V, off, per_wave;  // values in front of the row in its first vector; vectors of a wavefront
-  __device__ __forceinline__ Row(const T* row, int V_) : x(row), V(V_), off((int)(((uintptr_t)row & 15) / sizeof(T))) {
-    const int vecs = (V + off + VEC - 1) / VEC;
-    per_wave = ((vecs + WAVES - 1) / WAVES + 63) & ~63;
+  int V, off, vecs, per_wave;  // values in front of the row in its first vector; vectors of it, of a wavefront
+  int begin;                   // the wavefront's first vector
+  __device__ __forceinline__ Row(const SampleArgs& a, int row, int part, int parts)
+      : x((const T*)a.logits + (int64_t)row * a.row_stride), V(a.V), off((int)(((uintptr_t)x & 15) / sizeof(T))), vecs((V + off + VEC - 1) / VEC) {
+    per_wave = ((vecs + parts * kWaves - 1) / (parts * kWaves) + 63) & ~63;
+    begin = (part * kWaves + (threadIdx.x >> 6)) * per_wave;
   }
   __device__ __forceinline__ vec load(int v) const {
     const int i = v * VEC - off;
@@ -101,14 +176,13 @@ struct Row {
   }
   template <class Each>
   __device__ __forceinline__ void walk(Each each) const {
-    const int begin = (threadIdx.x >> 6) * per_wave, end = begin + per_wave, last = (V + off + VEC - 1) / VEC;
-    for (int v0 = begin + (threadIdx.x & 63); v0 < end && v0 < last; v0 += 64 * AHEAD) {
+    const int end = begin + per_wave < vecs ? begin + per_wave : vecs;
+    for (int v0 = begin + (threadIdx.x & 63); v0 < end; v0 += 64 * AHEAD) {
       vec r[AHEAD];
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j) {
-        const int v = v0 + 64 * j;
-        if (v < end && v < last) {
-          r[j] = load(v);
+        if (v0 + 64 * j < end) {
+          r[j] = load(v0 + 64 * j);
         } else {
 #pragma unroll
           for (int e = 0; e < VEC; ++e) r[j][e] = (T)-__builtin_inff();
@@ -120,38 +194,184 @@ struct Row {
         for (int e = 0; e < VEC; ++e) each((float)r[j][e], (v0 + 64 * j) * VEC - off + e);
     }
   }
-  // the indices that wavefront w has
-  __device__ __forceinline__ int first_of(int w) const {
-    const int64_t i = (int64_t)w * per_wave * VEC - off;
+  __device__ __forceinline__ int stretch_of(int i) const { return (i + off) / (per_wave * VEC); }
+  __device__ __forceinline__ int first_of(int stretch) const {
+    const int64_t i = (int64_t)stretch * per_wave * VEC - off;
     return i < 0 ? 0 : i < V ? (int)i : V;
   }
+  // begins with another wavefront of the row
+  __device__ __forceinline__ void to_part(int part) { begin = (part * kWaves + (threadIdx.x >> 6)) * per_wave; }
 };
 
-// The row's weights meet a histogram of their distance from the greatest logit, in 2048 bins of 28 / 2048 of the temperature: which bin the k-th token
-// lies in, and between which two the p-th share ends, is known from it; the tokens of those bins alone are sorted, and decide.  So a row is read three
-// times: for its greatest, for the histogram, for the sums and those tokens.  A wavefront sums its own stretch of the vocabulary; the token lies in the
-// stretch that passes the random share, which is looked at once more.
-constexpr int kListed = 4096;
-constexpr float kBinsOfUnit = kBins / 28.0f;  // (2^-40 is 27.73 below)
-
-struct Shared {
-  Block block;
-  double table[64];
-  u64 masses[kBins];
-  unsigned counts[kBins];
-  u64 list[kListed];
-  u64 sums[kThreads / 64], found[2];
-  unsigned listed, of_k_bin;
+// What a row asks for
+struct Asked {
+  float temperature;
+  int k;        // 0: all
+  bool shares;  // whether a share of the weight is cut
+  double p;
+  u64 least;  // weight that min_p asks for
+  __device__ __forceinline__ Asked(const SampleArgs& a, int row) {
+    temperature = a.temperature != nullptr ? a.temperature[row] : 1.0f;
+    const int k_given = a.top_k != nullptr ? a.top_k[row] : 0;
+    const float p_given = a.top_p != nullptr ? a.top_p[row] : 1.0f, m = a.min_p != nullptr ? a.min_p[row] : 0.0f;
+    k = k_given > 0 && k_given < a.V ? k_given : 0;
+    shares = p_given < 1.0f;
+    p = p_given > 0.0f ? (double)p_given : 0.0;
+    least = m > 0.0f ? (u64)ceil((m < 1.0f ? (double)m : 1.0) * 0x1p44) : 0;
+  }
+  __device__ __forceinline__ bool greedy() const { return !(temperature > 0.0f); }
+  __device__ __forceinline__ bool cuts() const { return k != 0 || shares; }
+  __device__ __forceinline__ float heat() const { return fmaxf(temperature, 0x1p-100f); }
 };
 
-// Descending; n tokens, the rest of a power of two zeros
+__device__ __forceinline__ void clear(Shared& sh) {
+  const int tid = threadIdx.x;
+  if (tid < 64) sh.table[tid] = exp2(tid * (1.0 / 64));
+  for (int i = tid; i < kBins; i += kThreads) {
+    sh.masses[i] = 0;
+    sh.counts[i] = 0;
+  }
+  if (tid == 0) sh.listed = sh.of_k_bin = 0;
+  __syncthreads();
+}
+
+template <typename T>
+__device__ __forceinline__ float greatest_of_thread(const Row<T>& row) {
+  float mine = -__builtin_inff();
+  row.walk([&](float x, int) { mine = fmaxf(mine, x); });  // (a NaN is left out)
+  return mine;
+}
+
+// The first bin for which it is so, and so for all behind it; kBins: none
+template <class Reached>
+__device__ __forceinline__ int first_bin(Shared& sh, Reached reached) {
+  return sh.block.count(!reached(2 * threadIdx.x), !reached(2 * threadIdx.x + 1));
+}
+__device__ __forceinline__ void cumulate_counts(Shared& sh) {
+  const int b = 2 * threadIdx.x;
+  __syncthreads();
+  const unsigned c0 = sh.counts[b], c1 = sh.counts[b + 1], before = (unsigned)sh.block.before(c0 + c1);
+  sh.counts[b] = before + c0;
+  sh.counts[b + 1] = before + c0 + c1;
+  __syncthreads();
+}
+
+// Of the greatest logits of the threads (maxima(i), n of this one) the k-th lies in the row's k-th's bin or behind it: behind it nothing is asked.
+template <class Maxima>
+__device__ __forceinline__ int bins_asked(Shared& sh, const Asked& asked, const Weights& weight, int n, Maxima maxima) {
+  if (asked.k == 0 || asked.k > n * kThreads) return kBins;
+  for (int i = 0; i < n; ++i) {
+    const float d = weight.distance(maxima(i));
+    if (d < (float)kBins) atomicAdd(&sh.counts[(int)d], 1u);
+  }
+  cumulate_counts(sh);
+  const int last = first_bin(sh, [&](int b) { return sh.counts[b] >= (unsigned)asked.k; });
+  sh.counts[2 * threadIdx.x] = sh.counts[2 * threadIdx.x + 1] = 0;
+  __syncthreads();
+  return last < kBins ? last + 1 : kBins;
+}
+
+template <typename T>
+__device__ __forceinline__ void histogram(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, int behind) {
+  const float most = (float)behind;
+  if (asked.k != 0 && asked.shares) {
+    row.walk([&](float x, int) {
+      const float d = weight.distance(x);
+      if (d < most) {
+        atomicAdd(&sh.counts[(int)d], 1u);
+        if (weight.has(x)) atomicAdd(&sh.masses[(int)d], weight.of(x));
+      }
+    });
+  } else if (asked.k != 0) {
+    row.walk([&](float x, int) {
+      const float d = weight.distance(x);
+      if (d < most) atomicAdd(&sh.counts[(int)d], 1u);
+    });
+  } else {
+    row.walk([&](float x, int) {
+      if (weight.has(x)) atomicAdd(&sh.masses[(int)weight.distance(x)], weight.of(x));
+    });
+  }
+}
+
+// What the whole row's histogram says
+struct Zones {
+  int k_bin, z0, z1;  // the k-th token's bin (kBins: none); the bins that the share's end may lie in
+  int sure;           // tokens of bins in front of this one are kept, of those behind it those of the list alone
+  int before_k;       // tokens in front of the k-th's bin
+  u64 front, between, all;  // weight in front of `sure`, between the share's bins and the k-th's, of all
+  __device__ __forceinline__ bool lists(int b) const { return b == k_bin || (b >= z0 && b <= z1); }
+};
+__device__ __forceinline__ Zones zones_of(Shared& sh, const Asked& asked) {
+  Zones z{kBins, kBins, -1, kBins, 0, 0, 0, 0};
+  if (asked.k != 0) {
+    cumulate_counts(sh);
+    z.k_bin = first_bin(sh, [&](int b) { return sh.counts[b] >= (unsigned)asked.k; });
+    z.before_k = z.k_bin < kBins && z.k_bin > 0 ? (int)sh.counts[z.k_bin - 1] : 0;
+  }
+  if (asked.shares) {
+    __syncthreads();
+    const int b = 2 * threadIdx.x;
+    const u64 m0 = sh.masses[b], m1 = sh.masses[b + 1], before = sh.block.before(m0 + m1);
+    sh.masses[b] = before + m0;
+    sh.masses[b + 1] = before + m0 + m1;
+    __syncthreads();
+    // the k tokens' weight lies between what is in front of the k-th's bin and what is up to it
+    const u64 most = sh.masses[z.k_bin < kBins ? z.k_bin : kBins - 1], fewest = z.k_bin == kBins ? most : z.k_bin > 0 ? sh.masses[z.k_bin - 1] : 0;
+    const double t0 = fmax(asked.p * (double)fewest, 1.0), t1 = fmax(asked.p * (double)most, 1.0);  // (a share of nothing: the greatest's bin)
+    z.z0 = first_bin(sh, [&](int i) { return (double)sh.masses[i] >= t0; });
+    z.z1 = first_bin(sh, [&](int i) { return (double)sh.masses[i] >= t1; });
+    z.z0 = z.z0 < z.k_bin ? z.z0 : z.k_bin;
+    z.z1 = z.z1 < z.k_bin ? z.z1 : z.k_bin;
+  }
+  z.sure = z.z0 < z.k_bin ? z.z0 : z.k_bin;
+  if (asked.shares) {
+    z.front = z.sure > 0 ? sh.masses[z.sure - 1] : 0;
+    z.between = z.k_bin < kBins && z.k_bin > 0 && z.z1 < z.k_bin ? sh.masses[z.k_bin - 1] - sh.masses[z.z1] : 0;
+    z.all = sh.masses[kBins - 1];
+  }
+  return z;
+}
+
+// The sum of the wavefront's stretch, of the tokens that are sure; the tokens of the list's bins to the list
+template <typename T>
+__device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, const Zones& z) {
+  u64 sum = 0;
+  const u64 least = asked.least;
+  if (z.sure == kBins) {  // no cut
+    row.walk([&](float x, int) {
+      const u64 w = weight(x);
+      sum += w >= least ? w : 0;
+    });
+  } else {
+    const float sure = (float)z.sure, last = (float)((z.k_bin < kBins ? z.k_bin : z.z1) + 1);
+    row.walk([&](float x, int i) {
+      const float d = weight.distance(x);
+      if (d < last) {
+        if (d < sure) {
+          const u64 w = weight(x);
+          sum += w >= least ? w : 0;
+        } else if (z.lists((int)d)) {
+          if ((int)d == z.k_bin) atomicAdd(&sh.of_k_bin, 1u);
+          const unsigned at = atomicAdd(&sh.listed, 1u);
+          if (at < kListed) sh.list[at] = place_of(x, i);
+        }
+      }
+    });
+  }
+  return last_lane(scan(sum, sum_of));
+}
+
+// Descending; n tokens, the rest of a power of two zeros.  A wavefront has 128 places in a row of its own, so only the steps beyond 64 need all of
+// them to meet.
 __device__ __forceinline__ void sort_list(u64* list, int n) {
-  int size = 64;
+  int size = 128;
   while (size < n) size *= 2;
   for (int i = n + threadIdx.x; i < size; i += kThreads) list[i] = 0;
+  __syncthreads();
   for (int span = 2; span <= size; span *= 2)
     for (int step = span / 2; step > 0; step /= 2) {
-      __syncthreads();
+      if (step > 32 && (step > 64 || span > 128)) __syncthreads();
       for (int i = threadIdx.x; i < size / 2; i += kThreads) {
         const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
         const u64 a = list[lo], b = list[hi];
@@ -160,11 +380,48 @@ __device__ __forceinline__ void sort_list(u64* list, int n) {
           list[hi] = a;
         }
       }
+      asm volatile("" ::: "memory");
     }
   __syncthreads();
 }
 
-// By histograms of the places' digits, one after the other, over the whole row: of rows whose bins hold too many tokens to sort (ties).  The least place of the smallest front part of the order from `from` on that has `target` tokens, or so much weight.
+// The cut, from the list's n tokens (at most kListed); the kept ones of them to the sums of the stretches that they lie in
+template <typename T>
+__device__ __forceinline__ u64 cut_of_list(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, const Zones& z, int n, int of_k_bin) {
+  sort_list(sh.list, n);
+  constexpr int EACH = kListed / kThreads;  // tokens of a thread, in order
+  const int i0 = threadIdx.x * EACH;
+  int end = z.k_bin < kBins ? n - of_k_bin + (asked.k - z.before_k) - 1 : n - 1;  // the last that is kept
+  if (asked.shares) {
+    u64 w[EACH], upto = 0;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      w[j] = i0 + j <= end ? weight(logit_of(sh.list[i0 + j])) : 0;
+      upto += w[j];
+    }
+    u64 listed;
+    const u64 before = sh.block.before(upto, &listed);
+    const double target = asked.p * (double)(z.k_bin < kBins ? z.front + listed + z.between : z.all);
+    int short_of = 0;  // the thread's tokens in front of which the share has not ended, and which do not end it
+    upto = z.front + before;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      upto += w[j];
+      short_of += i0 + j <= end && (double)upto < target ? 1 : 0;
+    }
+    const int at = (int)sh.block.all((u64)short_of, sum_of);
+    if (at < end) end = at;
+  }
+  const u64 cut = sh.list[end];
+  for (int i = threadIdx.x; i <= end; i += kThreads) {
+    const u64 place = sh.list[i], w = weight(logit_of(place));
+    if (w >= asked.least) atomicAdd(&sh.sums[row.stretch_of(index_of(place))], w);
+  }
+  return cut;
+}
+
+// By histograms of the places' digits, one after the other, over the whole row: of rows whose bins hold too many tokens to sort (ties).  The least
+// place of the smallest front part of the order from `from` on that has `target` tokens, or so much weight.
 template <typename T>
 __device__ __attribute__((noinline)) u64 cut_by_digits(Shared& sh, const Row<T>& row, const Weights& weight, bool by_mass, double target, u64 from) {
   const int tid = threadIdx.x;
@@ -214,218 +471,302 @@ __device__ __attribute__((noinline)) u64 cut_by_digits(Shared& sh, const Row<T>&
   }
   return prefix << shift;
 }
-
+// The cut of a row whose list is too long, and the sums of all its stretches
 template <typename T>
-__global__ void __launch_bounds__(kThreads) sample_rows_kernel(const SampleArgs a) {
-  __shared__ Shared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const Row<T> row((const T*)a.logits + (int64_t)blockIdx.x * a.row_stride, a.V);
-  if (tid < 64) sh.table[tid] = exp2(tid * (1.0 / 64));
-  for (int i = tid; i < kBins; i += kThreads) {
-    sh.masses[i] = 0;
-    sh.counts[i] = 0;
+__device__ __attribute__((noinline)) u64 cut_without_list(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, const Zones& z, int stretches) {
+  u64 cut = 0;
+  const int tid = threadIdx.x;
+  if (z.k_bin < kBins) cut = cut_by_digits<T>(sh, row, weight, false, (double)asked.k, 0);
+  if (asked.shares) {
+    u64 sum = 0;
+    for (int i = tid; i < row.V; i += kThreads) sum += place_of((float)row.x[i], i) >= cut ? weight((float)row.x[i]) : 0;
+    cut = max_of(cut, cut_by_digits<T>(sh, row, weight, true, asked.p * (double)sh.block.all(sum, sum_of), cut));
   }
-  if (tid == 0) sh.listed = sh.of_k_bin = 0;
-  auto store_sums = [&](u64 sum) {
+  __syncthreads();
+  for (int s = tid >> 6; s < stretches; s += kWaves) {
+    u64 sum = 0;
+    for (int i = row.first_of(s) + (tid & 63); i < row.first_of(s + 1); i += 64) {
+      const u64 w = place_of((float)row.x[i], i) >= cut ? weight((float)row.x[i]) : 0;
+      sum += w >= asked.least ? w : 0;
+    }
+    sum = last_lane(scan(sum, sum_of));
+    if ((tid & 63) == 0) sh.sums[s] = sum;
+  }
+  return cut;
+}
+
+// Of `vecs` vectors from `first` on, some of them a thread in a row: the first value up to which what they have passes `share`, counted from `before` on;
+// where none does the last that has any.  To the results, with its part of the total.
+template <typename T, class Has>
+__device__ __forceinline__ void answer(Shared& sh, const SampleArgs& a, int row_number, const Row<T>& row, int first, int vecs, u64 before, double share, u64 total, Has has) {
+  constexpr int VEC = Row<T>::VEC;
+  const int tid = threadIdx.x, each = (vecs + kThreads - 1) / kThreads, v0 = first + tid * each, most = first + vecs < row.vecs ? first + vecs : row.vecs;
+  const int v1 = v0 + each < most ? v0 + each : most;
+  u64 own = 0;
+#pragma unroll 4
+  for (int v = v0; v < v1; ++v) {
+    const auto x = row.load(v);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += (u64)__shfl_xor(sum, d);
-    if (lane == 0) sh.sums[wave] = sum;
-    __syncthreads();
-  };
-  const float temperature = a.temperature != nullptr ? a.temperature[blockIdx.x] : 1.0f;
-  const int k_given = a.top_k != nullptr ? a.top_k[blockIdx.x] : 0, k = k_given > 0 && k_given < a.V ? k_given : 0;
-  const float p_given = a.top_p != nullptr ? a.top_p[blockIdx.x] : 1.0f, m = a.min_p != nullptr ? a.min_p[blockIdx.x] : 0.0f;
-  const bool shares = p_given < 1.0f;
-  const double least = m > 1.0f ? 1.0 : m > 0.0f ? (double)m : 0.0, p = p_given > 0.0f ? (double)p_given : 0.0;
-  float mine = -__builtin_inff();
-  row.walk([&](float x, int) { mine = fmaxf(mine, x); });  // (a NaN is left out)
-  const float top = value_of((unsigned)sh.block.all((u64)key_of(mine), max_of));
-  if (top == -__builtin_inff() || !(temperature > 0.0f)) {
-    u64 first = 0;  // of the greatest, the lowest index (counted down)
-    if (mine == top) row.walk([&](float x, int i) { first = x == top && i >= 0 && i < a.V ? max_of(first, (u64)(unsigned)~i) : first; });
+    for (int e = 0; e < VEC; ++e) own += has((float)x[e], v * VEC - row.off + e);
+  }
+  before += sh.block.before(own);
+  const int who = sh.block.first(own != 0 && !((double)(before + own) <= share), own != 0);
+  if (tid != who) return;
+  int token = -1;
+  u64 w = 0;
+  bool on = true;
+  for (int v = v0; v < v1; ++v) {
+    const auto x = row.load(v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const int i = v * VEC - row.off + e;
+      const u64 next = on ? has((float)x[e], i) : 0;
+      token = next != 0 ? i : token;
+      w = next != 0 ? next : w;
+      before += next;
+      on = on && (next == 0 || (double)before <= share);
+    }
+  }
+  a.tokens[row_number] = token;
+  a.probs[row_number] = (float)((double)w / (double)total);
+}
+
+// From the sums of the stretches: the one that the random share ends in (of 1 and more the last one with a token, of what is no number the first)
+template <typename T>
+__device__ __forceinline__ void draw(Shared& sh, const SampleArgs& a, int row_number, const Row<T>& row, const Asked& asked, const Weights& weight, u64 cut, int stretches) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  const u64 own = tid < stretches ? sh.sums[tid] : 0;
+  u64 total;
+  const u64 before = sh.block.before(own, &total);
+  const double share = (double)a.random[row_number] * (double)total;
+  const int at = sh.block.first(own != 0 && !((double)(before + own) <= share), own != 0);
+  if (tid == at) sh.found[0] = before;
+  __syncthreads();
+  const u64 least = asked.least;
+  answer<T>(sh, a, row_number, row, at * row.per_wave, row.per_wave, sh.found[0], share, total, [&](float x, int i) {
+    const u64 w = place_of(x, i) >= cut ? weight(x) : 0;
+    return w >= least ? w : 0;
+  });
+}
+
+// Rows that need no weights: of a greatest logit of -infinity (none is drawn) or +infinity (its tokens have 1 each, the others none), greedy ones.
+// (part: the row, or the first part of it that has the greatest logit)
+template <typename T>
+__device__ __forceinline__ void draw_plain(Shared& sh, const SampleArgs& a, int row_number, const Row<T>& part, const Asked& asked, float top) {
+  const int tid = threadIdx.x;
+  if (top == -__builtin_inff() || asked.greedy()) {
+    u64 first = 0;  // the lowest index, counted down
+    part.walk([&](float x, int i) { first = x == top && i >= 0 && i < part.V ? max_of(first, (u64)(unsigned)~i) : first; });
     first = sh.block.all(first, max_of);
     if (tid == 0) {
-      a.tokens[blockIdx.x] = top == -__builtin_inff() ? -1 : (int)~(unsigned)first;
-      a.probs[blockIdx.x] = top == -__builtin_inff() ? 0.0f : 1.0f;
+      a.tokens[row_number] = top == -__builtin_inff() ? -1 : (int)~(unsigned)first;
+      a.probs[row_number] = top == -__builtin_inff() ? 0.0f : 1.0f;
     }
     return;
   }
-  const Weights weight{top, 92.332482616893657 / (double)temperature, sh.table};
-  const float scale = fminf(kBinsOfUnit / temperature, 3.4e38f);
-  auto bin_of = [&](float x) {  // in the logits' order; kBins: without weight
-    const float d = x == top ? 0.0f : (top - x) * scale;
-    return d < (float)kBins ? (int)d : kBins;
-  };
-  auto of_weight = [&](float x) {  // with what min_p leaves
-    const double w = weight.exact(x);
-    return w >= least ? Weights::whole(w) : (u64)0;
-  };
-  u64 cut = 0;
-  bool summed = false;
-  if (k != 0 || shares) {
-    // Of the greatest logits of the threads the k-th lies in a bin behind or at the row's k-th: behind it nothing is asked.
-    int behind = kBins;
-    auto first_bin = [&](auto reached) {  // the first for which it is so, kBins: none
-      const u64 at = sh.block.all(reached(2 * tid) ? (u64)(kBins - 2 * tid) : reached(2 * tid + 1) ? (u64)(kBins - 2 * tid - 1) : 0, max_of);
-      return kBins - (int)at;
-    };
-    auto cumulate_counts = [&] {
-      __syncthreads();
-      const unsigned c0 = sh.counts[2 * tid], c1 = sh.counts[2 * tid + 1], before = (unsigned)sh.block.before(c0 + c1);
-      sh.counts[2 * tid] = before + c0;
-      sh.counts[2 * tid + 1] = before + c0 + c1;
-      __syncthreads();
-    };
-    auto enough = [&](int b) { return sh.counts[b] >= (unsigned)k; };
-    if (k != 0 && k <= kThreads) {
-      const int b = bin_of(mine);
-      if (b < kBins) atomicAdd(&sh.counts[b], 1u);
-      cumulate_counts();
-      behind = first_bin(enough);
-      if (behind < kBins) ++behind;
-      sh.counts[2 * tid] = sh.counts[2 * tid + 1] = 0;
-      __syncthreads();
-    }
-    row.walk([&](float x, int) {
-      const int b = bin_of(x);
-      if (b < behind) {
-        if (k != 0) atomicAdd(&sh.counts[b], 1u);
-        if (shares) atomicAdd(&sh.masses[b], weight(x));
-      }
-    });
-    cumulate_counts();
-    int k_bin = kBins, z0 = kBins, z1 = -1;  // the k-th token's bin; those that the share may end in
-    if (k != 0) k_bin = first_bin(enough);
-    if (shares) {
-      const u64 m0 = sh.masses[2 * tid], m1 = sh.masses[2 * tid + 1], before = sh.block.before(m0 + m1);
-      sh.masses[2 * tid] = before + m0;
-      sh.masses[2 * tid + 1] = before + m0 + m1;
-      __syncthreads();
-      // the k tokens' weight lies between what is in front of the k-th's bin and what is up to it
-      const u64 most = sh.masses[k_bin < kBins ? k_bin : kBins - 1], fewest = k_bin == kBins ? most : k_bin > 0 ? sh.masses[k_bin - 1] : 0;
-      const double t0 = fmax(p * (double)fewest, 1.0), t1 = fmax(p * (double)most, 1.0);  // (a share of nothing: the greatest's bin)
-      z0 = first_bin([&](int b) { return (double)sh.masses[b] >= t0; });
-      z1 = first_bin([&](int b) { return (double)sh.masses[b] >= t1; });
-      z0 = z0 < k_bin ? z0 : k_bin;
-      z1 = z1 < k_bin ? z1 : k_bin;
-    }
-    if (k_bin < kBins || shares) {
-      const int sure = z0 < k_bin ? z0 : k_bin;  // tokens of bins in front of this one are kept, of those behind it those of the list alone
-      u64 sum = 0;
-      row.walk([&](float x, int i) {
-        const int b = bin_of(x);
-        if (b < sure) {
-          sum += of_weight(x);
-        } else if (b < kBins && (b == k_bin || (b >= z0 && b <= z1))) {
-          if (b == k_bin) atomicAdd(&sh.of_k_bin, 1u);
-          const unsigned at = atomicAdd(&sh.listed, 1u);
-          if (at < kListed) sh.list[at] = place_of(x, i);
-        }
-      });
-      store_sums(sum);
-      const int n = (int)sh.listed;
-      summed = n <= kListed;
-      if (summed) {
-        sort_list(sh.list, n);
-        // four tokens a thread, in order
-        constexpr int EACH = kListed / kThreads;
-        const int i0 = tid * EACH;
-        int end = n - 1;  // the last that is kept
-        if (k_bin < kBins) end = n - (int)sh.of_k_bin + (k - (int)(k_bin > 0 ? sh.counts[k_bin - 1] : 0)) - 1;
-        if (shares) {
-          u64 w[EACH], upto = 0, kept = 0;
-#pragma unroll
-          for (int j = 0; j < EACH; ++j) {
-            w[j] = i0 + j <= end ? weight(value_of((unsigned)(sh.list[i0 + j] >> 32))) : 0;
-            upto += w[j];
-          }
-          const u64 before = sh.block.before(upto), listed = sh.block.all(upto, sum_of), front = sure > 0 ? sh.masses[sure - 1] : 0;
-          if (k_bin < kBins)  // (with the bins between the share's and the k-th token's, which are not in the list)
-            kept = front + listed + (z1 < k_bin && k_bin > 0 ? sh.masses[k_bin - 1] - sh.masses[z1] : 0);
-          else
-            kept = sh.masses[kBins - 1];
-          const double target = p * (double)kept;
-          u64 at = 0;
-          upto = front + before;
-#pragma unroll
-          for (int j = 0; j < EACH; ++j) {
-            upto += w[j];
-            if (at == 0 && i0 + j <= end && (double)upto >= target) at = (u64)(kListed - (i0 + j));
-          }
-          at = sh.block.all(at, max_of);
-          if (at != 0) end = kListed - (int)at;
-        }
-        cut = sh.list[end];
-        // the kept tokens of the list, to the sums of the stretches that they lie in
-        for (int i = tid; i <= end; i += kThreads) {
-          const u64 place = sh.list[i];
-          atomicAdd(&sh.sums[((int)~(unsigned)place + row.off) / (row.per_wave * Row<T>::VEC)], of_weight(value_of((unsigned)(place >> 32))));
-        }
-      }
-    }
-    if (!summed) {
-      if (k_bin < kBins) cut = cut_by_digits<T>(sh, row, weight, false, (double)k, 0);
-      if (shares) {
-        u64 sum = 0;
-        row.walk([&](float x, int i) { sum += place_of(x, i) >= cut ? weight(x) : 0; });
-        cut = max_of(cut, cut_by_digits<T>(sh, row, weight, true, p * (double)sh.block.all(sum, sum_of), cut));
-      }
-    }
+  u64 count = 0;
+  for (int i = tid; i < part.V; i += kThreads) count += (float)part.x[i] == top;
+  // kept are the first of them, by index
+  u64 kept = sh.block.all(count, sum_of);
+  if (asked.k != 0 && kept > (u64)asked.k) kept = asked.k;
+  if (asked.shares) kept = (u64)fmax(1.0, ceil(asked.p * (double)kept));
+  // (as weights of 1: a random share of the kept ones does not pass the last of them)
+  const double share = fmin((double)a.random[row_number] * (double)kept, (double)kept - 0.5);
+  answer<T>(sh, a, row_number, part, 0, part.vecs, 0, share, kept, [&](float x, int) { return (u64)(x == top); });
+}
+
+__device__ __forceinline__ bool is_plain(const Asked& asked, float top) { return top == -__builtin_inff() || top == __builtin_inff() || asked.greedy(); }
+
+// ---- a workgroup a row ------------------------------------------------------------------------------------------------------------------
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sample_rows_kernel(const SampleArgs a) {
+  __shared__ Shared sh;
+  const Row<T> row(a, blockIdx.x, 0, 1);
+  const Asked asked(a, blockIdx.x);
+  clear(sh);
+  const float mine = greatest_of_thread(row), top = value_of((unsigned)sh.block.all((u64)key_of(mine), max_of));
+  if (is_plain(asked, top)) return draw_plain<T>(sh, a, blockIdx.x, row, asked, top);
+  const Weights weight(top, asked.heat(), sh.table);
+  Zones z{kBins, kBins, -1, kBins, 0, 0, 0, 0};
+  if (asked.cuts()) {
+    histogram(sh, row, asked, weight, bins_asked(sh, asked, weight, 1, [&](int) { return mine; }));
+    z = zones_of(sh, asked);
   }
-  if (!summed) {
-    u64 sum = 0;
-    row.walk([&](float x, int i) { sum += bin_of(x) < kBins && place_of(x, i) >= cut ? of_weight(x) : 0; });
-    store_sums(sum);
-  }
+  const u64 sum = gather(sh, row, asked, weight, z);
+  if ((threadIdx.x & 63) == 0) sh.sums[threadIdx.x >> 6] = sum;
   __syncthreads();
-  // the stretch that the random share ends in (of 1 and more the last one with a token, of what is no number the first), ...
-  u64 total = 0, before = 0;
-  for (int w = 0; w < kThreads / 64; ++w) total += sh.sums[w];
-  const double share = (double)a.random[blockIdx.x] * (double)total;
-  int at = -1;
-  for (int w = 0; w < kThreads / 64; ++w) {
-    const u64 s = sh.sums[w];
-    if (s == 0) continue;
-    if (at >= 0) before += sh.sums[at];
-    at = w;
-    if (!((double)(before + s) <= share)) break;
+  u64 cut = 0;
+  if (z.sure < kBins) {
+    const int n = (int)sh.listed;
+    cut = n <= kListed ? cut_of_list<T>(sh, row, asked, weight, z, n, (int)sh.of_k_bin) : cut_without_list<T>(sh, row, asked, weight, z, kWaves);
   }
-  // ... a piece of it for each thread, and the token
-  const int begin = row.first_of(at), end = row.first_of(at + 1), each = (end - begin + kThreads - 1) / kThreads;
-  const int i0 = begin + tid * each, i1 = i0 + each < end ? i0 + each : end;
-  auto kept = [&](int i) {
-    const float x = (float)row.x[i];
-    return bin_of(x) < kBins && place_of(x, i) >= cut ? of_weight(x) : (u64)0;
-  };
-  u64 own = 0;
-  for (int i = i0; i < i1; ++i) own += kept(i);
-  before += sh.block.before(own);
-  const bool here = own != 0 && !((double)(before + own) <= share);
-  const u64 who = sh.block.all(here ? (u64)(kThreads - tid) : 0, max_of), last = sh.block.all(own != 0 ? (u64)(tid + 1) : 0, max_of);
-  if (tid == (who != 0 ? kThreads - (int)who : (int)last - 1)) {
-    int token = -1;
-    u64 w = 0;
-    for (int i = i0; i < i1; ++i) {
-      const u64 next = kept(i);
-      if (next == 0) continue;
-      token = i;
-      w = next;
-      before += next;
-      if (!((double)before <= share)) break;
+  draw<T>(sh, a, blockIdx.x, row, asked, weight, cut, kWaves);
+}
+
+// ---- several workgroups a row: a launch a reading, what they leave for each other in the workspace -----------------------------------------
+struct Parts {
+  uint8_t* space;
+  int parts;
+};
+struct Space {
+  uint32_t* tops;
+  float* maxima;
+  u64 *masses, *sums, *list;
+  unsigned *counts, *listed;
+  Zones* zones;
+  __device__ __forceinline__ Space(const Parts& p, int row) {
+    const SampleSpace s = sample_space(p.parts);
+    uint8_t* at = p.space + row * s.bytes;
+    tops = (uint32_t*)(at + s.tops);
+    maxima = (float*)(at + s.maxima);
+    masses = (u64*)(at + s.masses);
+    counts = (unsigned*)(at + s.counts);
+    sums = (u64*)(at + s.sums);
+    listed = (unsigned*)(at + s.listed);
+    list = (u64*)(at + s.list);
+    zones = (Zones*)(at + s.zones);
+  }
+};
+static_assert(sizeof(Zones) <= 64, "as the workspace has it");
+
+__device__ __forceinline__ float top_of(const Space& s, int parts) {
+  unsigned key = 0;
+  for (int i = 0; i < parts; ++i) key = key > s.tops[i] ? key : s.tops[i];
+  return value_of(key);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sample_tops_kernel(const SampleArgs a, const Parts p) {
+  __shared__ Block block;
+  const Row<T> row(a, blockIdx.y, blockIdx.x, p.parts);
+  const Space s(p, blockIdx.y);
+  const float mine = greatest_of_thread(row);
+  s.maxima[blockIdx.x * kThreads + threadIdx.x] = mine;
+  const u64 key = block.all((u64)key_of(mine), max_of);
+  if (threadIdx.x == 0) s.tops[blockIdx.x] = (unsigned)key;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sample_histograms_kernel(const SampleArgs a, const Parts p) {
+  __shared__ Shared sh;
+  const Row<T> row(a, blockIdx.y, blockIdx.x, p.parts);
+  const Space s(p, blockIdx.y);
+  const Asked asked(a, blockIdx.y);
+  const float top = top_of(s, p.parts);
+  if (is_plain(asked, top) || !asked.cuts()) return;
+  clear(sh);
+  const Weights weight(top, asked.heat(), sh.table);
+  histogram(sh, row, asked, weight, bins_asked(sh, asked, weight, p.parts, [&](int i) { return s.maxima[i * kThreads + threadIdx.x]; }));
+  __syncthreads();
+  for (int i = threadIdx.x; i < kBins; i += kThreads) {
+    s.masses[blockIdx.x * kBins + i] = sh.masses[i];
+    s.counts[blockIdx.x * kBins + i] = sh.counts[i];
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sample_sums_kernel(const SampleArgs a, const Parts p) {
+  __shared__ Shared sh;
+  const int tid = threadIdx.x;
+  const Row<T> row(a, blockIdx.y, blockIdx.x, p.parts);
+  const Space s(p, blockIdx.y);
+  const Asked asked(a, blockIdx.y);
+  const float top = top_of(s, p.parts);
+  if (is_plain(asked, top)) return;
+  clear(sh);
+  const Weights weight(top, asked.heat(), sh.table);
+  Zones z{kBins, kBins, -1, kBins, 0, 0, 0, 0};
+  if (asked.cuts()) {
+    for (int i = tid; i < kBins; i += kThreads) {
+      u64 m = 0;
+      unsigned c = 0;
+      for (int j = 0; j < p.parts; ++j) {
+        m += s.masses[j * kBins + i];
+        c += s.counts[j * kBins + i];
+      }
+      sh.masses[i] = m;
+      sh.counts[i] = c;
     }
-    a.tokens[blockIdx.x] = token;
-    a.probs[blockIdx.x] = (float)((double)w / (double)total);
+    __syncthreads();
+    z = zones_of(sh, asked);
   }
+  const u64 sum = gather(sh, row, asked, weight, z);
+  if ((tid & 63) == 0) s.sums[blockIdx.x * kWaves + (tid >> 6)] = sum;
+  __syncthreads();
+  const int n = (int)sh.listed;
+  for (int i = tid; i < n && i < kListed; i += kThreads) s.list[blockIdx.x * kListed + i] = sh.list[i];
+  if (tid == 0) {
+    s.listed[2 * blockIdx.x] = n;
+    s.listed[2 * blockIdx.x + 1] = sh.of_k_bin;
+    if (blockIdx.x == 0) *s.zones = z;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) sample_answers_kernel(const SampleArgs a, const Parts p) {
+  __shared__ Shared sh;
+  const int tid = threadIdx.x, stretches = p.parts * kWaves;
+  Row<T> row(a, blockIdx.x, 0, p.parts);
+  const Space s(p, blockIdx.x);
+  const Asked asked(a, blockIdx.x);
+  const float top = top_of(s, p.parts);
+  if (is_plain(asked, top)) {
+    int part = 0;
+    while (s.tops[part] != key_of(top)) ++part;
+    row.to_part(part);
+    return draw_plain<T>(sh, a, blockIdx.x, row, asked, top);
+  }
+  clear(sh);
+  const Weights weight(top, asked.heat(), sh.table);
+  if (tid < stretches) sh.sums[tid] = s.sums[tid];
+  const Zones z = *s.zones;
+  u64 cut = 0;
+  if (z.sure < kBins) {
+    u64 n = 0;
+    int of_k_bin = 0;
+    for (int j = 0; j < p.parts; ++j) n += s.listed[2 * j];
+    if (n <= kListed) {
+      int at = 0;
+      for (int j = 0; j < p.parts; ++j) {
+        const int m = (int)s.listed[2 * j];
+        for (int i = tid; i < m; i += kThreads) sh.list[at + i] = s.list[j * kListed + i];
+        at += m;
+        of_k_bin += (int)s.listed[2 * j + 1];
+      }
+      __syncthreads();
+      cut = cut_of_list<T>(sh, row, asked, weight, z, (int)n, of_k_bin);
+    } else {
+      cut = cut_without_list<T>(sh, row, asked, weight, z, stretches);
+    }
+  }
+  draw<T>(sh, a, blockIdx.x, row, asked, weight, cut, stretches);
+}
+
+template <typename T>
+gpusq_status launch_typed(const SampleArgs& a, int64_t rows, void* workspace, hipStream_t s) {
+  const int parts = sample_parts(rows, a.V);
+  if (parts == 1) {
+    sample_rows_kernel<T><<<(unsigned)rows, kThreads, 0, s>>>(a);
+    return check_launch();
+  }
+  const Parts p{(uint8_t*)workspace, parts};
+  const dim3 grid((unsigned)parts, (unsigned)rows);
+  gpusq_status st;
+  sample_tops_kernel<T><<<grid, kThreads, 0, s>>>(a, p);
+  if ((st = check_launch()) != GPUSQ_OK) return st;
+  sample_histograms_kernel<T><<<grid, kThreads, 0, s>>>(a, p);
+  if ((st = check_launch()) != GPUSQ_OK) return st;
+  sample_sums_kernel<T><<<grid, kThreads, 0, s>>>(a, p);
+  if ((st = check_launch()) != GPUSQ_OK) return st;
+  sample_answers_kernel<T><<<(unsigned)rows, kThreads, 0, s>>>(a, p);
+  return check_launch();
 }
 
 }  // namespace
 
-gpusq_status launch_sample_tokens(const SampleArgs& a, bool f32, int64_t rows, hipStream_t s) {
-  if (f32)
-    sample_rows_kernel<float><<<(unsigned)rows, kThreads, 0, s>>>(a);
-  else
-    sample_rows_kernel<_Float16><<<(unsigned)rows, kThreads, 0, s>>>(a);
-  return check_launch();
+gpusq_status launch_sample_tokens(const SampleArgs& a, bool f32, int64_t rows, void* workspace, hipStream_t s) {
+  return f32 ? launch_typed<float>(a, rows, workspace, s) : launch_typed<_Float16>(a, rows, workspace, s);
 }
 
 }  // namespace gpusq

@@ -35,7 +35,8 @@ EXPORTS = [
     "gpusq_block_mlp_int8", "gpusq_block_mlp_int8_launches",
     "gpusq_int4_groups_packed_bytes", "gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_kv4_page_bytes",
     "gpusq_qk_norm_rope", "gpusq_attention_kv4_workspace_bytes", "gpusq_attention_kv4", "gpusq_cross_attention_workspace_bytes", "gpusq_cross_attention",
-    "gpusq_attention_tree_kv4", "gpusq_draft_tree", "gpusq_accept_drafts", "gpusq_linear_int8_tokens_workspace_bytes", "gpusq_linear_int8_tokens", "gpusq_sample_tokens",
+    "gpusq_attention_tree_kv4", "gpusq_draft_tree", "gpusq_accept_drafts", "gpusq_linear_int8_tokens_workspace_bytes", "gpusq_linear_int8_tokens", "gpusq_sample_tokens_workspace_bytes",
+    "gpusq_sample_tokens",
 ]
 
 
@@ -67,7 +68,7 @@ _SIGNATURES = {
     "gpusq_quantize_groups_int4": "tittiis", "gpusq_pack_int4_groups": "ttitiis", "gpusq_linear_int4": "ttittiiiiis",
     "gpusq_qk_norm_rope": "piiiiiiittftttiiitttttis", "gpusq_attention_kv4": "tttttttiiiiiiiifs", "gpusq_cross_attention": "pppttttiiiiiiiiiiiiiiifs",
     "gpusq_attention_tree_kv4": "uuuuuuiuuiiiiiiiifs", "gpusq_draft_tree": "uuuuuuuiiiis", "gpusq_accept_drafts": "uuuuuupiuuuuiiiiiiis",
-    "gpusq_linear_int8_tokens": "uiuuuuiuiiiis", "gpusq_sample_tokens": "viiuuuuuuuiis",
+    "gpusq_linear_int8_tokens": "uiuuuuiuiiiis", "gpusq_sample_tokens": "viiuuuuuuuuiis",
 }
 
 
@@ -206,11 +207,12 @@ def lib():
         L.gpusq_accept_drafts.argtypes = [vp] * 7 + [i64] + [vp] * 4 + [i64] * 7 + [vp]
         L.gpusq_linear_int8_tokens_workspace_bytes.argtypes = [i64] * 2
         L.gpusq_linear_int8_tokens.argtypes = [vp, ci] + [vp] * 4 + [ci, vp] + [i64] * 3 + [ci, vp]
-        L.gpusq_sample_tokens.argtypes = [vp, ci, i64] + [vp] * 7 + [i64] * 2 + [vp]
+        L.gpusq_sample_tokens_workspace_bytes.argtypes = [i64] * 2
+        L.gpusq_sample_tokens.argtypes = [vp, ci, i64] + [vp] * 8 + [i64] * 2 + [vp]
         for name in ("gpusq_attention_tree_kv4", "gpusq_draft_tree", "gpusq_accept_drafts", "gpusq_linear_int8_tokens", "gpusq_sample_tokens"):
             getattr(L, name).restype = ci
         for name in ("gpusq_int4_groups_packed_bytes", "gpusq_kv4_page_bytes", "gpusq_attention_kv4_workspace_bytes", "gpusq_cross_attention_workspace_bytes",
-                     "gpusq_linear_int8_tokens_workspace_bytes"):
+                     "gpusq_linear_int8_tokens_workspace_bytes", "gpusq_sample_tokens_workspace_bytes"):
             getattr(L, name).restype = sz
         for name in ("gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_qk_norm_rope", "gpusq_attention_kv4", "gpusq_cross_attention"):
             getattr(L, name).restype = ci
@@ -728,7 +730,7 @@ def linear_int8_tokens(X, Wq, w_scale, bias=None, gelu=False, out_dtype=torch.fl
     return out
 
 
-def sample_tokens(logits, random, temperature=None, top_k=None, top_p=None, min_p=None):
+def sample_tokens(logits, random, temperature=None, top_k=None, top_p=None, min_p=None, workspace=None):
     """gpusq_sample_tokens: logits [rows,vocabulary] fp16 or fp32 (rows contiguous, any stride between them), random [rows] fp32 in [0, 1), temperature, top_p,
     min_p [rows] fp32, top_k [rows] int32 (None: 1, no cut) -> (tokens [rows] int32, their shares of what was kept [rows] fp32)"""
     f32, i32 = torch.float32, torch.int32
@@ -739,5 +741,6 @@ def sample_tokens(logits, random, temperature=None, top_k=None, top_p=None, min_
     for t, dt, name in ((temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"), (min_p, f32, "min_p")):
         _want(t is None or _is(t, dt, R), "%s: [rows] %s on the GPU" % (name, "int32" if dt is i32 else "float32"))
     tokens, probs = _empty(logits, i32, R), _empty(logits, f32, R)
-    calls.gpusq_sample_tokens(logits, _TORCH_DT[logits.dtype], logits.stride(0) if R > 1 else V, random, temperature, top_k, top_p, min_p, tokens, probs, R, V)
+    workspace = _workspace(logits, workspace, _size("gpusq_sample_tokens_workspace_bytes", R, V))
+    calls.gpusq_sample_tokens(logits, _TORCH_DT[logits.dtype], logits.stride(0) if R > 1 else V, random, temperature, top_k, top_p, min_p, tokens, probs, workspace, R, V)
     return tokens, probs

@@ -57,9 +57,11 @@ def test_linear_int8_tokens(g):
 
 
 def test_sample_tokens(g):
-    base = dict(logits=P, dt=g.F32, stride=1000, random=P, T=P, k=P, p=P, m=P, tokens=P, probs=P, rows=3, V=999, stream=None)
+    base = dict(logits=P, dt=g.F32, stride=1000, random=P, T=P, k=P, p=P, m=P, tokens=P, probs=P, ws=P, rows=3, V=999, stream=None)
     _refuses(g, "gpusq_sample_tokens", base, [
         (ERR_NULL, dict(logits=None)), (ERR_NULL, dict(random=None)), (ERR_NULL, dict(tokens=None)), (ERR_NULL, dict(probs=None)), (ERR_SHAPE, dict(rows=0)), (ERR_SHAPE, dict(V=0)),
         (ERR_SHAPE, dict(V=1001)), (ERR_SHAPE, dict(V=2**18 + 1, stride=2**19)), (ERR_SHAPE, dict(stride=2**31)), (ERR_SHAPE, dict(rows=2**22)), (ERR_UNSUPPORTED, dict(dt=g.I8)),
         (ERR_ALIGN, dict(logits=P + 2)), (ERR_ALIGN, dict(logits=P + 1, dt=g.F16)), (ERR_ALIGN, dict(random=P + 2)), (ERR_ALIGN, dict(T=P + 2)), (ERR_ALIGN, dict(k=P + 2)), (ERR_ALIGN, dict(p=P + 2)),
-        (ERR_ALIGN, dict(m=P + 2)), (ERR_ALIGN, dict(tokens=P + 2)), (ERR_ALIGN, dict(probs=P + 2))])
+        (ERR_ALIGN, dict(m=P + 2)), (ERR_ALIGN, dict(tokens=P + 2)), (ERR_ALIGN, dict(probs=P + 2)), (ERR_ALIGN, dict(ws=ODD)), (ERR_NULL, dict(V=200000, stride=200000, ws=None))])
+    size = g.lib().gpusq_sample_tokens_workspace_bytes
+    assert size(1, 200000) > 0 and size(1, 200000) % 16 == 0 and size(1000, 200000) == 0 and size(1, 1000) == 0 and size(0, 1000) == 0 and size(1, 2**18 + 1) == 0

@@ -78,6 +78,42 @@ def test_the_most_tokens(g, dt):
         _check(g, x, r.random(6).astype(F32), [1.0, 1.0, 0.7, 1.0, 1.3, 2.0], k, p, m)
 
 
+# 2, 4 and 8 workgroups a row
+@pytest.mark.parametrize("rows,V", [(12, 65536), (12, 70000), (12, 150001), (60, 66000), (128, 65537)])
+@pytest.mark.parametrize("dt", [np.float32, np.float16])
+def test_rows_over_several_workgroups(g, rows, V, dt):
+    r = np.random.default_rng(V)
+    size = g.lib().gpusq_sample_tokens_workspace_bytes(rows, V)
+    assert size > 0
+    params = [(1.0, 0, 1, 0), (0.7, 50, 1, 0), (1.3, 0, 0.9, 0), (1, 700, 0.95, 0.01), (1, 3000, 1, 0), (0, 5, 0.5, 0.2), (1, 0, 1, 0.05), (1, V - 3, 0.999, 0), (1, 0, 0.01, 0), (0.5, 1, 1, 0), (1, 2, 0, 2)]
+    for n, kind in enumerate(KINDS + ["none", "infinite"]):
+        x = np.array([_row(r, V, kind if kind in KINDS else "normal") for _ in range(rows)])
+        if kind == "none":
+            x[:] = -np.inf
+            x[::2, 5] = np.nan
+        if kind == "infinite":
+            x[:, r.integers(0, V, 9)] = np.inf
+        T, k, p, m = zip(*[params[(n + i) % len(params)] for i in range(rows)])
+        with np.errstate(over="ignore"):
+            x = x.astype(dt)
+        u = r.random(rows).astype(F32)
+        tokens, _ = _check(g, x, u, T, k, p, m)
+        t = lambda a, d: dev(np.asarray(a, d))  # noqa: E731
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        again, _ = g.sample_tokens(dev(x), dev(u), temperature=t(T, F32), top_k=t(k, np.int32), top_p=t(p, F32), min_p=t(m, F32), workspace=ws)
+        assert np.array_equal(host(again), tokens)
+
+
+def test_infinite_logits_are_cut_like_others(g):
+    """Tokens of +infinity weigh 1 each: by k, by share, by index"""
+    x = np.zeros((8, 300), F32)
+    x[:, [7, 50, 60, 299]] = np.inf
+    u = np.array([0.0, 0.3, 0.6, 0.99, 0.99, 0.99, 1.0, 0.99], F32)
+    k, p = np.array([0, 0, 0, 0, 2, 0, 3, 3], np.int32), np.array([1, 1, 1, 1, 1, 0.5, 1, 0.1], F32)
+    tokens, probs = g.sample_tokens(dev(x), dev(u), top_k=dev(k), top_p=dev(p))
+    assert host(tokens).tolist() == [7, 50, 60, 299, 50, 50, 60, 7] and host(probs).tolist() == [0.25, 0.25, 0.25, 0.25, 0.5, 0.5, F32(1) / F32(3), 1]
+
+
 def test_ties_go_to_the_lowest_index(g):
     V = 4096
     x = np.zeros((6, V), F32)
