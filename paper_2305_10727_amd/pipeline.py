@@ -325,17 +325,19 @@ class DecoderLayer:
     def _linear(self, name, x, gelu=False):
         return G.linear_int4(x, self.packed[name], self.widths[name][0], self.group, gelu=gelu)
 
-    def forward(self, x, norms, rope, positions, slots, block_table, kv_lens, head_weights=(None, None), state_lens=None):
+    def forward(self, x, norms, rope, positions, slots, block_table, kv_lens, head_weights=(None, None), state_lens=None, tree=None):
         """x [T, D] fp16, T / batch new tokens of each sequence; rope: (cos, sin); positions, slots [T], block_table [batch, pages of a sequence],
-        kv_lens [batch] (with the new tokens), state_lens [batch] or None: int32.  -> [T, D] fp16"""
+        kv_lens [batch] (with the new tokens), state_lens [batch] or None, tree [T, words] or None (gpusq.draft_tree, as positions and slots then are:
+        the new tokens are drafts, and see what they follow): int32.  -> [T, D] fp16"""
         T, H, hd = x.shape[0], self.heads, self.head_dim
         # what a later call would refuse, before the tokens are in the cache
         G._want(T % self.batch == 0, "x: as many tokens of each of the %d sequences" % self.batch)
         G._want(G._is(block_table, torch.int32, self.batch, -1) and G._is(kv_lens, torch.int32, self.batch) and
                 (state_lens is None or G._is(state_lens, torch.int32, self.batch)), "block_table: [batch, pages] int32, kv_lens and state_lens: [batch] int32, on the GPU")
+        G._want(tree is None or G._is(tree, torch.int32, T, max(1, (T // self.batch + 31) // 32)), "tree: [tokens, words] int32 of draft_tree")
         q = G.qk_norm_rope(self._linear("qkv", norms[0](x)), H, self.kv_heads, hd, q_weight=head_weights[0], k_weight=head_weights[1], cos=rope[0], sin=rope[1],
                            positions=positions, cache=self.cache, slots=slots)
-        a = G.attention_kv4(q, self.cache, block_table, kv_lens, max_q=T // self.batch)
+        a = G.attention_kv4(q, self.cache, block_table, kv_lens, max_q=T // self.batch, tree=tree)
         x = x + self._linear("out", a.view(T, H * hd))
         q = self._linear("query", norms[1](x)).view(self.batch, T // self.batch, H, hd)
         kv = self.states_kv.Y.view(self.batch, self.states, 2 * self.kv_heads, hd)
@@ -356,4 +358,66 @@ class DecoderLayer:
 
     def replay(self):
         self.graph.replay()
+        return self.out
+
+
+class DraftedAnswers:
+    """DecoderLayers that answer several tokens a step: something cheap drafts tokens behind each sequence's last one, a tree of them, the layers run all of them
+    at once, a token is drawn behind each, and the drafts that were drawn are kept.  A step is, besides the layers,
+        which nodes see each other, their positions and places (draft_tree), [embedding], the layers, [norm], products with the vocabulary's 8-bit weights with a
+        scale for each token (linear_int8_tokens), a token behind each node (sample_tokens), the branch that agrees, its keys and values moved together in
+        every layer's cache (accept_drafts):
+    `embed` ([T] int32 -> [T, D] fp16) and the norms are the caller's, and so are the drafts.  Whatever is drafted, greedy answers are those of one token a step;
+    drawn ones have the tokens' own shares, as a draft is kept only where it is what was drawn.  capture() records a step into a HIP graph."""
+
+    def __init__(self, layers, vocabulary, device="cuda"):
+        if not layers or len({id(l) for l in layers}) < len(layers) or any(l.batch != layers[0].batch or l.D != layers[0].D or l.cache.shape != layers[0].cache.shape for l in layers):
+            raise ValueError("layers: at least one, each another, of one width, batch and size of the cache")
+        self.layers, self.vocabulary, self.batch, self.D = list(layers), vocabulary, layers[0].batch, layers[0].D
+        self.Wq = torch.empty((vocabulary, self.D), dtype=torch.int8, device=device)
+        self.w_scale = torch.empty((vocabulary,), dtype=torch.float32, device=device)
+        self.graph = self.logits = None
+
+    def prepare_weights(self, W):
+        """W [vocabulary, D] fp32 or fp16, to 8 bits with a scale for each row.  (The layers' weights are theirs to prepare.)  Weights that are prepared
+        again go to where the former ones were."""
+        G._want(W.shape == (self.vocabulary, self.D), "W: [%d, %d] wanted" % (self.vocabulary, self.D))
+        G.calls.gpusq_quantize_int8(W, G._TORCH_DT[W.dtype], self.Wq, self.w_scale, G.PER_ROW, 0, self.vocabulary, self.D, None)
+
+    def step(self, drafted, parents, random, embed, norms, head_norm, rope, block_table, kv_lens, head_weights=None, state_lens=None, temperature=None, top_k=None,
+             top_p=None, min_p=None):
+        """drafted, parents [T] int32, T / batch nodes of each sequence: node 0 is its last answer, whose parent is -1; random [T] fp32 in [0, 1); norms: a triple
+        for each layer, as DecoderLayer.forward takes it; kv_lens [batch] int32, with all nodes; head_weights: a pair for each layer, or None; temperature, top_k,
+        top_p, min_p [T], as sample_tokens takes them.  -> (path [batch, T / batch], accepted [batch], answers [batch], new lengths [batch]); the next
+        step's node 0 is the answer, its kv_lens the new lengths and its nodes.  `logits` [T, vocabulary] fp32 are this step's until the next."""
+        T, f32, i32 = drafted.shape[0], torch.float32, torch.int32
+        # what a later call would refuse, before the tokens are in the caches
+        G._want(T % self.batch == 0, "drafted: as many nodes of each of the %d sequences" % self.batch)
+        G._want(G._is(drafted, i32, T) and G._is(parents, i32, T) and G._is(kv_lens, i32, self.batch), "drafted, parents: [tokens] int32, kv_lens: [batch] int32, on the GPU")
+        for t, dt, name in ((random, f32, "random"), (temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"), (min_p, f32, "min_p")):
+            G._want((t is None and name != "random") or G._is(t, dt, T), "%s: [tokens] %s on the GPU" % (name, "int32" if dt is i32 else "float32"))
+        G._want(len(norms) == len(self.layers) and (head_weights is None or len(head_weights) == len(self.layers)), "norms, head_weights: of each layer")
+        tree, positions, slots = G.draft_tree(parents, kv_lens, block_table)
+        x = embed(drafted)
+        for i, layer in enumerate(self.layers):
+            x = layer.forward(x, norms[i], rope, positions, slots, block_table, kv_lens, head_weights=(None, None) if head_weights is None else head_weights[i],
+                              state_lens=state_lens, tree=tree)
+        self.logits = G.linear_int8_tokens(head_norm(x), self.Wq, self.w_scale, out_dtype=f32)
+        sampled, _ = G.sample_tokens(self.logits, random, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+        return G.accept_drafts(drafted, sampled, parents, kv_lens, caches=[layer.cache for layer in self.layers], block_table=block_table)
+
+    def capture(self, *args, **kwargs):
+        """Records step() on these tensors into a HIP graph: replay() reruns it on what they hold then, into the same outputs.  They are kept here, as the graph
+        has their addresses.  (The eager run in front of it, which loads every kernel, is a step: it keeps drafts and moves them in the caches.)"""
+        self.step(*args, **kwargs)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = self.step(*args, **kwargs)
+        self.graph, self.out, self.captured = graph, out, (args, kwargs, self.logits)
+        return self.graph
+
+    def replay(self):
+        self.graph.replay()
+        self.logits = self.captured[2]
         return self.out
