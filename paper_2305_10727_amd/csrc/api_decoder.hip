@@ -45,9 +45,9 @@ bool are_cross_sizes(int64_t batch, int64_t q_len, int64_t kv_len, int64_t heads
 }
 
 // whether the launches of an attention and of its parts' join count their threads
-bool is_launchable(bool kv4, int64_t batch, int64_t q_len, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t D, const AttendParts& p, bool reach) {
+bool is_launchable(bool kv4, int64_t batch, int64_t q_len, int64_t tokens, int64_t heads, int64_t kv_heads, int64_t D, const AttendParts& p, bool reach, bool tree = false) {
   const int64_t cols = q_len * (heads / kv_heads);
-  return attend_launchable(batch * kv_heads * p.parts, cols, attend_shape(kv4, padded_head((int)D), cols, reach)) &&
+  return attend_launchable(batch * kv_heads * p.parts, cols, attend_shape(kv4, padded_head((int)D), cols, reach, tree ? batch * kv_heads : 0)) &&
          (p.parts == 1 || launchable(join_workgroups(tokens * heads, D, p.parts), 256));
 }
 
@@ -65,8 +65,8 @@ gpusq_status attend_kv4(AttentionKv4 x, hipStream_t s) {
   if (!are_kv4_sizes(x.tokens, x.batch, x.max_q, x.max_pages, x.heads, x.head_dim) || !is_size(x.num_pages) || (!x.cu_q && x.tokens != x.batch * x.max_q))
     return GPUSQ_ERR_SHAPE;
   if (!score_scale(x.scale, x.head_dim, &x.scale)) return GPUSQ_ERR_UNSUPPORTED;
-  const AttendParts p = attend_parts(true, x.batch, x.max_q, x.heads, x.kv_heads, x.head_dim, x.max_pages * kPageTokens);
-  if (!is_launchable(true, x.batch, x.max_q, x.tokens, x.heads, x.kv_heads, x.head_dim, p, true)) return GPUSQ_ERR_SHAPE;
+  const AttendParts p = attend_parts(true, x.batch, x.max_q, x.heads, x.kv_heads, x.head_dim, x.max_pages * kPageTokens, x.tree != nullptr);
+  if (!is_launchable(true, x.batch, x.max_q, x.tokens, x.heads, x.kv_heads, x.head_dim, p, true, x.tree != nullptr)) return GPUSQ_ERR_SHAPE;
   if (p.parts > 1 && !x.workspace) return GPUSQ_ERR_NULL;
   if (!aligned16(x.q) || !aligned16(x.cache) || !aligned16(x.out) || !aligned16(x.workspace) || !aligned4(x.block_table) || !aligned4(x.kv_lens) || !aligned4(x.cu_q))
     return GPUSQ_ERR_ALIGN;
@@ -155,6 +155,11 @@ gpusq_status gpusq_qk_norm_rope(const void* qkv, gpusq_dtype dt, int64_t row_str
 size_t gpusq_attention_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads, int64_t head_dim) {
   if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !are_kv4_sizes(tokens, batch, max_q, max_pages, heads, head_dim)) return 0;
   return parts_bytes(attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens), tokens, heads, head_dim);
+}
+
+size_t gpusq_attention_tree_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads, int64_t head_dim) {
+  if (check_heads(heads, kv_heads, head_dim) != GPUSQ_OK || !are_kv4_sizes(tokens, batch, max_q, max_pages, heads, head_dim)) return 0;
+  return parts_bytes(attend_parts(true, batch, max_q, heads, kv_heads, head_dim, max_pages * kPageTokens, true), tokens, heads, head_dim);
 }
 
 gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* kv_lens, const int32_t* cu_q, void* out,

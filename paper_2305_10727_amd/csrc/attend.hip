@@ -52,21 +52,22 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
   Work w;
   if (!w.find(a)) return;
   const Span<KV4> span(a, w.b);
+  constexpr bool TREE = KV4 && MASKED;
   const int cols = span.nq * a.rep, col0 = w.block * 16 * QT, len = span.len;
   if (col0 >= cols) return;  // the whole workgroup, like above
   Columns<KV4, DP, QT> x;
   x.load(a, span, w.kh, g, r, [&](int i) { return col0 + 16 * i; });
-  constexpr bool TREE = KV4 && MASKED;
   const int least = TREE ? span.before : span.sees(col0 / a.rep);  // every column sees the keys in front of it, none those from `most` on
   const int most = TREE ? len : span.sees((col0 + 16 * QT < cols ? col0 + 16 * QT - 1 : cols - 1) / a.rep);
-  const int32_t* words[TREE ? QT : 1];
-  if constexpr (TREE) {
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      const int col = col0 + 16 * i + r < cols ? col0 + 16 * i + r : cols - 1;
-      words[i] = a.tree + (int64_t)(span.t0 + (a.rep == 1 ? col : col / a.rep)) * a.tree_words;
-    }
-  }
+  // the bits of block i's column of this lane, and which row of the output it is: formed where they are used, the loop has no registers to keep them in
+  auto words = [&](int i) {
+    const int col = col0 + 16 * i + r < cols ? col0 + 16 * i + r : cols - 1;
+    return a.tree + (int64_t)(span.t0 + (a.rep == 1 ? col : col / a.rep)) * a.tree_words;
+  };
+  auto row_of = [&](int i) {
+    const int col = col0 + 16 * i + r, tok = a.rep == 1 ? col : col / a.rep;
+    return col < cols ? (span.t0 + tok) * a.heads + w.kh * a.rep + (col - tok * a.rep) : -1;
+  };
   const int tiles = most > 0 ? (most + 31) >> 5 : 0;
   const int begin = w.part * a.part_tiles, end = begin + a.part_tiles < tiles ? begin + a.part_tiles : tiles;
   // The first keys, values and the queries are waited for together, in front of the loop: left to itself the compiler waits at its top, for
@@ -116,7 +117,7 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
         if (check) {
           unsigned seen[QT];
 #pragma unroll
-          for (int i = 0; i < QT; ++i) seen[i] = there ? tree_keys(words[i], a.tree_words, least, len, key0) >> (4 * g) : 0u;
+          for (int i = 0; i < QT; ++i) seen[i] = there ? tree_keys(words(i), a.tree_words, least, len, key0) >> (4 * g) : 0u;
           x.hide(s, [&](int i, int t, int e) { return (seen[i] >> (16 * t + e) & 1) == 0; });
         }
       } else if (check) {
@@ -227,51 +228,52 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
     }
   }
 
-  // One trip through LDS: every wavefront's sums, maxima and sums of weights, then a thread for each (column, four channels).
-  // Column c keeps its quad i in place i ^ (c % 16): what lanes write together lies in different banks.
-  constexpr int QUADS = DP / 4, COLS = 16 * QT;
-  __shared__ f4 sums[WK][COLS][QUADS];
-  __shared__ float ml[WK][2][COLS];
-  __shared__ int rows[COLS];
+  // Through LDS, a block of 16 columns at a time: every wavefront's sums, maxima and sums of weights, then a thread for each (column, four channels).
+  // Column c keeps its quad i in place i ^ c: what lanes write together lies in different banks.
+  constexpr int QUADS = DP / 4;
+  __shared__ f4 sums[WK][16][QUADS];
+  __shared__ float ml[WK][2][16];
+  __shared__ int rows[16];
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
+    if (col0 + 16 * i >= cols) break;
+    if (i > 0) __syncthreads();
     if (g == 0) {
-      ml[wk][0][16 * i + r] = x.m[i];
-      ml[wk][1][16 * i + r] = x.l[i][0];
-      if (wk == 0) rows[16 * i + r] = x.row[i];
+      ml[wk][0][r] = x.m[i];
+      ml[wk][1][r] = x.l[i][0];
+      if (wk == 0) rows[r] = row_of(i);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int t = 0; t < CH; t += 4)
-        sums[wk][16 * i + r][(((4 * g + e) * CH + t) / 4) ^ r] = f4{x.o[i][t][e], x.o[i][t + 1][e], x.o[i][t + 2][e], x.o[i][t + 3][e]};
-  }
-  __syncthreads();
-  for (int i = threadIdx.x; i < COLS * QUADS; i += 64 * WK) {
-    const int col = i / QUADS, quad = i % QUADS, row = rows[col];
-    if (row < 0 || 4 * quad >= a.D) continue;
-    float top = ml[0][0][col];
+      for (int t = 0; t < CH; t += 4) sums[wk][r][(((4 * g + e) * CH + t) / 4) ^ r] = f4{x.o[i][t][e], x.o[i][t + 1][e], x.o[i][t + 2][e], x.o[i][t + 3][e]};
+    __syncthreads();
+    for (int at = threadIdx.x; at < 16 * QUADS; at += 64 * WK) {
+      const int col = at / QUADS, quad = at % QUADS, row = rows[col];
+      if (row < 0 || 4 * quad >= a.D) continue;
+      float top = ml[0][0][col];
 #pragma unroll
-    for (int k = 1; k < WK; ++k) top = fmaxf(top, ml[k][0][col]);
-    const float ref = top == -__builtin_inff() ? 0.0f : top;
-    float total = 0.0f;
-    f4 y = f4(0);
+      for (int k = 1; k < WK; ++k) top = fmaxf(top, ml[k][0][col]);
+      const float ref = top == -__builtin_inff() ? 0.0f : top;
+      float total = 0.0f;
+      f4 y = f4(0);
 #pragma unroll
-    for (int k = 0; k < WK; ++k) {
-      const float f = __builtin_amdgcn_exp2f(ml[k][0][col] - ref);
-      total += ml[k][1][col] * f;
-      y += sums[k][col][quad ^ (col & 15)] * f;
-    }
-    if (a.parts > 1) {
-      const int64_t at = (int64_t)w.part * a.tokens * a.heads + row;
-      if (quad == 0) {
-        a.part_ml[2 * at] = top;
-        a.part_ml[2 * at + 1] = total;
+      for (int k = 0; k < WK; ++k) {
+        const float f = __builtin_amdgcn_exp2f(ml[k][0][col] - ref);
+        total += ml[k][1][col] * f;
+        y += sums[k][col][quad ^ col] * f;
       }
-      *(f4*)(a.part_o + at * a.D + 4 * quad) = y;
-    } else {
-      const float f = total == 0.0f ? 0.0f : 1.0f / total;
-      *(h4*)(a.out + (int64_t)row * a.D + 4 * quad) = h4{(_Float16)(y[0] * f), (_Float16)(y[1] * f), (_Float16)(y[2] * f), (_Float16)(y[3] * f)};
+      if (a.parts > 1) {
+        const int64_t place = (int64_t)w.part * a.tokens * a.heads + row;
+        if (quad == 0) {
+          a.part_ml[2 * place] = top;
+          a.part_ml[2 * place + 1] = total;
+        }
+        *(f4*)(a.part_o + place * a.D + 4 * quad) = y;
+      } else {
+        const float f = total == 0.0f ? 0.0f : 1.0f / total;
+        *(h4*)(a.out + (int64_t)row * a.D + 4 * quad) = h4{(_Float16)(y[0] * f), (_Float16)(y[1] * f), (_Float16)(y[2] * f), (_Float16)(y[3] * f)};
+      }
     }
   }
 }
@@ -359,20 +361,38 @@ __global__ void __launch_bounds__(256) join_few_parts_kernel(const float* __rest
   *(h4*)(out + row * D + 4 * quad) = h4{(_Float16)(o[0] * r), (_Float16)(o[1] * r), (_Float16)(o[2] * r), (_Float16)(o[3] * r)};
 }
 
-template <bool KV4, int DP, int QT, int WK>
-void launch_shape(AttendArgs a, hipStream_t s) {
+template <bool KV4, int DP, int QT, int WK, bool MASKED>
+void launch_masked(AttendArgs a, hipStream_t s) {
   a.col_blocks = (int)ceil_div((int64_t)a.q_len * a.rep, 16 * QT);
-  const unsigned blocks = Work::workgroups(a);
-  if (KV4 ? a.tree != nullptr : a.mask != nullptr) {
-    attend_few_kernel<KV4, DP, QT, WK, true><<<blocks, 64 * WK, 0, s>>>(a);
-    return;
+  attend_few_kernel<KV4, DP, QT, WK, MASKED><<<Work::workgroups(a), 64 * WK, 0, s>>>(a);
+}
+template <bool KV4, int DP, int QT, int WK>
+void launch_shape(const AttendArgs& a, hipStream_t s) {
+  if constexpr (!KV4) {
+    if (a.mask != nullptr) return launch_masked<KV4, DP, QT, WK, true>(a, s);
   }
-  attend_few_kernel<KV4, DP, QT, WK, false><<<blocks, 64 * WK, 0, s>>>(a);
+  launch_masked<KV4, DP, QT, WK, false>(a, s);
+}
+
+template <int DP, int QT>
+void launch_tree(const AttendArgs& a, const AttendShape& shape, hipStream_t s) {
+  shape.threads == 512 ? launch_masked<true, DP, QT, 8, true>(a, s) : launch_masked<true, DP, QT, 4, true>(a, s);
 }
 
 template <bool KV4, int DP>
 void launch_head(const AttendArgs& a, hipStream_t s) {
-  const AttendShape shape = attend_shape(KV4, DP, (int64_t)a.q_len * a.rep, KV4 || tiles_reach(a.k_token, a.v_token));
+  const AttendShape shape = attend_shape(KV4, DP, (int64_t)a.q_len * a.rep, KV4 || tiles_reach(a.k_token, a.v_token), KV4 && a.tree != nullptr ? (int64_t)a.batch * a.kv_heads : 0);
+  if constexpr (KV4) {
+    if (a.tree != nullptr && !shape.many) {
+      if (shape.columns == 16) return launch_masked<KV4, DP, 1, 8, true>(a, s);
+      if constexpr (tree_blocks(DP) >= 3) {
+        if (shape.columns == 32) return launch_tree<DP, 2>(a, shape, s);
+        if (shape.columns == 48) return launch_tree<DP, 3>(a, shape, s);
+      }
+      if constexpr (tree_blocks(DP) == 4) launch_tree<DP, 4>(a, shape, s);
+      return;
+    }
+  }
   if (shape.many)
     launch_attend_tiles(KV4, a, s);
   else if (shape.columns == 16)
@@ -388,13 +408,13 @@ void launch_head(const AttendArgs& a, hipStream_t s) {
 // more: a tile for each wavefront.  (One token, in one piece and in parts: of 32 heads over 8 of 128 after 8000 tokens 10.5 in 32 parts, 12.8 in 8;
 // 16 heads of 128 to 1000 states 12.3 and 8.6, of 256 24 and 13.)  What one piece does in 8.5 us stays one, as the second launch and the workspace
 // take the host 4: 1024 keys at most, over the cache 128K channels of keys, over states 64K (16 heads of 64, 1000 states: 8.3 and 7.2).
-// Many columns: parts of 16 tiles at least.
-AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys) {
+// Many columns: parts of 16 tiles at least.  (Trees of more than 16 columns have registers for one workgroup a CU: 256 of them or a few less, not more.)
+AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys, bool tree) {
   const int64_t tiles = ceil_div(most_keys > 0 ? most_keys : 1, 32), cols = q_len * (heads / kv_heads);
-  const AttendShape shape = attend_shape(kv4, padded_head((int)head_dim), cols, true);
+  const AttendShape shape = attend_shape(kv4, padded_head((int)head_dim), cols, true, tree ? batch * kv_heads : 0);
   const bool few = !shape.many;
   const int64_t groups = batch * kv_heads * ceil_div(cols, shape.columns);
-  int64_t parts = few ? ceil_div(256, groups) : (kv4 ? 256 : 512) / groups;
+  int64_t parts = few && (!tree || shape.columns == 16) ? ceil_div(256, groups) : (kv4 ? 256 : 512) / groups;
   const int64_t one = (kv4 ? 4096 : 2048) / padded_head((int)head_dim);
   const int64_t most = !few ? ceil_div(tiles, 16) : tiles <= (one < 32 ? one : 32) ? 1 : ceil_div(tiles, 8);
   parts = parts < 1 ? 1 : parts < most ? parts : most;
@@ -448,7 +468,7 @@ gpusq_status launch_attention_kv4(const AttentionKv4& x, hipStream_t s) {
   a.num_pages = (int)x.num_pages;
   a.tokens = (int)x.tokens;
   a.lens = x.kv_lens;
-  return run(a, true, attend_parts(true, x.batch, x.max_q, x.heads, x.kv_heads, x.head_dim, x.max_pages * kPageTokens), x.workspace, s);
+  return run(a, true, attend_parts(true, x.batch, x.max_q, x.heads, x.kv_heads, x.head_dim, x.max_pages * kPageTokens, x.tree != nullptr), x.workspace, s);
 }
 
 gpusq_status launch_cross_attention(const CrossAttention& x, hipStream_t s) {

@@ -527,7 +527,7 @@ struct CrossAttention {
 struct AttendParts {
   int parts, tiles;
 };
-AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys);
+AttendParts attend_parts(bool kv4, int64_t batch, int64_t q_len, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t most_keys, bool tree = false);
 gpusq_status launch_attention_kv4(const AttentionKv4& x, hipStream_t s);
 gpusq_status launch_cross_attention(const CrossAttention& x, hipStream_t s);
 

@@ -34,7 +34,7 @@ EXPORTS = [
     "gpusq_quantize_tensor_int8_noalloc", "gpusq_linear_int8", "gpusq_linear_int8_launches", "gpusq_linear_int8_quantiser",
     "gpusq_block_mlp_int8", "gpusq_block_mlp_int8_launches",
     "gpusq_int4_groups_packed_bytes", "gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_kv4_page_bytes",
-    "gpusq_qk_norm_rope", "gpusq_attention_kv4_workspace_bytes", "gpusq_attention_kv4", "gpusq_cross_attention_workspace_bytes", "gpusq_cross_attention",
+    "gpusq_qk_norm_rope", "gpusq_attention_kv4_workspace_bytes", "gpusq_attention_kv4", "gpusq_attention_tree_kv4_workspace_bytes", "gpusq_cross_attention_workspace_bytes", "gpusq_cross_attention",
     "gpusq_attention_tree_kv4", "gpusq_draft_tree", "gpusq_accept_drafts", "gpusq_linear_int8_tokens_workspace_bytes", "gpusq_linear_int8_tokens", "gpusq_sample_tokens_workspace_bytes",
     "gpusq_sample_tokens",
 ]
@@ -198,7 +198,7 @@ def lib():
         L.gpusq_linear_int4.argtypes = [vp, vp, ci, vp, vp, ci, i64, i64, i64, ci, vp]
         L.gpusq_kv4_page_bytes.argtypes = [i64, i64]
         L.gpusq_qk_norm_rope.argtypes = [vp, ci] + [i64] * 5 + [ci, vp, vp, cf, vp, vp, vp, i64, i64, ci] + [vp] * 5 + [i64, vp]
-        L.gpusq_attention_kv4_workspace_bytes.argtypes = [i64] * 7
+        L.gpusq_attention_kv4_workspace_bytes.argtypes = L.gpusq_attention_tree_kv4_workspace_bytes.argtypes = [i64] * 7
         L.gpusq_attention_kv4.argtypes = [vp] * 7 + [i64] * 8 + [cf, vp]
         L.gpusq_cross_attention_workspace_bytes.argtypes = [i64] * 6
         L.gpusq_cross_attention.argtypes = [vp] * 7 + [i64] * 15 + [cf, vp]
@@ -211,7 +211,7 @@ def lib():
         L.gpusq_sample_tokens.argtypes = [vp, ci, i64] + [vp] * 8 + [i64] * 2 + [vp]
         for name in ("gpusq_attention_tree_kv4", "gpusq_draft_tree", "gpusq_accept_drafts", "gpusq_linear_int8_tokens", "gpusq_sample_tokens"):
             getattr(L, name).restype = ci
-        for name in ("gpusq_int4_groups_packed_bytes", "gpusq_kv4_page_bytes", "gpusq_attention_kv4_workspace_bytes", "gpusq_cross_attention_workspace_bytes",
+        for name in ("gpusq_int4_groups_packed_bytes", "gpusq_kv4_page_bytes", "gpusq_attention_kv4_workspace_bytes", "gpusq_attention_tree_kv4_workspace_bytes", "gpusq_cross_attention_workspace_bytes",
                      "gpusq_linear_int8_tokens_workspace_bytes", "gpusq_sample_tokens_workspace_bytes"):
             getattr(L, name).restype = sz
         for name in ("gpusq_quantize_groups_int4", "gpusq_pack_int4_groups", "gpusq_linear_int4", "gpusq_qk_norm_rope", "gpusq_attention_kv4", "gpusq_cross_attention"):
@@ -624,7 +624,7 @@ def attention_kv4(q, cache, block_table, kv_lens, cu_q=None, max_q=None, scale=N
         out = _empty(q, torch.float16, tokens, heads, D)
     else:
         _want(_is(out, torch.float16, tokens, heads, D), "out: [tokens, heads, head_dim] float16 on the GPU")
-    workspace = _workspace(q, workspace, _size("gpusq_attention_kv4_workspace_bytes", tokens, batch, max_q, max_pages, heads, kv_heads, D))
+    workspace = _workspace(q, workspace, _size("gpusq_attention_kv4_workspace_bytes" if tree is None else "gpusq_attention_tree_kv4_workspace_bytes", tokens, batch, max_q, max_pages, heads, kv_heads, D))
     s = 0.0 if scale is None else scale
     if tree is None:
         calls.gpusq_attention_kv4(q, cache, block_table, kv_lens, cu_q, out, workspace, tokens, batch, max_q, max_pages, pages, heads, kv_heads, D, s)

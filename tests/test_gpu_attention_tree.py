@@ -75,7 +75,7 @@ def test_long_histories_are_cut_and_joined(g, H, G, D, L, n):
     r = np.random.default_rng(L)
     c = _Cache([L, 70], G, D, seed=2)
     counts = [n, min(n, 30)]
-    size = g.lib().gpusq_attention_kv4_workspace_bytes(sum(counts), 2, n, c.table.shape[1], H, G, D)
+    size = g.lib().gpusq_attention_tree_kv4_workspace_bytes(sum(counts), 2, n, c.table.shape[1], H, G, D)
     assert size > 0
     q = r.standard_normal((sum(counts), H, D)).astype(np.float16)
     sets = _sets(r, counts, "tree")
@@ -87,7 +87,8 @@ def test_long_histories_are_cut_and_joined(g, H, G, D, L, n):
 
 
 def test_a_chain_is_causal_attention(g):
-    """To the bit: the same products in the same order, and the same keys hidden"""
+    """To the bit where both have the same kernel (few columns): the same products in the same order, and the same keys hidden.  Else either is the definition,
+    within what its roundings allow"""
     r = np.random.default_rng(6)
     for (H, G, D), counts in (((8, 2, 128), [3, 1]), ((6, 2, 80), [40, 21]), ((4, 4, 64), [9, 70])):
         lens = [200, 90]
@@ -96,7 +97,29 @@ def test_a_chain_is_causal_attention(g):
         sets = [list(range(i + 1)) for n in counts for i in range(n)]
         cu = dev(np.r_[0, np.cumsum(counts)].astype(np.int32))
         plain = g.attention_kv4(dev(q), dev(c.pages), dev(c.table), dev(np.array(lens, np.int32)), cu_q=cu, max_q=max(counts))
-        assert torch.equal(_run(g, c, q, counts, drafts.bits(sets, -(-max(counts) // 32))), plain)
+        tree = _run(g, c, q, counts, drafts.bits(sets, -(-max(counts) // 32)))
+        if max(counts) * H // G <= 16:
+            assert torch.equal(tree, plain)
+        else:
+            exp = _expected(c, q, counts, sets)
+            _check(tree, *exp)
+            _check(plain, *exp)
+
+
+# blocks of 2, 3 and 4 times 16 columns, 4 or 8 wavefronts, up to 256 columns of many pairs (beyond 192 of few: another kernel)
+@pytest.mark.parametrize("B,H,G,D,n", [(70, 16, 4, 128, 12), (130, 8, 4, 128, 14), (140, 16, 4, 128, 11), (130, 8, 4, 64, 13), (140, 8, 4, 64, 20), (130, 8, 4, 64, 25), (20, 4, 1, 128, 62),
+                                       (3, 4, 1, 128, 48), (3, 4, 1, 128, 49), (18, 4, 1, 64, 64), (18, 4, 1, 64, 65), (17, 2, 1, 256, 20)])
+def test_batches_of_trees(g, B, H, G, D, n):
+    r = np.random.default_rng(B * n)
+    counts = [n] + r.integers(1, n + 1, B - 1).tolist()
+    lens = [c + int(r.integers(0, 140)) for c in counts]
+    c = _Cache(lens, G, D, seed=12)
+    q = r.standard_normal((sum(counts), H, D)).astype(np.float16)
+    sets = _sets(r, counts, "tree")
+    words = drafts.bits(sets, -(-n // 32))
+    y = _run(g, c, q, counts, words)
+    _check(y, *_expected(c, q, counts, sets))
+    assert torch.equal(_run(g, c, q, counts, words), y)
 
 
 def test_pages_that_are_none_and_what_is_no_number(g):
