@@ -11,8 +11,10 @@
 // A row is read three times: for its greatest logit; for a histogram of the logits' distances from it, in 2048 bins of 28 / 2048 of the temperature, from
 // which the bin of the k-th token and the bins between which the p-th share ends are known; for the sums, and the tokens of those bins, which are sorted
 // and decide.  A wavefront sums a stretch of the vocabulary; the token lies in the stretch that passes the random share, which is looked at once more.
-// What bounds it is the instructions of the weights, some thirty a token and pass, and of the histogram's atomics in LDS.  So few rows are cut into parts,
-// a workgroup each, in a launch for each reading and one that decides.
+// What bounds it is the instructions of the weights, 22 a token and pass, and of the histogram's atomics in LDS; the first reading is memory's.  So few rows
+// are cut into parts, a workgroup each, in a launch for each reading and one that decides.  256 rows of 131072 fp32 logits (134 MB, 27 us at a copy's
+// rate): 65 us without a cut, 88 with top-k, 114 with top-p, 113 with all; 256 of 32000 fp16 20, 32, 40, 41; one of 32000 17, 23, 34, 28, of 131072 19,
+// 39, 46, 44; greedy ones, of one reading and a launch, 9.
 #include "common.h"
 #include "sample_plan.h"
 
@@ -118,7 +120,7 @@ struct Block {
 
 struct Shared {
   Block block;
-  double table[64];  // 2^(j / 64)
+  double table[128];  // 2^(j / 128)
   u64 masses[kBins];
   unsigned counts[kBins];
   u64 list[kListed];
@@ -126,27 +128,28 @@ struct Shared {
   unsigned listed, of_k_bin;
 };
 
-// exp(y) is 2^(k / 64), from a table, times 2^(f / 64), |f| at most 1/2: k and f of 64 (x - max) / (T ln 2) in 64 bits, 2^(f / 64) - 1, at most
-// 0.0055, by a polynomial in 32 bits: off by 2^-31 of the weight.
+// exp(y) is 2^e times 2^(j / 128), from a table, times 2^(f / 128), 0 <= f < 1, of one fused step: 128 y / ln 2 in whole numbers of 2^-24 stands in the last
+// places of a number of 64 bits, f in 24 of them, j in the next 7, e behind.  2^(f / 128) - 1, at most 0.0054, is three terms of its series in 32 bits: off by
+// 2^-31 of the weight, by nothing for the greatest.
 struct Weights {
   float top, limit, scale;  // the greatest logit; the distance of 2^-40 from it; bins of a distance
-  double steps;             // 64 / (T ln 2)
+  double steps;             // 128 / (T ln 2)
   const double* table;
   __device__ __forceinline__ Weights(float top_, float temperature, const double* table_)
-      : top(top_), limit(fminf(27.725887f * temperature, 3.4028235e38f)), scale(kBinsOfUnit / temperature), steps(92.332482616893657 / (double)temperature), table(table_) {}
+      : top(top_), limit(fminf(27.725887f * temperature, 3.4028235e38f)), scale(kBinsOfUnit / temperature), steps(184.664965233787314 / (double)temperature), table(table_) {}
   // (not so for what is no number, or -infinity)
   __device__ __forceinline__ bool has(float x) const { return top - x <= limit; }
-  // of a logit that has one: whole numbers of 2^-44
-  __device__ __forceinline__ u64 of(float x) const {
-    const double t = ((double)x - (double)top) * steps, shifted = t + 0x1.8p52;
-    const float f = (float)(t - (shifted - 0x1.8p52));
-    const float q = f * __builtin_fmaf(f, __builtin_fmaf(f, 0x1.c6b08ep-23f, 0x1.ebfbep-15f), 0x1.62e430p-7f);
-    const int k = (int)(unsigned)__double_as_longlong(shifted);
-    const double c = table[k & 63], w = __builtin_fma(c, (double)q, c);
-    const double scaled = __hiloint2double(__double2hiint(w) + (int)((unsigned)(k & ~63) << 14), __double2loint(w));  // times 2^(k / 64 whole)
-    const double sum = scaled + 256.0;  // the last place is 2^-44
-    return (u64)(unsigned)(__double2hiint(sum) - 0x40700000) << 32 | (unsigned)__double2loint(sum);
+  // of a logit that has one (of another any number): whole numbers of 2^-44, and kNone
+  __device__ __forceinline__ u64 beyond_none(float x) const {
+    const double s = __builtin_fma((double)x - (double)top, steps, 0x1.8p28);  // the last place is 2^-24
+    const unsigned lo = (unsigned)__double2loint(s), hi = (unsigned)__double2hiint(s);
+    const float f = (float)(lo & 0xFFFFFFu), q = f * __builtin_fmaf(f, __builtin_fmaf(f, 0x1.c6b08ep-98f, 0x1.ebfbep-65f), 0x1.62e430p-32f);
+    const double c = table[lo >> 24 & 127], w = __builtin_fma(c, (double)q, c);
+    const double scaled = __hiloint2double(__double2hiint(w) + (int)(__builtin_amdgcn_alignbit(hi, lo, 31) << 20), __double2loint(w));  // times 2^e
+    return (u64)__double_as_longlong(scaled + 256.0);  // the last place is 2^-44
   }
+  static constexpr u64 kNone = 0x4070000000000000ull;  // 256 in 64 bits
+  __device__ __forceinline__ u64 of(float x) const { return beyond_none(x) - kNone; }
   __device__ __forceinline__ u64 operator()(float x) const { return has(x) ? of(x) : 0; }
   // ... a logit's bin, in the logits' order
   __device__ __forceinline__ float distance(float x) const { return (top - x) * scale; }
@@ -173,6 +176,24 @@ struct Row {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) r[e] = i + e >= 0 && i + e < V ? x[i + e] : (T)-__builtin_inff();
     return r;
+  }
+  // For much work a value: each(values, index of the first) a vector at a time, the next two on their way
+  template <class Each>
+  __device__ __forceinline__ void step(Each each) const {
+    const int end = begin + per_wave < vecs ? begin + per_wave : vecs;
+    int v = begin + (threadIdx.x & 63);
+    if (v >= end) return;
+    vec now = load(v), next = load(v + 64 < end ? v + 64 : v);
+#pragma unroll 1
+    for (; v < end; v += 64) {
+      const vec later = load(v + 128 < end ? v + 128 : v);
+      float x[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[e] = (float)now[e];
+      each(x, v * VEC - off);
+      now = next;
+      next = later;
+    }
   }
   template <class Each>
   __device__ __forceinline__ void walk(Each each) const {
@@ -226,7 +247,7 @@ struct Asked {
 
 __device__ __forceinline__ void clear(Shared& sh) {
   const int tid = threadIdx.x;
-  if (tid < 64) sh.table[tid] = exp2(tid * (1.0 / 64));
+  if (tid < 128) sh.table[tid] = exp2(tid * (1.0 / 128));
   for (int i = tid; i < kBins; i += kThreads) {
     sh.masses[i] = 0;
     sh.counts[i] = 0;
@@ -273,23 +294,27 @@ __device__ __forceinline__ int bins_asked(Shared& sh, const Asked& asked, const 
 
 template <typename T>
 __device__ __forceinline__ void histogram(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, int behind) {
+  constexpr int VEC = Row<T>::VEC;
   const float most = (float)behind;
-  if (asked.k != 0 && asked.shares) {
-    row.walk([&](float x, int) {
-      const float d = weight.distance(x);
-      if (d < most) {
-        atomicAdd(&sh.counts[(int)d], 1u);
-        if (weight.has(x)) atomicAdd(&sh.masses[(int)d], weight.of(x));
+  if (asked.k != 0) {
+    row.step([&](const float (&x)[VEC], int) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float d = weight.distance(x[e]);
+        if (d < most) {
+          atomicAdd(&sh.counts[(int)d], 1u);
+          if (asked.shares && weight.has(x[e])) atomicAdd(&sh.masses[(int)d], weight.of(x[e]));
+        }
       }
     });
-  } else if (asked.k != 0) {
-    row.walk([&](float x, int) {
-      const float d = weight.distance(x);
-      if (d < most) atomicAdd(&sh.counts[(int)d], 1u);
-    });
   } else {
-    row.walk([&](float x, int) {
-      if (weight.has(x)) atomicAdd(&sh.masses[(int)weight.distance(x)], weight.of(x));
+    row.step([&](const float (&x)[VEC], int) {
+      u64 w[VEC];  // (formed side by side, without a branch)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) w[e] = weight.of(x[e]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (weight.has(x[e])) atomicAdd(&sh.masses[(int)weight.distance(x[e])], w[e]);
     });
   }
 }
@@ -336,25 +361,59 @@ __device__ __forceinline__ Zones zones_of(Shared& sh, const Asked& asked) {
 // The sum of the wavefront's stretch, of the tokens that are sure; the tokens of the list's bins to the list
 template <typename T>
 __device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, const Zones& z) {
+  constexpr int VEC = Row<T>::VEC;
   u64 sum = 0;
   const u64 least = asked.least;
-  if (z.sure == kBins) {  // no cut
-    row.walk([&](float x, int) {
-      const u64 w = weight(x);
-      sum += w >= least ? w : 0;
-    });
+  const float sure = (float)z.sure, last = (float)((z.k_bin < kBins ? z.k_bin : z.z1) + 1);
+  auto list = [&](float x, int bin, int i) {
+    if (bin == z.k_bin) atomicAdd(&sh.of_k_bin, 1u);
+    const unsigned at = atomicAdd(&sh.listed, 1u);
+    if (at < kListed) sh.list[at] = place_of(x, i);
+  };
+  if (z.k_bin == kBins) {  // Most tokens weigh: their weights side by side, without a branch, and what each has too much is taken off at the end
+    const u64 enough = least + Weights::kNone;
+    u64 none = 0;
+    if (z.sure == kBins) {
+      row.step([&](const float (&x)[VEC], int) {
+        none += VEC * Weights::kNone;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const u64 w = weight.beyond_none(x[e]);
+          sum += (int)weight.has(x[e]) & (int)(w >= enough) ? w : Weights::kNone;
+        }
+      });
+    } else {
+      row.step([&](const float (&x)[VEC], int i0) {
+        none += VEC * Weights::kNone;
+        bool some = false;
+        float d[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          d[e] = weight.distance(x[e]);
+          const u64 w = weight.beyond_none(x[e]);
+          sum += (int)(d[e] < sure) & (int)(w >= enough) ? w : Weights::kNone;
+          some |= (int)(d[e] >= sure) & (int)(d[e] < last);
+        }
+        if (some) {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e)
+            if (d[e] >= sure && d[e] < last && z.lists((int)d[e])) list(x[e], (int)d[e], i0 + e);
+        }
+      });
+    }
+    sum -= none;
   } else {
-    const float sure = (float)z.sure, last = (float)((z.k_bin < kBins ? z.k_bin : z.z1) + 1);
-    row.walk([&](float x, int i) {
-      const float d = weight.distance(x);
-      if (d < last) {
-        if (d < sure) {
-          const u64 w = weight(x);
-          sum += w >= least ? w : 0;
-        } else if (z.lists((int)d)) {
-          if ((int)d == z.k_bin) atomicAdd(&sh.of_k_bin, 1u);
-          const unsigned at = atomicAdd(&sh.listed, 1u);
-          if (at < kListed) sh.list[at] = place_of(x, i);
+    row.step([&](const float (&x)[VEC], int i0) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float d = weight.distance(x[e]);
+        if (d < last) {
+          if (d < sure) {
+            const u64 w = weight(x[e]);
+            sum += w >= least ? w : 0;
+          } else if (z.lists((int)d)) {
+            list(x[e], (int)d, i0 + e);
+          }
         }
       }
     });
@@ -503,7 +562,7 @@ __device__ __forceinline__ void answer(Shared& sh, const SampleArgs& a, int row_
   const int tid = threadIdx.x, each = (vecs + kThreads - 1) / kThreads, v0 = first + tid * each, most = first + vecs < row.vecs ? first + vecs : row.vecs;
   const int v1 = v0 + each < most ? v0 + each : most;
   u64 own = 0;
-#pragma unroll 4
+#pragma unroll 1
   for (int v = v0; v < v1; ++v) {
     const auto x = row.load(v);
 #pragma unroll
@@ -515,6 +574,7 @@ __device__ __forceinline__ void answer(Shared& sh, const SampleArgs& a, int row_
   int token = -1;
   u64 w = 0;
   bool on = true;
+#pragma unroll 1
   for (int v = v0; v < v1; ++v) {
     const auto x = row.load(v);
 #pragma unroll
