@@ -84,14 +84,15 @@ __global__ void __launch_bounds__(256) draft_tree_kernel(const DraftArgs a, cons
 
 // ---- the kept branch --------------------------------------------------------------------------------------------------------------------
 // From node 0 on to the first child whose draft is what was drawn behind its parent.  Every workgroup walks by itself, one wavefront with 64 nodes at
-// a time: the first of a sequence's writes the results, the others move a head's tokens in a layer's cache each.
-constexpr int kUnits = 8;  // 16-bit units of a cache that a thread has on its way
+// a time: the first of a sequence's writes the results, the others move some heads' tokens in a layer's cache each.  (16 trees, 24 layers of 4 heads: all of a
+// layer's heads in a workgroup 10.2 us, a workgroup a head 13.6.)
 __global__ void __launch_bounds__(256) accept_drafts_kernel(const DraftArgs a, const int32_t* __restrict__ drafted, const int32_t* __restrict__ sampled,
                                                             const int32_t* __restrict__ parents, const int32_t* __restrict__ table, int max_pages,
                                                             int32_t* __restrict__ path, int32_t* __restrict__ accepted, int32_t* __restrict__ answers,
-                                                            int32_t* __restrict__ new_lens, const CacheList caches, int num_pages, int kv_heads, int DP) {
+                                                            int32_t* __restrict__ new_lens, const CacheList caches, int num_pages, int kv_heads, int heads, int DP) {
   __shared__ int parent[kMostDrafts], draft[kMostDrafts], drawn[kMostDrafts], kept[kMostDrafts], count;
   __shared__ int64_t place[kMostDrafts];  // of the kept node and of where it goes: token of a page, -1 where there is none
+  __shared__ int pages[kMostDrafts / kPageTokens + 1];  // of the new tokens
   const int b = blockIdx.x, tid = threadIdx.x;
   const Drafts d(a, b);
   const int n = d.nodes;
@@ -100,6 +101,8 @@ __global__ void __launch_bounds__(256) accept_drafts_kernel(const DraftArgs a, c
     draft[i] = drafted[d.t0 + i];
     drawn[i] = sampled[d.t0 + i];
   }
+  const int first_page = d.before >> 6;  // (in front of the sequence: negative, and no page)
+  if (blockIdx.y > 0 && tid <= kMostDrafts / kPageTokens) pages[tid] = first_page + tid >= 0 && first_page + tid < max_pages ? table[(int64_t)b * max_pages + first_page + tid] : -1;
   __syncthreads();
   if (tid < 64) {
     int at = 0, len = 0;
@@ -134,12 +137,13 @@ __global__ void __launch_bounds__(256) accept_drafts_kernel(const DraftArgs a, c
     for (int i = tid; i < a.max_q; i += 256) path[(int64_t)b * a.max_q + i] = i < len ? kept[i] : -1;
     return;
   }
-  const int unit_of_head = blockIdx.y - 1, layer = unit_of_head / kv_heads, head = unit_of_head - layer * kv_heads;
+  const int groups = (kv_heads + heads - 1) / heads, group = blockIdx.y - 1, layer = group / groups, head0 = (group - layer * groups) * heads;
+  const int own = kv_heads - head0 < heads ? kv_heads - head0 : heads;
   uint8_t* cache = (uint8_t*)caches.of[layer];
   // (32 bits each: pages and tokens of them, together 31)
   for (int i = tid; i < len; i += 256) {
     auto slot = [&](int at) {
-      const int page = page_of(table + (int64_t)b * max_pages, max_pages, at);
+      const int page = at >= 0 ? pages[(at >> 6) - first_page] : -1;
       return page >= 0 && page < num_pages ? page * kPageTokens + (at & 63) : -1;
     };
     const int from = slot(d.before + kept[i]), to = slot(d.before + i);
@@ -147,8 +151,8 @@ __global__ void __launch_bounds__(256) accept_drafts_kernel(const DraftArgs a, c
   }
   __syncthreads();
   // A token of a head is DP / 4 units of key codes, J of key scales, DP / 4 of value codes, J of value scales.
-  const int J = DP / 32, quads = DP / 4, per = 2 * (quads + J);
-  auto unit_at = [&](int slot, int u) {  // in 16-bit units from the cache's beginning
+  const int J = DP / 32, quads = DP / 4, per = token_units(DP);
+  auto unit_at = [&](int slot, int head, int u) {  // in 16-bit units from the cache's beginning
     const int t = slot & 63;
     const int64_t page = ((int64_t)(slot >> 6) * kv_heads + head) * (page_bytes(DP) / 2);
     if (u < quads) return page + t * quads + u;
@@ -165,19 +169,23 @@ __global__ void __launch_bounds__(256) accept_drafts_kernel(const DraftArgs a, c
   uint16_t* units = (uint16_t*)cache;
   // Some tokens at a time, all of them read before any is written; a token moves to the front or stays, so what is written lies in front of what
   // the later ones are read from.
-  const int chunk = 256 * kUnits / per;
+  const int of_token = per * own, chunk = kUnitsOfWorkgroup / of_token;
   for (int i0 = 0; i0 < len; i0 += chunk) {
-    const int total = (len - i0 < chunk ? len - i0 : chunk) * per;
+    const int total = (len - i0 < chunk ? len - i0 : chunk) * of_token;
+    constexpr int kUnits = kUnitsOfWorkgroup / 256;
     uint16_t v[kUnits];
     int64_t to[kUnits];
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
-      const int x = tid + 256 * j, i = x / per, u = x - i * per;
+      const int x = tid + 256 * j;
       to[j] = -1;
       v[j] = 0;
-      if (x < total && place[i0 + i] >= 0) {
-        to[j] = unit_at((int)(unsigned)place[i0 + i], u);
-        v[j] = units[unit_at((int)(place[i0 + i] >> 32), u)];
+      if (x >= total) continue;
+      const int i = x / of_token, rest = x - i * of_token, head = rest / per, u = rest - head * per;
+      const int64_t p = place[i0 + i];
+      if (p >= 0) {
+        to[j] = unit_at((int)(unsigned)p, head0 + head, u);
+        v[j] = units[unit_at((int)(p >> 32), head0 + head, u)];
       }
     }
     __syncthreads();
@@ -200,15 +208,16 @@ gpusq_status launch_draft_tree(const DraftArgs& a, const int32_t* parents, const
 gpusq_status launch_accept_drafts(const DraftArgs& a, const int32_t* drafted, const int32_t* sampled, const int32_t* parents, const int32_t* table, int64_t max_pages,
                                   int32_t* path, int32_t* accepted, int32_t* answers, int32_t* new_lens, void* const* caches, int64_t layers, int64_t num_pages,
                                   int64_t kv_heads, int64_t D, hipStream_t s) {
-  const int64_t most = caches_of_launch(a.batch, kv_heads);
+  const int DP = padded_head((int)D), heads = heads_of_workgroup(kv_heads, DP);
+  const int64_t groups = ceil_div(kv_heads, heads), most = caches_of_launch(a.batch, groups);
   int64_t from = 0;
   do {  // (at least once: the results)
     CacheList list{};
     const int64_t n = layers - from < most ? layers - from : most;
     for (int64_t i = 0; i < n; ++i) list.of[i] = caches[from + i];
-    const dim3 grid((unsigned)a.batch, (unsigned)(1 + n * kv_heads));
+    const dim3 grid((unsigned)a.batch, (unsigned)(1 + n * groups));
     accept_drafts_kernel<<<grid, 256, 0, s>>>(a, drafted, sampled, parents, table, (int)max_pages, path, accepted, answers, new_lens, list, (int)num_pages, (int)kv_heads,
-                                              padded_head((int)D));
+                                              heads, DP);
     const gpusq_status st = check_launch();
     if (st != GPUSQ_OK) return st;
     from += most;

@@ -293,7 +293,33 @@ PyObject* strides(PyObject*, PyObject* o) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef g_methods[] = {{"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, "empty(like, dtype, *sizes)"},
+// addresses(tensors): (bytes, where they lie) of the addresses of tensors on one GPU, contiguous and all of the first one's type and sizes; None: they are not
+PyObject* addresses(PyObject*, PyObject* given) {
+  HANDLE_TH_ERRORS
+  PyObject* all = PySequence_Fast(given, "addresses(tensors): a sequence");
+  if (!all) return nullptr;
+  const Py_ssize_t n = PySequence_Fast_GET_SIZE(all);
+  PyObject* bytes = PyBytes_FromStringAndSize(nullptr, n * (Py_ssize_t)sizeof(void*));
+  bool yes = bytes != nullptr;
+  for (Py_ssize_t i = 0; i < n && yes; ++i) {
+    PyObject* o = PySequence_Fast_GET_ITEM(all, i);
+    yes = THPVariable_Check(o);
+    if (!yes) break;
+    const at::Tensor &t = THPVariable_Unpack(o), &first = THPVariable_Unpack(PySequence_Fast_GET_ITEM(all, 0));
+    yes = t.is_cuda() && t.is_contiguous() && t.scalar_type() == first.scalar_type() && t.sizes() == first.sizes() && t.get_device() == first.get_device();
+    const void* p = yes ? t.data_ptr() : nullptr;
+    memcpy(PyBytes_AS_STRING(bytes) + i * sizeof(void*), &p, sizeof(void*));
+  }
+  Py_DECREF(all);
+  if (!bytes) return nullptr;
+  if (yes) return Py_BuildValue("Nn", bytes, (Py_ssize_t)(uintptr_t)PyBytes_AS_STRING(bytes));
+  Py_DECREF(bytes);
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef g_methods[] = {{"addresses", (PyCFunction)addresses, METH_O, "addresses(tensors)"},
+                           {"empty", (PyCFunction)(void (*)(void))empty, METH_FASTCALL, "empty(like, dtype, *sizes)"},
                            {"is_tensor", (PyCFunction)(void (*)(void))is_tensor, METH_FASTCALL, "is_tensor(t, dtype, *sizes)"},
                            {"strides", (PyCFunction)strides, METH_O, "strides(t)"},
                            {"setup", setup, METH_VARARGS, "setup(get_device, get_stream, on_error)"}, {nullptr, nullptr, 0, nullptr}};

@@ -700,14 +700,13 @@ def accept_drafts(drafted, sampled, parents, kv_lens, cu_q=None, max_q=None, cac
         pages, kv_heads, nbytes = caches[0].shape
         head_dim = nbytes // 72  # (of the padded one: the places are the same)
         _want(nbytes == _size("gpusq_kv4_page_bytes", 1, head_dim), "caches: pages of kv4_cache")
-        device = caches[0].get_device()
-        for c in caches:
-            _want(_is(c, torch.uint8, pages, kv_heads, nbytes) and c.is_contiguous() and c.get_device() == device, "caches: contiguous, of one size, on one GPU")
-        _want(device == torch.cuda.current_device(), "caches: on the current device")
-        addresses = (ctypes.c_void_p * layers)(*[c.data_ptr() for c in caches])
+        from . import _fastcall
+        addresses = _fastcall.addresses(caches)  # (kept until the call is made)
+        _want(addresses is not None, "caches: contiguous, of one size, on one GPU")
+        _want(caches[0].get_device() == torch.cuda.current_device(), "caches: on the current device")
     path = _empty(parents, i32, batch, max(1, max_q))
     accepted, answers, new_lens = _empty(parents, i32, batch), _empty(parents, i32, batch), _empty(parents, i32, batch)
-    calls.gpusq_accept_drafts(drafted, sampled, parents, kv_lens, cu_q, block_table, None if addresses is None else ctypes.addressof(addresses), layers, path, accepted,
+    calls.gpusq_accept_drafts(drafted, sampled, parents, kv_lens, cu_q, block_table, None if addresses is None else addresses[1], layers, path, accepted,
                               answers, new_lens, tokens, batch, max_q, max_pages, pages, kv_heads, head_dim)
     return path, accepted, answers, new_lens
 

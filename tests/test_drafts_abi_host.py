@@ -1,10 +1,29 @@
 """Host-only checks of the operators that answer with drafted tokens: arguments that are refused before anything is launched, sizes of buffers.  No kernel is
 launched here."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 
-from test_decoder_abi_host import ERR_ALIGN, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ODD, P, _refuses, g  # noqa: F401
+from test_decoder_abi_host import ERR_ALIGN, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ODD, P, ROOT, _refuses, g  # noqa: F401
+
+
+def test_plans(tmp_path):
+    """How products, rows of logits and caches are cut, walked on the host with the code the kernels read it with (drafts_plan_walk.cpp)"""
+    exe = str(tmp_path / "walk")
+    build = subprocess.run(["g++", "-O2", "-std=c++17", "-Wall", "-Werror", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                            "-I", os.path.join(ROOT, "paper_2305_10727_amd", "csrc"), os.path.join(ROOT, "tests", "drafts_plan_walk.cpp"), "-o", exe],
+                           capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr
+    run = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert run.returncode == 0 and run.stdout == "ok\n", run.stdout
+
+
+def test_a_trees_workspace(g):
+    """Of sizes that the call would refuse: 0"""
+    size = g.lib().gpusq_attention_tree_kv4_workspace_bytes
+    assert size(63, 1, 63, 1025, 32, 8, 128) > 0 == size(63, 1, 64, 1025, 32, 8, 128) == size(63, 1, 63, 2**25 - 1, 32, 8, 128) == size(63, 1, 63, 1025, 31, 8, 128)
 
 
 def test_attention_tree_kv4(g):

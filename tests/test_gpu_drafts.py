@@ -117,6 +117,12 @@ def test_accept_drafts(g, D, G, layers, counts, kinds, depth):
     assert all(np.array_equal(host(a), b) for a, b in zip(again, got))
 
 
+# heads of one layer for more than one workgroup
+@pytest.mark.parametrize("D,G", [(256, 17), (64, 60), (128, 29)])
+def test_accept_drafts_of_many_heads(g, D, G):
+    test_accept_drafts(g, D, G, 2, [9, 70], ("tree", "comb"), 200)
+
+
 def test_accept_drafts_where_places_are_missing(g):
     """No page in the table, a page that the cache has not, a history that is shorter than the new tokens, a drawn token that is none, more nodes than max_q"""
     r = np.random.default_rng(8)
