@@ -231,10 +231,16 @@ struct Asked {
   bool shares;  // whether a share of the weight is cut
   double p;
   u64 least;  // weight that min_p asks for
+  float random;
   __device__ __forceinline__ Asked(const SampleArgs& a, int row) {
-    temperature = a.temperature != nullptr ? a.temperature[row] : 1.0f;
-    const int k_given = a.top_k != nullptr ? a.top_k[row] : 0;
-    const float p_given = a.top_p != nullptr ? a.top_p[row] : 1.0f, m = a.min_p != nullptr ? a.min_p[row] : 0.0f;
+    temperature = 1.0f;
+    int k_given = 0;
+    float p_given = 1.0f, m = 0.0f;
+    random = a.random[row];  // (all of them requested before one is looked at)
+    if (a.temperature != nullptr) temperature = a.temperature[row];
+    if (a.top_k != nullptr) k_given = a.top_k[row];
+    if (a.top_p != nullptr) p_given = a.top_p[row];
+    if (a.min_p != nullptr) m = a.min_p[row];
     k = k_given > 0 && k_given < a.V ? k_given : 0;
     shares = p_given < 1.0f;
     p = p_given > 0.0f ? (double)p_given : 0.0;
@@ -245,12 +251,15 @@ struct Asked {
   __device__ __forceinline__ float heat() const { return fmaxf(temperature, 0x1p-100f); }
 };
 
-__device__ __forceinline__ void clear(Shared& sh) {
+__device__ __forceinline__ void clear(Shared& sh, bool histogram) {
   const int tid = threadIdx.x;
   if (tid < 128) sh.table[tid] = exp2(tid * (1.0 / 128));
-  for (int i = tid; i < kBins; i += kThreads) {
-    sh.masses[i] = 0;
-    sh.counts[i] = 0;
+  if (histogram) {
+#pragma unroll
+    for (int i = 0; i < kBins; i += kThreads) {
+      sh.masses[tid + i] = 0;
+      sh.counts[tid + i] = 0;
+    }
   }
   if (tid == 0) sh.listed = sh.of_k_bin = 0;
   __syncthreads();
@@ -561,34 +570,38 @@ __device__ __forceinline__ void answer(Shared& sh, const SampleArgs& a, int row_
   constexpr int VEC = Row<T>::VEC;
   const int tid = threadIdx.x, each = (vecs + kThreads - 1) / kThreads, v0 = first + tid * each, most = first + vecs < row.vecs ? first + vecs : row.vecs;
   const int v1 = v0 + each < most ? v0 + each : most;
-  u64 own = 0;
-#pragma unroll 1
-  for (int v = v0; v < v1; ++v) {
+  u64 own = 0, w[VEC];
+  auto look = [&](int v) {
     const auto x = row.load(v);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) own += has((float)x[e], v * VEC - row.off + e);
+    for (int e = 0; e < VEC; ++e) w[e] = has((float)x[e], v * VEC - row.off + e);
+  };
+#pragma unroll 1
+  for (int v = v0; v < v1; ++v) {
+    look(v);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) own += w[e];
   }
   before += sh.block.before(own);
   const int who = sh.block.first(own != 0 && !((double)(before + own) <= share), own != 0);
   if (tid != who) return;
   int token = -1;
-  u64 w = 0;
+  u64 of_token = 0;
   bool on = true;
 #pragma unroll 1
   for (int v = v0; v < v1; ++v) {
-    const auto x = row.load(v);
+    if (each > 1) look(v);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      const int i = v * VEC - row.off + e;
-      const u64 next = on ? has((float)x[e], i) : 0;
-      token = next != 0 ? i : token;
-      w = next != 0 ? next : w;
-      before += next;
-      on = on && (next == 0 || (double)before <= share);
+      const bool is = (int)on & (int)(w[e] != 0);
+      token = is ? v * VEC - row.off + e : token;
+      of_token = is ? w[e] : of_token;
+      before += w[e];
+      on = (int)on & (int)(w[e] == 0 || (double)before <= share);
     }
   }
   a.tokens[row_number] = token;
-  a.probs[row_number] = (float)((double)w / (double)total);
+  a.probs[row_number] = (float)((double)of_token / (double)total);
 }
 
 // From the sums of the stretches: the one that the random share ends in (of 1 and more the last one with a token, of what is no number the first)
@@ -599,7 +612,7 @@ __device__ __forceinline__ void draw(Shared& sh, const SampleArgs& a, int row_nu
   const u64 own = tid < stretches ? sh.sums[tid] : 0;
   u64 total;
   const u64 before = sh.block.before(own, &total);
-  const double share = (double)a.random[row_number] * (double)total;
+  const double share = (double)asked.random * (double)total;
   const int at = sh.block.first(own != 0 && !((double)(before + own) <= share), own != 0);
   if (tid == at) sh.found[0] = before;
   __syncthreads();
@@ -632,7 +645,7 @@ __device__ __forceinline__ void draw_plain(Shared& sh, const SampleArgs& a, int 
   if (asked.k != 0 && kept > (u64)asked.k) kept = asked.k;
   if (asked.shares) kept = (u64)fmax(1.0, ceil(asked.p * (double)kept));
   // (as weights of 1: a random share of the kept ones does not pass the last of them)
-  const double share = fmin((double)a.random[row_number] * (double)kept, (double)kept - 0.5);
+  const double share = fmin((double)asked.random * (double)kept, (double)kept - 0.5);
   answer<T>(sh, a, row_number, part, 0, part.vecs, 0, share, kept, [&](float x, int) { return (u64)(x == top); });
 }
 
@@ -644,7 +657,7 @@ __global__ void __launch_bounds__(kThreads) sample_rows_kernel(const SampleArgs 
   __shared__ Shared sh;
   const Row<T> row(a, blockIdx.x, 0, 1);
   const Asked asked(a, blockIdx.x);
-  clear(sh);
+  clear(sh, asked.cuts());
   const float mine = greatest_of_thread(row), top = value_of((unsigned)sh.block.all((u64)key_of(mine), max_of));
   if (is_plain(asked, top)) return draw_plain<T>(sh, a, blockIdx.x, row, asked, top);
   const Weights weight(top, asked.heat(), sh.table);
@@ -691,8 +704,11 @@ struct Space {
 static_assert(sizeof(Zones) <= 64, "as the workspace has it");
 
 __device__ __forceinline__ float top_of(const Space& s, int parts) {
-  unsigned key = 0;
-  for (int i = 0; i < parts; ++i) key = key > s.tops[i] ? key : s.tops[i];
+  unsigned keys[kSampleParts], key = 0;
+#pragma unroll
+  for (int i = 0; i < kSampleParts; ++i) keys[i] = s.tops[i < parts ? i : 0];  // (side by side)
+#pragma unroll
+  for (int i = 0; i < kSampleParts; ++i) key = key > keys[i] ? key : keys[i];
   return value_of(key);
 }
 
@@ -715,13 +731,13 @@ __global__ void __launch_bounds__(kThreads) sample_histograms_kernel(const Sampl
   const Asked asked(a, blockIdx.y);
   const float top = top_of(s, p.parts);
   if (is_plain(asked, top) || !asked.cuts()) return;
-  clear(sh);
+  clear(sh, true);
   const Weights weight(top, asked.heat(), sh.table);
   histogram(sh, row, asked, weight, bins_asked(sh, asked, weight, p.parts, [&](int i) { return s.maxima[i * kThreads + threadIdx.x]; }));
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kThreads) {
-    s.masses[blockIdx.x * kBins + i] = sh.masses[i];
-    s.counts[blockIdx.x * kBins + i] = sh.counts[i];
+    if (asked.shares) s.masses[blockIdx.x * kBins + i] = sh.masses[i];
+    if (asked.k != 0) s.counts[blockIdx.x * kBins + i] = sh.counts[i];
   }
 }
 
@@ -734,19 +750,25 @@ __global__ void __launch_bounds__(kThreads) sample_sums_kernel(const SampleArgs 
   const Asked asked(a, blockIdx.y);
   const float top = top_of(s, p.parts);
   if (is_plain(asked, top)) return;
-  clear(sh);
+  clear(sh, false);
   const Weights weight(top, asked.heat(), sh.table);
   Zones z{kBins, kBins, -1, kBins, 0, 0, 0, 0};
   if (asked.cuts()) {
-    for (int i = tid; i < kBins; i += kThreads) {
-      u64 m = 0;
-      unsigned c = 0;
-      for (int j = 0; j < p.parts; ++j) {
-        m += s.masses[j * kBins + i];
-        c += s.counts[j * kBins + i];
+    u64 m[kBins / kThreads] = {};
+    unsigned c[kBins / kThreads] = {};
+#pragma unroll
+    for (int j = 0; j < kSampleParts; ++j) {
+      if (j >= p.parts) break;
+#pragma unroll
+      for (int i = 0; i < kBins / kThreads; ++i) {
+        if (asked.shares) m[i] += s.masses[j * kBins + i * kThreads + tid];
+        if (asked.k != 0) c[i] += s.counts[j * kBins + i * kThreads + tid];
       }
-      sh.masses[i] = m;
-      sh.counts[i] = c;
+    }
+#pragma unroll
+    for (int i = 0; i < kBins / kThreads; ++i) {
+      sh.masses[i * kThreads + tid] = m[i];
+      sh.counts[i * kThreads + tid] = c[i];
     }
     __syncthreads();
     z = zones_of(sh, asked);
@@ -777,22 +799,31 @@ __global__ void __launch_bounds__(kThreads) sample_answers_kernel(const SampleAr
     row.to_part(part);
     return draw_plain<T>(sh, a, blockIdx.x, row, asked, top);
   }
-  clear(sh);
+  clear(sh, false);
   const Weights weight(top, asked.heat(), sh.table);
   if (tid < stretches) sh.sums[tid] = s.sums[tid];
   const Zones z = *s.zones;
   u64 cut = 0;
   if (z.sure < kBins) {
-    u64 n = 0;
-    int of_k_bin = 0;
-    for (int j = 0; j < p.parts; ++j) n += s.listed[2 * j];
+    int listed[kSampleParts], of_k_bin = 0;  // (4096 and more of a part: no list)
+    int64_t n = 0;
+#pragma unroll
+    for (int j = 0; j < kSampleParts; ++j) {
+      listed[j] = j < p.parts ? (int)s.listed[2 * j] : 0;
+      of_k_bin += j < p.parts ? (int)s.listed[2 * j + 1] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < kSampleParts; ++j) n += (unsigned)listed[j];
     if (n <= kListed) {
-      int at = 0;
-      for (int j = 0; j < p.parts; ++j) {
-        const int m = (int)s.listed[2 * j];
-        for (int i = tid; i < m; i += kThreads) sh.list[at + i] = s.list[j * kListed + i];
-        at += m;
-        of_k_bin += (int)s.listed[2 * j + 1];
+      for (int i = tid; i < n; i += kThreads) {
+        int part = 0, at = i;
+#pragma unroll
+        for (int j = 0; j + 1 < kSampleParts; ++j) {
+          const bool behind = part == j && at >= listed[j];
+          at -= behind ? listed[j] : 0;
+          part += behind ? 1 : 0;
+        }
+        sh.list[i] = s.list[part * kListed + at];
       }
       __syncthreads();
       cut = cut_of_list<T>(sh, row, asked, weight, z, (int)n, of_k_bin);
