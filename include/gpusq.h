@@ -434,7 +434,7 @@ gpusq_status gpusq_cross_attention(const void* q, const void* k, const void* v, 
 /* ---- answers with drafted tokens.  A step runs, for each sequence, the token that was answered last (node 0) and the tokens that something drafted
  * behind it, a tree: node i is its i-th new token, parents[i] the number, in its sequence, of the node that it follows, one in front of it; any
  * other number: none.  kv_lens counts all of them, cu_q and max_q (at most 512: GPUSQ_ERR_UNSUPPORTED) are as in attention over the cache.  Tokens
- * that no sequence has, and nodes beyond max_q, are not written.
+ * that no sequence has, and nodes beyond max_q, are not written.  Outputs of this part's calls must not overlap inputs.
  *
  * gpusq_draft_tree, before the step: tree [tokens][ceil(max_q / 32)] with the bits of a node and of all that it follows; positions (or NULL) [tokens]:
  *   tokens in front of the new ones, and the nodes that it follows; slots (or NULL) [tokens]: where the cache keeps it, through block_table
