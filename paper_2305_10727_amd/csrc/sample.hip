@@ -18,6 +18,8 @@
 #include "common.h"
 #include "sample_plan.h"
 
+#include <type_traits>
+
 namespace gpusq {
 
 namespace {
@@ -430,11 +432,59 @@ __device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked
   return last_lane(scan(sum, sum_of));
 }
 
-// Descending; n tokens, the rest of a power of two zeros.  A wavefront has 128 places in a row of its own, so only the steps beyond 64 need all of
-// them to meet.
+// The value of lane ^ STEP
+template <int STEP>
+__device__ __forceinline__ unsigned across(unsigned v, int lane) {
+  auto dpp = [](unsigned x, auto ctrl) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xF, 0xF, false); };
+  if constexpr (STEP == 1) return dpp(v, std::integral_constant<int, 0xB1>());  // quad_perm 1 0 3 2
+  if constexpr (STEP == 2) return dpp(v, std::integral_constant<int, 0x4E>());  // quad_perm 2 3 0 1
+  if constexpr (STEP == 4) return dpp(dpp(v, std::integral_constant<int, 0x141>()), std::integral_constant<int, 0x1B>());  // row_half_mirror, quad_perm 3 2 1 0
+  if constexpr (STEP == 8) return dpp(v, std::integral_constant<int, 0x128>());  // row_ror 8
+  if constexpr (STEP == 16) {
+    const auto s = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane & 16 ? s[0] : s[1];
+  }
+  if constexpr (STEP == 32) {
+    const auto s = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane & 32 ? s[0] : s[1];
+  }
+}
+template <int STEP>
+__device__ __forceinline__ void sort_step(u64& v, int span) {
+  const int tid = threadIdx.x;
+  const u64 other = (u64)across<STEP>((unsigned)(v >> 32), tid) << 32 | across<STEP>((unsigned)v, tid);
+  v = ((tid & span) == 0) == ((tid & STEP) == 0) ? max_of(v, other) : v < other ? v : other;
+}
+// Descending; n tokens, the rest of a power of two zeros.  Up to 1024 a thread has one, and only the steps from 64 on go through LDS (250 tokens: 5 us with all
+// of them there, 2.5 so).  Beyond, a wavefront has 128 places in a row of its own, so only the steps beyond 64 need all wavefronts to meet.
 __device__ __forceinline__ void sort_list(u64* list, int n) {
+  const int tid = threadIdx.x;
   int size = 128;
   while (size < n) size *= 2;
+  if (size <= kThreads) {
+    u64 v = tid < n ? list[tid] : 0;
+    for (int span = 2; span <= size; span *= 2) {
+      for (int step = span / 2; step >= 64; step /= 2) {
+        __syncthreads();
+        if (tid < size) list[tid] = v;
+        __syncthreads();
+        if (tid < size) {
+          const u64 other = list[tid ^ step];
+          v = ((tid & span) == 0) == ((tid & step) == 0) ? max_of(v, other) : v < other ? v : other;
+        }
+      }
+      if (span >= 64) sort_step<32>(v, span);
+      if (span >= 32) sort_step<16>(v, span);
+      if (span >= 16) sort_step<8>(v, span);
+      if (span >= 8) sort_step<4>(v, span);
+      if (span >= 4) sort_step<2>(v, span);
+      sort_step<1>(v, span);
+    }
+    __syncthreads();
+    if (tid < size) list[tid] = v;
+    __syncthreads();
+    return;
+  }
   for (int i = n + threadIdx.x; i < size; i += kThreads) list[i] = 0;
   __syncthreads();
   for (int span = 2; span <= size; span *= 2)

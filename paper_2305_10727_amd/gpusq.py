@@ -120,6 +120,14 @@ def _empty(like, dtype, *sizes):
     return _empty(like, dtype, *sizes)
 
 
+def _empties(like, *tensors):
+    """Tensors of (dtype, *sizes) each, on like's device, in one allocation; the extension module, loaded on first use, takes its place"""
+    global _empties
+    from . import _fastcall
+    _empties = _fastcall.empties
+    return _empties(like, *tensors)
+
+
 _lib = None
 
 
@@ -678,7 +686,7 @@ def draft_tree(parents, kv_lens, block_table, cu_q=None, max_q=None):
     i32 = torch.int32
     tokens, batch, max_q = _drafts(parents, kv_lens, cu_q, max_q)
     _want(_is(block_table, i32, batch, -1), "block_table: [batch, max_pages] int32 on the GPU")
-    tree, positions, slots = _empty(parents, i32, tokens, max(1, (max_q + 31) // 32)), _empty(parents, i32, tokens), _empty(parents, i32, tokens)
+    tree, positions, slots = _empties(parents, (i32, tokens, max(1, (max_q + 31) // 32)), (i32, tokens), (i32, tokens))
     calls.gpusq_draft_tree(parents, kv_lens, cu_q, block_table, tree, positions, slots, tokens, batch, max_q, block_table.shape[1])
     return tree, positions, slots
 
@@ -704,8 +712,7 @@ def accept_drafts(drafted, sampled, parents, kv_lens, cu_q=None, max_q=None, cac
         addresses = _fastcall.addresses(caches)  # (kept until the call is made)
         _want(addresses is not None, "caches: contiguous, of one size, on one GPU")
         _want(caches[0].get_device() == torch.cuda.current_device(), "caches: on the current device")
-    path = _empty(parents, i32, batch, max(1, max_q))
-    accepted, answers, new_lens = _empty(parents, i32, batch), _empty(parents, i32, batch), _empty(parents, i32, batch)
+    path, accepted, answers, new_lens = _empties(parents, (i32, batch, max(1, max_q)), (i32, batch), (i32, batch), (i32, batch))
     calls.gpusq_accept_drafts(drafted, sampled, parents, kv_lens, cu_q, block_table, None if addresses is None else addresses[1], layers, path, accepted,
                               answers, new_lens, tokens, batch, max_q, max_pages, pages, kv_heads, head_dim)
     return path, accepted, answers, new_lens
@@ -739,7 +746,7 @@ def sample_tokens(logits, random, temperature=None, top_k=None, top_p=None, min_
     _want(_is(random, f32, R), "random: [rows] float32 on the GPU")
     for t, dt, name in ((temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"), (min_p, f32, "min_p")):
         _want(t is None or _is(t, dt, R), "%s: [rows] %s on the GPU" % (name, "int32" if dt is i32 else "float32"))
-    tokens, probs = _empty(logits, i32, R), _empty(logits, f32, R)
+    tokens, probs = _empties(logits, (i32, R), (f32, R))
     workspace = _workspace(logits, workspace, _size("gpusq_sample_tokens_workspace_bytes", R, V))
     calls.gpusq_sample_tokens(logits, _TORCH_DT[logits.dtype], logits.stride(0) if R > 1 else V, random, temperature, top_k, top_p, min_p, tokens, probs, workspace, R, V)
     return tokens, probs
