@@ -303,10 +303,12 @@ __device__ __forceinline__ int bins_asked(Shared& sh, const Asked& asked, const 
   return last < kBins ? last + 1 : kBins;
 }
 
+// (mine: the thread's greatest; a thread whose greatest is behind what is asked reads nothing, here and below)
 template <typename T>
-__device__ __forceinline__ void histogram(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, int behind) {
+__device__ __forceinline__ void histogram(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, float mine, int behind) {
   constexpr int VEC = Row<T>::VEC;
   const float most = (float)behind;
+  if (!(weight.distance(mine) < most)) return;
   if (asked.k != 0) {
     row.step([&](const float (&x)[VEC], int) {
 #pragma unroll
@@ -371,7 +373,7 @@ __device__ __forceinline__ Zones zones_of(Shared& sh, const Asked& asked) {
 
 // The sum of the wavefront's stretch, of the tokens that are sure; the tokens of the list's bins to the list
 template <typename T>
-__device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, const Zones& z) {
+__device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked& asked, const Weights& weight, float mine, const Zones& z) {
   constexpr int VEC = Row<T>::VEC;
   u64 sum = 0;
   const u64 least = asked.least;
@@ -381,11 +383,12 @@ __device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked
     const unsigned at = atomicAdd(&sh.listed, 1u);
     if (at < kListed) sh.list[at] = place_of(x, i);
   };
+  const float nearest = weight.distance(mine);
   if (z.k_bin == kBins) {  // Most tokens weigh: their weights side by side, without a branch, and what each has too much is taken off at the end
     const u64 enough = least + Weights::kNone;
     u64 none = 0;
     if (z.sure == kBins) {
-      row.step([&](const float (&x)[VEC], int) {
+      if (nearest < sure) row.step([&](const float (&x)[VEC], int) {
         none += VEC * Weights::kNone;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
@@ -394,7 +397,7 @@ __device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked
         }
       });
     } else {
-      row.step([&](const float (&x)[VEC], int i0) {
+      if (nearest < last) row.step([&](const float (&x)[VEC], int i0) {
         none += VEC * Weights::kNone;
         bool some = false;
         float d[VEC];
@@ -414,7 +417,7 @@ __device__ __forceinline__ u64 gather(Shared& sh, const Row<T>& row, const Asked
     }
     sum -= none;
   } else {
-    row.step([&](const float (&x)[VEC], int i0) {
+    if (nearest < last) row.step([&](const float (&x)[VEC], int i0) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         const float d = weight.distance(x[e]);
@@ -713,10 +716,10 @@ __global__ void __launch_bounds__(kThreads) sample_rows_kernel(const SampleArgs 
   const Weights weight(top, asked.heat(), sh.table);
   Zones z{kBins, kBins, -1, kBins, 0, 0, 0, 0};
   if (asked.cuts()) {
-    histogram(sh, row, asked, weight, bins_asked(sh, asked, weight, 1, [&](int) { return mine; }));
+    histogram(sh, row, asked, weight, mine, bins_asked(sh, asked, weight, 1, [&](int) { return mine; }));
     z = zones_of(sh, asked);
   }
-  const u64 sum = gather(sh, row, asked, weight, z);
+  const u64 sum = gather(sh, row, asked, weight, mine, z);
   if ((threadIdx.x & 63) == 0) sh.sums[threadIdx.x >> 6] = sum;
   __syncthreads();
   u64 cut = 0;
@@ -783,7 +786,8 @@ __global__ void __launch_bounds__(kThreads) sample_histograms_kernel(const Sampl
   if (is_plain(asked, top) || !asked.cuts()) return;
   clear(sh, true);
   const Weights weight(top, asked.heat(), sh.table);
-  histogram(sh, row, asked, weight, bins_asked(sh, asked, weight, p.parts, [&](int i) { return s.maxima[i * kThreads + threadIdx.x]; }));
+  const float mine = s.maxima[blockIdx.x * kThreads + threadIdx.x];
+  histogram(sh, row, asked, weight, mine, bins_asked(sh, asked, weight, p.parts, [&](int i) { return s.maxima[i * kThreads + threadIdx.x]; }));
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kThreads) {
     if (asked.shares) s.masses[blockIdx.x * kBins + i] = sh.masses[i];
@@ -823,7 +827,7 @@ __global__ void __launch_bounds__(kThreads) sample_sums_kernel(const SampleArgs 
     __syncthreads();
     z = zones_of(sh, asked);
   }
-  const u64 sum = gather(sh, row, asked, weight, z);
+  const u64 sum = gather(sh, row, asked, weight, s.maxima[blockIdx.x * kThreads + tid], z);
   if ((tid & 63) == 0) s.sums[blockIdx.x * kWaves + (tid >> 6)] = sum;
   __syncthreads();
   const int n = (int)sh.listed;
