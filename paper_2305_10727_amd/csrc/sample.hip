@@ -12,9 +12,9 @@
 // which the bin of the k-th token and the bins between which the p-th share ends are known; for the sums, and the tokens of those bins, which are sorted
 // and decide.  A wavefront sums a stretch of the vocabulary; the token lies in the stretch that passes the random share, which is looked at once more.
 // What bounds it is the instructions of the weights, 22 a token and pass, and of the histogram's atomics in LDS; the first reading is memory's.  So few rows
-// are cut into parts, a workgroup each, in a launch for each reading and one that decides.  256 rows of 131072 fp32 logits (134 MB, 27 us at a copy's
-// rate): 65 us without a cut, 88 with top-k, 114 with top-p, 113 with all; 256 of 32000 fp16 20, 32, 40, 41; one of 32000 17, 23, 34, 28, of 131072 19,
-// 39, 46, 44; greedy ones, of one reading and a launch, 9.
+// are cut into parts, a workgroup each, in a launch for each reading and one that decides; and a thread whose greatest logit is behind the bins that are
+// asked reads nothing more.  256 rows of 131072 fp32 logits (134 MB, 27 us at a copy's rate): 62 us without a cut, 74 with top-k, 109 with top-p, 105 with
+// all; 256 of 32000 fp16 19, 30, 37, 39; one of 32000 16, 21, 31, 26, of 131072 18, 33, 40, 43; greedy ones, of one reading, 5.3.
 #include "common.h"
 #include "sample_plan.h"
 
@@ -704,12 +704,30 @@ __device__ __forceinline__ void draw_plain(Shared& sh, const SampleArgs& a, int 
 
 __device__ __forceinline__ bool is_plain(const Asked& asked, float top) { return top == -__builtin_inff() || top == __builtin_inff() || asked.greedy(); }
 
+// The greedy answer of one reading: the first of the greatest
+template <typename T>
+__device__ __forceinline__ void draw_greatest(Shared& sh, const SampleArgs& a, int row_number, const Row<T>& row) {
+  float best = -__builtin_inff();
+  int at = 0;
+  row.walk([&](float x, int i) {  // (a thread's indices grow; a NaN is not greater)
+    at = x > best ? i : at;
+    best = x > best ? x : best;
+  });
+  const u64 place = sh.block.all(place_of(best, at), max_of);
+  if (threadIdx.x == 0) {
+    const bool none = logit_of(place) == -__builtin_inff();
+    a.tokens[row_number] = none ? -1 : index_of(place);
+    a.probs[row_number] = none ? 0.0f : 1.0f;
+  }
+}
+
 // ---- a workgroup a row ------------------------------------------------------------------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(kThreads) sample_rows_kernel(const SampleArgs a) {
   __shared__ Shared sh;
   const Row<T> row(a, blockIdx.x, 0, 1);
   const Asked asked(a, blockIdx.x);
+  if (asked.greedy()) return draw_greatest<T>(sh, a, blockIdx.x, row);
   clear(sh, asked.cuts());
   const float mine = greatest_of_thread(row), top = value_of((unsigned)sh.block.all((u64)key_of(mine), max_of));
   if (is_plain(asked, top)) return draw_plain<T>(sh, a, blockIdx.x, row, asked, top);
