@@ -84,3 +84,27 @@ def test_sample_tokens(g):
         (ERR_ALIGN, dict(m=P + 2)), (ERR_ALIGN, dict(tokens=P + 2)), (ERR_ALIGN, dict(probs=P + 2)), (ERR_ALIGN, dict(ws=ODD)), (ERR_NULL, dict(V=200000, stride=200000, ws=None))])
     size = g.lib().gpusq_sample_tokens_workspace_bytes
     assert size(1, 200000) > 0 and size(1, 200000) % 16 == 0 and size(1000, 200000) == 0 and size(1, 1000) == 0 and size(0, 1000) == 0 and size(1, 2**18 + 1) == 0
+
+
+def test_results_in_one_allocation(g):
+    """Types and sizes as asked for, each at a multiple of 16 bytes, none over another"""
+    torch = pytest.importorskip("torch")
+    like = torch.zeros(1)
+    wanted = [(torch.int32, 3, 5), (torch.float32, 7), (torch.int32, 0), (torch.uint8, 33), (torch.float16, 2, 1, 3, 1), (torch.int64, 1)]
+    got = g._empties(like, *wanted)
+    assert isinstance(got, tuple) and len(got) == len(wanted)
+    for i, (t, (dtype, *sizes)) in enumerate(zip(got, wanted)):
+        assert t.dtype is dtype and list(t.shape) == sizes and t.is_contiguous() and t.data_ptr() % 16 == 0 and t.device == like.device
+        t.fill_(i + 1)
+    assert all((t == i + 1).all() for i, t in enumerate(got))
+    kept = got[3]
+    del got, t
+    assert (kept.clone() == 4).all()
+    for bad in ((), (torch.int32,), ((torch.int32,),), ((3, 4),), ([torch.int32, 3],), ((torch.int32, 1, 1, 1, 1, 1),), ((torch.int32, "3"),), ((torch.int32, 1),) * 9):
+        with pytest.raises(TypeError):
+            g._empties(like, *bad)
+    for bad in ((torch.int32, -1), (torch.int32, 2**40, 2**40)):
+        with pytest.raises((ValueError, TypeError)):
+            g._empties(like, (torch.int32, 2), bad)
+    with pytest.raises(TypeError):
+        g._empties(3, (torch.int32, 2))

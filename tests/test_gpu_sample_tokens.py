@@ -202,3 +202,34 @@ def test_refusals(g):
         with pytest.raises(g.GpusqError) as e:
             g.sample_tokens(bad, u)
         assert e.value.status == g.ERR_SHAPE
+
+
+@pytest.mark.parametrize("dt", [np.float32, np.float16])
+@pytest.mark.parametrize("V", [1, 5, 1000, 33001, 70001])
+def test_greedy_rows(g, V, dt):
+    """The first of the greatest: zeros of either sign, ties, what is no number in front of it, infinities, nothing at all"""
+    r = np.random.default_rng(V)
+    x = np.round(r.standard_normal((9, V)) * 2).astype(dt)  # (many equal ones)
+    x[1] = np.where(r.random(V) < 0.5, dt(0.0), dt(-0.0))
+    x[2] = -np.inf
+    x[3] = np.nan
+    x[4, : V // 2] = np.nan
+    x[5, r.integers(0, V, 3)] = np.inf
+    x[6, : V - 1] = -np.inf
+    x[7, :] = -65504
+    tokens, probs = g.sample_tokens(dev(x), dev(r.random(9).astype(F32)), temperature=dev(np.array([0, 0, 0, 0, -1, 0, 0, 0, np.nan], F32)), top_k=dev(np.full(9, 3, np.int32)))
+    numbers = np.where(np.isnan(x), -np.inf, x.astype(np.float64))
+    exp = np.where(numbers.max(-1) == -np.inf, -1, numbers.argmax(-1))
+    assert np.array_equal(host(tokens), exp) and np.array_equal(host(probs), (exp >= 0).astype(F32))
+
+
+def test_on_another_stream(g):
+    r = np.random.default_rng(0)
+    x, u = dev(r.standard_normal((5, 70000)).astype(F32)), dev(r.random(5).astype(F32))
+    T, k, p = dev(np.array([1, 0, 0.5, 2, 1], F32)), dev(np.array([0, 0, 40, 2000, 1], np.int32)), dev(np.array([0.9, 1, 1, 0.8, 1], F32))
+    want = [host(t) for t in g.sample_tokens(x, u, temperature=T, top_k=k, top_p=p)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = g.sample_tokens(x, u, temperature=T, top_k=k, top_p=p)
+        torch.cuda.current_stream().synchronize()
+    assert all(np.array_equal(a, host(b)) for a, b in zip(want, got))
