@@ -5,7 +5,9 @@
 //   - the weights stay as they are, rows of K bytes: a wavefront reads 64 consecutive bytes of 16 rows with an instruction, and the next 64 with the next;
 //   - they are the first operand of the 16 x 16 x 64 instruction, whose rows are channels, and the tokens the second: one to 16 tokens cost the same;
 //   - a workgroup's wavefronts share its channels and deal out K; their sums, which are exact, meet in LDS once a tile;
-//   - up to 16 tokens each workgroup quantises them itself, straight into the registers that are multiplied: no launch in front, no codes in memory.
+//   - a few of 32768 values in all each workgroup quantises itself, straight into the registers that are multiplied: no launch in front, no codes in memory.
+// 9 tokens, 4096 -> 131072 (542 MB): 102 us with the quantiser, weights at 5.3 TB/s, where a large copy has 5.0.  1, 16 and 32 tokens, 5120 -> 13824
+// (71 MB): 20, 23 and 26; 8, 16, 32 and 64, 4096 -> 4096: 12.4, 10.8, 12.9, 16.7; 1, 1024 -> 1024: 5.8.
 #include "epilogue.h"
 #include "gelu4.h"
 #include "linear8_plan.h"
@@ -329,6 +331,9 @@ gpusq_status launch_linear_int8_tokens(const Linear8Args& a, hipStream_t s) {
   a.x_f32 ? launch_quantiser<float>(a, s) : launch_quantiser<_Float16>(a, s);
   gpusq_status st = check_launch();
   if (st != GPUSQ_OK) return st;
+  // Whole rows of weights against tokens in registers, or tiles: with 32 tokens the rows are ahead up to 4096 -> 4096 (12.9 us, tiles 20.0) and level at
+  // 5120 -> 13824 (25.5, 24.7); with 64 ahead where the tiles leave CUs idle (4096 -> 4096 16.7 and 19.9, 2048 -> 8192 12.2 and 14.7), behind them
+  // from 16384 channels on (25.8 and 21.8, 28672 32.9 and 28.0).  A workgroup's registers hold 64 tokens of 4096 values.
   if (a.M <= 16)
     steps <= 64 ? launch_16<int8_t>(a, steps, s) : steps <= 96 ? launch_rows<int8_t, 1, 6, 1, false>(a, s) : steps <= 128 ? launch_rows<int8_t, 1, 8, 1, false>(a, s) : launch_rows<int8_t, 1, 8, 1, true>(a, s);
   else if (a.M <= 32)
@@ -337,7 +342,7 @@ gpusq_status launch_linear_int8_tokens(const Linear8Args& a, hipStream_t s) {
     : steps <= 64 ? launch_rows<int8_t, 2, 4, 1, false>(a, s)
     : steps <= 96 ? launch_rows<int8_t, 2, 6, 1, false>(a, s)
                   : launch_rows<int8_t, 2, 4, 1, true>(a, s);
-  else if (a.M <= 64 && steps <= 64 && a.N < 32768)
+  else if (a.M <= 64 && steps <= 64 && a.N <= 8192)
     steps <= 32 ? launch_rows<int8_t, 4, 2, 1, false>(a, s) : launch_rows<int8_t, 4, 4, 1, false>(a, s);
   else {
     const Tokens8Plan plan = tokens8_plan(a.M, a.N, a.K, num_cus());
