@@ -13,7 +13,7 @@
 // and decide.  A wavefront sums a stretch of the vocabulary; the token lies in the stretch that passes the random share, which is looked at once more.
 // What bounds it is the instructions of the weights, 22 a token and pass, and of the histogram's atomics in LDS; the first reading is memory's.  So few rows
 // are cut into parts, a workgroup each, in a launch for each reading and one that decides; and a thread whose greatest logit is behind the bins that are
-// asked reads nothing more.  256 rows of 131072 fp32 logits (134 MB, 27 us at a copy's rate): 62 us without a cut, 74 with top-k, 109 with top-p, 105 with
+// asked reads nothing more.  256 rows of 131072 fp32 logits (134 MB, 27 us at a copy's rate): 60 us without a cut, 70 with top-k, 106 with top-p, 102 with
 // all; 256 of 32000 fp16 19, 30, 37, 39; one of 32000 16, 21, 31, 26, of 131072 18, 33, 40, 43; greedy ones, of one reading, 5.3.
 #include "common.h"
 #include "sample_plan.h"
@@ -169,6 +169,8 @@ struct Row {
   __device__ __forceinline__ Row(const SampleArgs& a, int row, int part, int parts)
       : x((const T*)a.logits + (int64_t)row * a.row_stride), V(a.V), off((int)(((uintptr_t)x & 15) / sizeof(T))), vecs((V + off + VEC - 1) / VEC) {
     per_wave = ((vecs + parts * kWaves - 1) / (parts * kWaves) + 63) & ~63;
+    // (Wavefronts whose stretches begin a multiple of 16 KB apart ask the same channels of the memory at once: 256 rows of 131072 31 us a reading, 25 so)
+    per_wave += per_wave % 1024 == 0 ? 64 : 0;
     begin = (part * kWaves + (threadIdx.x >> 6)) * per_wave;
   }
   __device__ __forceinline__ vec load(int v) const {
