@@ -122,6 +122,20 @@ __device__ __forceinline__ unsigned tree_keys(const int32_t* row, int words, int
   return left >= 32 ? seen : left > 0 ? seen & ((1u << left) - 1) : 0u;
 }
 
+// Value scales of four tokens of a tree, as lane 16 g + r has them (in: of channels that there are): which of the tokens have one that is no finite number in
+// any of the group's lanes, a bit each, and 0 in its place.  Nodes that do not see such a token would have 0 times it otherwise; those that do have no number.
+__device__ __forceinline__ unsigned take_out_infinite(u2& s, bool in, int g) {
+  unsigned bad = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const unsigned word = s[e >> 1], exponent = 0x7C00u << (16 * (e & 1));
+    const bool mine = (word & exponent) == exponent;
+    bad |= (__builtin_amdgcn_ballot_w64(mine && in) >> (16 * g) & 0xFFFF) != 0 ? 1u << e : 0u;
+    s[e >> 1] = mine ? word & (0xFFFF0000u >> (16 * (e & 1))) : word;
+  }
+  return bad;
+}
+
 // (One instruction.  A NaN is passed on, which fmaxf would leave out, with another instruction for each operand to see to it: a column with a
 // NaN among its scores has no other value.)
 __device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }

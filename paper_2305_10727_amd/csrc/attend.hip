@@ -119,6 +119,15 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
 #pragma unroll
           for (int i = 0; i < QT; ++i) seen[i] = there ? tree_keys(words(i), a.tree_words, least, len, key0) >> (4 * g) : 0u;
           x.hide(s, [&](int i, int t, int e) { return (seen[i] >> (16 * t + e) & 1) == 0; });
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            v.s[t] = scales_in_front(v.s[t], there ? len - (key0 + 16 * t + 4 * g) : 0);
+            const unsigned bad = take_out_infinite(v.s[t], CH * r < a.D, g);
+#pragma unroll
+            for (int i = 0; i < QT; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[i][t][e] = (seen[i] >> (16 * t) & bad) >> e & 1 ? __builtin_nanf("") : s[i][t][e];
+          }
         }
       } else if (check) {
         x.hide(s, [&](int i, int t, int e) { return key0 + 16 * t + 4 * g + e >= (there ? x.limit[i] : 0); });
@@ -126,7 +135,7 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       x.follow(s, a);
       x.weights(s, a.c, p);
       x.sum(p);
-      if (check) {
+      if (!TREE && check) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) v.s[t] = scales_in_front(v.s[t], there ? len - (key0 + 16 * t + 4 * g) : 0);
       }

@@ -132,7 +132,8 @@ struct Codes {
       s[1] = u[1];
     }
   }
-  __device__ __forceinline__ void write(uint8_t* rows_of_keys, uint8_t* rows_of_values) const {
+  // (bad: of a tree's tile, for each of its keys whether its values are to be seen as no numbers; else NULL)
+  __device__ __forceinline__ void write(uint8_t* rows_of_keys, uint8_t* rows_of_values, uint8_t* bad, int D) const {
     const int g = lane >> 4, r = lane & 15;
     if (!values) {
 #pragma unroll
@@ -144,7 +145,12 @@ struct Codes {
       }
       return;
     }
-    const h2 s0 = __builtin_bit_cast(h2, (unsigned)s[0]), s1 = __builtin_bit_cast(h2, (unsigned)s[1]), off0 = s0 * (_Float16)-72.0f, off1 = s1 * (_Float16)-72.0f;
+    u2 u = {s[0], s[1]};
+    if (bad != nullptr) {
+      const unsigned b = take_out_infinite(u, CH * r < D, g);
+      if (r == 0) *(unsigned*)(bad + part * 16 + 4 * g) = (b & 1) | (b & 2) << 7 | (b & 4) << 14 | (b & 8) << 21;
+    }
+    const h2 s0 = __builtin_bit_cast(h2, (unsigned)u[0]), s1 = __builtin_bit_cast(h2, (unsigned)u[1]), off0 = s0 * (_Float16)-72.0f, off1 = s1 * (_Float16)-72.0f;
     constexpr int Q = CH >= 8 ? 2 : 1;  // quads of channels that are a piece of a row, or its half
 #pragma unroll
     for (int q0 = 0; q0 < CH / 4; q0 += Q) {
@@ -187,6 +193,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED &
   __shared__ __attribute__((aligned(16))) uint8_t lds[NB * 2 * kTile];  // [buffer][keys, values]
   __shared__ __attribute__((aligned(16))) float begin[BYTES ? NB * KT + 4 : 4];
   __shared__ int pages[2];
+  __shared__ __attribute__((aligned(16))) uint8_t bad[TREE ? 2 : 1][KT];  // whether a key's values are no finite numbers: of tiles that reach into the tree
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, r = lane & 15;
   Work w;
   if (!w.find(a)) return;
@@ -268,6 +275,14 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED &
 #pragma unroll
           for (int i = 0; i < N; ++i) seen[i] = there ? tree_keys(words[i], a.tree_words, least, span.len, key0 + 32 * half) >> (4 * g) : 0u;
           x.hide(s, [&](int i, int t, int e) { return (seen[i] >> (16 * t + e) & 1) == 0; });
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const unsigned b = *(const unsigned*)&bad[buf][32 * half + 16 * t + 4 * g];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[i][t][e] = (seen[i] >> (16 * t + e) & b >> (8 * e)) & 1 ? __builtin_nanf("") : s[i][t][e];
+          }
         }
       } else if (!BYTES && (!there || key0 + 32 * half + 32 > least)) {
         x.hide(s, [&](int i, int t, int e) { return at + 16 * t + e >= (there ? x.limit[i] : 0); });
@@ -289,12 +304,12 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED &
   auto run = [&](auto blocks) {
     int buf = 0;
     if constexpr (KV4) {
-      auto put = [&](int to) {
-        stage.write(lds + to * 2 * kTile, lds + to * 2 * kTile + kTile);
+      auto put = [&](int to, int key0) {
+        stage.write(lds + to * 2 * kTile, lds + to * 2 * kTile + kTile, TREE && key0 + KT > span.before ? bad[TREE ? to : 0] : nullptr, a.D);
         if (threadIdx.x == 0) pages[to] = stage.there;
       };
       if (first_key < end_key) {
-        put(0);
+        put(0, first_key);
         if (first_key + KT < end_key) stage.load(0, first_key + KT);
       }
       for (int key0 = first_key; key0 < end_key; key0 += KT) {
@@ -302,7 +317,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED &
         // the next tile, whose words have had the time of the one before, goes to LDS first: nobody waits for the writes at the next barrier
         const bool there = pages[buf] != 0;
         if (key0 + KT < end_key) {
-          put(buf ^ 1);
+          put(buf ^ 1, key0 + KT);
           if (key0 + 2 * KT < end_key) stage.load(0, key0 + 2 * KT);
         }
         if constexpr (decltype(blocks)::value > 0) multiply(blocks, buf, key0, there);

@@ -147,6 +147,37 @@ def test_pages_that_are_none_and_what_is_no_number(g):
         assert (np.abs(y[2:] - V[2:n, None]) <= 2.0 ** -10 * np.abs(V[2:n, None]) + 2.0 ** -24).all()  # one key each: its value
 
 
+# few columns, blocks of 2 and 3, the kernel for many; heads of every padding
+@pytest.mark.parametrize("H,G,D,L,n", [(4, 4, 64, 30, 9), (8, 2, 128, 300, 4), (8, 2, 128, 3000, 12), (4, 1, 80, 70, 40), (3, 1, 40, 64, 33), (2, 2, 136, 100, 12), (7, 1, 256, 90, 30), (8, 1, 128, 500, 40),
+                                       (16, 1, 64, 200, 30)])
+def test_nodes_that_are_no_numbers(g, H, G, D, L, n):
+    """Keys and values of some nodes with a scale that is infinite, or a value that is none: who sees one is NaN, of that head; nobody else notices"""
+    r = np.random.default_rng(L + n)
+    c = _Cache([L + n], G, D, seed=5)
+    pl = ref.Places(D)
+    sets = _sets(r, [n], "tree")
+    groups = -(-D // 32)
+    poisoned = {int(n // 2): [(pl.v_scale, groups - 1, 0x7C00)], n - 1: [(pl.v_scale, 0, 0x7E00)], n // 3: [(pl.k_scale, 0, 0x7C00)], 1: [(pl.v_scale, 0, 0xFC00), (pl.k_scale, groups - 1, 0x7E01)]}
+    head = G - 1  # the others' are as they were
+    for node, places in poisoned.items():
+        t = L + node
+        halves = c.pages[c.table[0, t // 64]].view(np.uint16)
+        for at, group, bits in places:
+            place = at[t % 64, group]
+            halves[head, place] = bits
+        c.K[0][t, head] = c.V[0][t, head] = 0
+    q = r.standard_normal((n, H, D)).astype(np.float16)
+    words = drafts.bits(sets, -(-n // 32))
+    y = host(_run(g, c, q, [n], words)).astype(np.float64)
+    exp, off = _expected(c, q, [n], sets)
+    sees = np.array([any(j in poisoned for j in nodes) for nodes in sets])
+    of_head = np.arange(H) * G // H == head
+    wrong = sees[:, None] & of_head[None]
+    assert sees.any() and not sees.all()
+    assert np.isnan(y[wrong]).all()
+    assert (np.abs(y - exp) <= off)[~wrong].all()
+
+
 def test_replayed_from_a_graph(g):
     r = np.random.default_rng(11)
     H, G, D, counts = 8, 2, 128, [7, 12]
