@@ -10,7 +10,7 @@ namespace gpusq {
 constexpr int64_t kMostTokens8N = (int64_t)1 << 24;
 inline bool tokens8_countable(int64_t M, int64_t N) { return ceil_div(M, 32) * ceil_div(N, 64) <= INT32_MAX; }
 
-// The tiles of the kernel for many rows (linear8_tiles.hip): 32 tn channels (tn = 8, 4 or 2) x chunks of whole 32-row units, all of the same height or
+// The tiles of the kernel for many rows (linear8_tiles.h): 32 tn channels (tn = 8, 4 or 2) x chunks of whole 32-row units, all of the same height or
 // one unit more.  Tiles are numbered in bands of `band` chunks, inside a band chunks first: round i takes the tiles from i * grid on, in runs of
 // grid / 8 to an XCD, whose L2 then holds the weights of some blocks of channels and the rows of some chunks, about as much of either.
 struct Tokens8Plan {

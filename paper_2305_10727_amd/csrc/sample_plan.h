@@ -9,8 +9,8 @@ namespace gpusq {
 constexpr int kSampleThreads = 1024, kSampleWaves = kSampleThreads / 64, kSampleBins = 2048, kSampleListed = 4096, kSampleParts = 8;
 
 // Parts of a row, a workgroup each.  One is one launch, more are four: worth it where the rows leave most of the device idle and a part has work for
-// longer than a launch takes.  (Top-k and top-p of one row, us, in 1, 2, 4, 8, 16 parts: 32000 tokens 28, 35, 37, 42, 52; 131072 43, 42, 40, 43, 52, and
-// with top-p alone 85, 63, 49, 46, 51; 64 rows of 100003 tokens 81, 69, 64, 82 in 1 to 8.)
+// longer than a launch takes.  (Top-k and top-p of one row, us, in 1, 2, 4, 8 parts: 32000 tokens 27, 34, 35, 41; 131072 47, 46, 40, 43, and with top-p
+// alone 78, 59, 44, 40; 64 rows of 100003 tokens 69, 60, 54, 82.)
 inline int sample_parts(int64_t rows, int64_t vocabulary) {
   int parts = 1;
   if (vocabulary < 65536) return parts;
