@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(64 * NW, tile_waves_per_simd(KV4, DP, MASKED &
       h8 p[N];
       const int at = key0 + 32 * half + 4 * g;
       if constexpr (TREE) {
-        if (!there || key0 + 32 * half + 32 > least) {
+        if (!there || key0 + KT > least) {  // (asked of the tile, as where its values are written: `bad` may name keys of the history)
           unsigned seen[N];
 #pragma unroll
           for (int i = 0; i < N; ++i) seen[i] = there ? tree_keys(words[i], a.tree_words, least, span.len, key0 + 32 * half) >> (4 * g) : 0u;
