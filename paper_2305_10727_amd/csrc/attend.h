@@ -33,8 +33,6 @@ struct AttendArgs {
   const uint8_t* cache;
   const int32_t *table, *cu_q;
   int max_pages, num_pages, tokens;
-  const int32_t* tree;  // [token][tree_words]: which of its sequence's new tokens a token sees (NULL: those up to itself)
-  int tree_words;
   // over fp16 states
   const _Float16 *k, *v;
   int64_t k_batch, k_token, k_head, v_batch, v_token, v_head;
@@ -45,6 +43,9 @@ struct AttendArgs {
   int col_blocks, parts, part_tiles;
   float* part_o;   // [part][row][D] sums, [part][row][2] maximum and sum
   float* part_ml;
+  // over the cache (behind what the kernels without it read: their arguments lie as they are read together)
+  const int32_t* tree;  // [token][tree_words]: which of its sequence's new tokens a token sees (NULL: those up to itself)
+  int tree_words;
 };
 
 __device__ __forceinline__ h8 join(h2 a, h2 b, h2 c, h2 d) { return h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]}; }

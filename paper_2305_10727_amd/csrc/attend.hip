@@ -237,27 +237,35 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
     }
   }
 
-  // Through LDS, a block of 16 columns at a time: every wavefront's sums, maxima and sums of weights, then a thread for each (column, four channels).
-  // Column c keeps its quad i in place i ^ c: what lanes write together lies in different banks.
-  constexpr int QUADS = DP / 4;
-  __shared__ f4 sums[WK][16][QUADS];
-  __shared__ float ml[WK][2][16];
-  __shared__ int rows[16];
+  // Through LDS, of a tree a block of 16 columns at a time (three or four of 8 wavefronts' are more than it holds), else all in one trip (of 17 to 32 columns two
+  // would take 1 to 3 % of a call more: 32 heads of 128 over 8, 8 tokens of 256 sequences of 100 31.3 us in one, 32.2 in two; 1000 states 13.1 and 13.4):
+  // every wavefront's sums, maxima and sums of weights, then a thread for each (column, four channels).
+  // Column c keeps its quad i in place i ^ (c % 16): what lanes write together lies in different banks.
+  constexpr int QUADS = DP / 4, TRIP = TREE ? 1 : QT, COLS = 16 * TRIP;
+  __shared__ f4 sums[WK][COLS][QUADS];
+  __shared__ float ml[WK][2][COLS];
+  __shared__ int rows[COLS];
 #pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    if (col0 + 16 * i >= cols) break;
-    if (i > 0) __syncthreads();
-    if (g == 0) {
-      ml[wk][0][r] = x.m[i];
-      ml[wk][1][r] = x.l[i][0];
-      if (wk == 0) rows[r] = row_of(i);
+  for (int i0 = 0; i0 < QT; i0 += TRIP) {
+    if (i0 > 0) {
+      if (col0 + 16 * i0 >= cols) break;
+      __syncthreads();
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int j = 0; j < TRIP; ++j) {
+      const int i = i0 + j, c = 16 * j + r;
+      if (g == 0) {
+        ml[wk][0][c] = x.m[i];
+        ml[wk][1][c] = x.l[i][0];
+        if (wk == 0) rows[c] = TREE ? row_of(i) : x.row[i];
+      }
 #pragma unroll
-      for (int t = 0; t < CH; t += 4) sums[wk][r][(((4 * g + e) * CH + t) / 4) ^ r] = f4{x.o[i][t][e], x.o[i][t + 1][e], x.o[i][t + 2][e], x.o[i][t + 3][e]};
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t = 0; t < CH; t += 4) sums[wk][c][(((4 * g + e) * CH + t) / 4) ^ r] = f4{x.o[i][t][e], x.o[i][t + 1][e], x.o[i][t + 2][e], x.o[i][t + 3][e]};
+    }
     __syncthreads();
-    for (int at = threadIdx.x; at < 16 * QUADS; at += 64 * WK) {
+    for (int at = threadIdx.x; at < COLS * QUADS; at += 64 * WK) {
       const int col = at / QUADS, quad = at % QUADS, row = rows[col];
       if (row < 0 || 4 * quad >= a.D) continue;
       float top = ml[0][0][col];
@@ -270,7 +278,7 @@ __global__ void __launch_bounds__(64 * WK, waves_per_simd(KV4, DP, QT)) attend_f
       for (int k = 0; k < WK; ++k) {
         const float f = __builtin_amdgcn_exp2f(ml[k][0][col] - ref);
         total += ml[k][1][col] * f;
-        y += sums[k][col][quad ^ col] * f;
+        y += sums[k][col][quad ^ (col & 15)] * f;
       }
       if (a.parts > 1) {
         const int64_t place = (int64_t)w.part * a.tokens * a.heads + row;
