@@ -373,9 +373,15 @@ class DraftedAnswers:
     def __init__(self, layers, vocabulary, device="cuda"):
         if not layers or len({id(l) for l in layers}) < len(layers) or any(l.batch != layers[0].batch or l.D != layers[0].D or l.cache.shape != layers[0].cache.shape for l in layers):
             raise ValueError("layers: at least one, each another, of one width, batch and size of the cache")
+        # what a step's calls behind the layers would refuse, when the tokens are in the caches
+        if len(layers) > 1024 or layers[0].D % 16 != 0 or not 0 < layers[0].D <= 132096:
+            raise ValueError("layers: at most 1024, of a width that is a multiple of 16, at most 132096")
+        if not 0 < vocabulary <= 1 << 18:
+            raise ValueError("vocabulary: 1 to 2^18 tokens")
         self.layers, self.vocabulary, self.batch, self.D = list(layers), vocabulary, layers[0].batch, layers[0].D
-        self.Wq = torch.empty((vocabulary, self.D), dtype=torch.int8, device=device)
-        self.w_scale = torch.empty((vocabulary,), dtype=torch.float32, device=device)
+        rows = -(-vocabulary // 4) * 4  # (the product's channels go by four: zeros behind the vocabulary, whose logits nobody sees)
+        self.Wq = torch.zeros((rows, self.D), dtype=torch.int8, device=device)
+        self.w_scale = torch.zeros((rows,), dtype=torch.float32, device=device)
         self.graph = self.logits = None
 
     def prepare_weights(self, W):
@@ -389,7 +395,8 @@ class DraftedAnswers:
         """drafted, parents [T] int32, T / batch nodes of each sequence: node 0 is its last answer, whose parent is -1; random [T] fp32 in [0, 1); norms: a triple
         for each layer, as DecoderLayer.forward takes it; kv_lens [batch] int32, with all nodes; head_weights: a pair for each layer, or None; temperature, top_k,
         top_p, min_p [T], as sample_tokens takes them.  -> (path [batch, T / batch], accepted [batch], answers [batch], new lengths [batch]); the next
-        step's node 0 is the answer, its kv_lens the new lengths and its nodes.  `logits` [T, vocabulary] fp32 are this step's until the next."""
+        step's node 0 is the answer, its kv_lens the new lengths and its nodes.  `logits` [T, vocabulary] fp32 are this step's until the next (rows in steps of
+        the next multiple of 4)."""
         T, f32, i32 = drafted.shape[0], torch.float32, torch.int32
         # what a later call would refuse, before the tokens are in the caches
         G._want(T % self.batch == 0, "drafted: as many nodes of each of the %d sequences" % self.batch)
@@ -403,6 +410,8 @@ class DraftedAnswers:
             x = layer.forward(x, norms[i], rope, positions, slots, block_table, kv_lens, head_weights=(None, None) if head_weights is None else head_weights[i],
                               state_lens=state_lens, tree=tree)
         self.logits = G.linear_int8_tokens(head_norm(x), self.Wq, self.w_scale, out_dtype=f32)
+        if self.logits.shape[1] > self.vocabulary:
+            self.logits = self.logits[:, :self.vocabulary]
         sampled, _ = G.sample_tokens(self.logits, random, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
         return G.accept_drafts(drafted, sampled, parents, kv_lens, caches=[layer.cache for layer in self.layers], block_table=block_table)
 
