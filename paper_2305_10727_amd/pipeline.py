@@ -288,6 +288,11 @@ class EncoderBlockLinears:
         return self.fc2.Y
 
 
+def _ready(t, device, dtype, *sizes):
+    """Whether t is what a launching call takes: of that type and those sizes, without gaps, on that device (None: on any)"""
+    return G._is(t, dtype, *sizes) and t.is_contiguous() and (device is None or t.get_device() == device)
+
+
 class DecoderLayer:
     """One layer of a decoder that answers from images which the layers above have encoded, as it serves: attention over its own tokens in a
     4-bit cache, attention to the encoder's states, two feed-forward layers; its weights in 4 bits with a scale for each group.
@@ -330,11 +335,12 @@ class DecoderLayer:
         kv_lens [batch] (with the new tokens), state_lens [batch] or None, tree [T, words] or None (gpusq.draft_tree, as positions and slots then are:
         the new tokens are drafts, and see what they follow): int32.  -> [T, D] fp16"""
         T, H, hd = x.shape[0], self.heads, self.head_dim
+        on = None if tree is None else torch.cuda.current_device()  # (which the calls with a tree ask for)
         # what a later call would refuse, before the tokens are in the cache
         G._want(T % self.batch == 0, "x: as many tokens of each of the %d sequences" % self.batch)
-        G._want(G._is(block_table, torch.int32, self.batch, -1) and G._is(kv_lens, torch.int32, self.batch) and
-                (state_lens is None or G._is(state_lens, torch.int32, self.batch)), "block_table: [batch, pages] int32, kv_lens and state_lens: [batch] int32, on the GPU")
-        G._want(tree is None or G._is(tree, torch.int32, T, max(1, (T // self.batch + 31) // 32)), "tree: [tokens, words] int32 of draft_tree")
+        G._want(_ready(block_table, on, torch.int32, self.batch, -1) and _ready(kv_lens, on, torch.int32, self.batch) and
+                (state_lens is None or _ready(state_lens, on, torch.int32, self.batch)), "block_table: [batch, pages] int32, kv_lens and state_lens: [batch] int32, on the GPU, contiguous")
+        G._want(tree is None or _ready(tree, on, torch.int32, T, max(1, (T // self.batch + 31) // 32)), "tree: [tokens, words] int32 of draft_tree")
         q = G.qk_norm_rope(self._linear("qkv", norms[0](x)), H, self.kv_heads, hd, q_weight=head_weights[0], k_weight=head_weights[1], cos=rope[0], sin=rope[1],
                            positions=positions, cache=self.cache, slots=slots)
         a = G.attention_kv4(q, self.cache, block_table, kv_lens, max_q=T // self.batch, tree=tree)
@@ -397,12 +403,12 @@ class DraftedAnswers:
         top_p, min_p [T], as sample_tokens takes them.  -> (path [batch, T / batch], accepted [batch], answers [batch], new lengths [batch]); the next
         step's node 0 is the answer, its kv_lens the new lengths and its nodes.  `logits` [T, vocabulary] fp32 are this step's until the next (rows in steps of
         the next multiple of 4)."""
-        T, f32, i32 = drafted.shape[0], torch.float32, torch.int32
+        T, f32, i32, on = drafted.shape[0], torch.float32, torch.int32, torch.cuda.current_device()
         # what a later call would refuse, before the tokens are in the caches
         G._want(T % self.batch == 0, "drafted: as many nodes of each of the %d sequences" % self.batch)
-        G._want(G._is(drafted, i32, T) and G._is(parents, i32, T) and G._is(kv_lens, i32, self.batch), "drafted, parents: [tokens] int32, kv_lens: [batch] int32, on the GPU")
+        G._want(_ready(drafted, on, i32, T) and _ready(parents, on, i32, T) and _ready(kv_lens, on, i32, self.batch), "drafted, parents: [tokens] int32, kv_lens: [batch] int32, on the GPU, contiguous")
         for t, dt, name in ((random, f32, "random"), (temperature, f32, "temperature"), (top_k, i32, "top_k"), (top_p, f32, "top_p"), (min_p, f32, "min_p")):
-            G._want((t is None and name != "random") or G._is(t, dt, T), "%s: [tokens] %s on the GPU" % (name, "int32" if dt is i32 else "float32"))
+            G._want((t is None and name != "random") or _ready(t, on, dt, T), "%s: [tokens] %s on the GPU, contiguous" % (name, "int32" if dt is i32 else "float32"))
         G._want(len(norms) == len(self.layers) and (head_weights is None or len(head_weights) == len(self.layers)), "norms, head_weights: of each layer")
         tree, positions, slots = G.draft_tree(parents, kv_lens, block_table)
         x = embed(drafted)

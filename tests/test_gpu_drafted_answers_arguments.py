@@ -1,9 +1,9 @@
-"""pipeline.DraftedAnswers: vocabularies of any size."""
+"""pipeline.DraftedAnswers: vocabularies of any size, and arguments that a later call of a step would refuse: before the caches are written."""
 import numpy as np
 import pytest
 
 import drafts_reference as drafts
-from test_gpu_drafted_answers import B, D, F32, V, Model
+from test_gpu_drafted_answers import B, D, F32, LAYERS, V, Model
 from test_gpu_parity import dev, g, host  # noqa: F401
 
 torch = pytest.importorskip("torch")
@@ -65,3 +65,37 @@ def test_a_vocabulary_that_is_no_multiple_of_4(model, vocabulary):
         again = some.replay()
         torch.cuda.synchronize()
         assert all(np.array_equal(host(a), b) for a, b in zip(again, got)) and np.array_equal(host(some.logits), logits[:, :vocabulary])
+
+
+def _apart(t):
+    """The same values with others between them"""
+    return torch.stack([t, t], -1)[..., 0]
+
+
+def test_arguments_with_gaps_are_refused_in_front_of_the_caches(model):
+    from paper_2305_10727_amd import gpusq as G
+    r = np.random.default_rng(1)
+    (args, kw), *_ = _step_arguments(model, r)
+    before = [layer.cache.clone() for layer in model.layers]
+    for at in (0, 1, 2, 7, 8):  # drafted, parents, random, the table, lengths
+        with pytest.raises(ValueError):
+            model.answers.step(*args[:at], _apart(args[at]), *args[at + 1:], **kw)
+    for name, t in kw.items():
+        with pytest.raises(ValueError):
+            model.answers.step(*args, **{**kw, name: _apart(t)})
+    states = torch.full((B,), 5, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        model.answers.step(*args, **kw, state_lens=_apart(states))
+    assert all(torch.equal(c, layer.cache) for c, layer in zip(before, model.layers))
+    # a layer by itself
+    tree, positions, slots = G.draft_tree(args[1], args[8], model.table)
+    x, layer = model.embed(args[0]), model.layers[0]
+    call = lambda table=model.table, lens=args[8], **k: layer.forward(x, model.norms[0], model.rope, positions, slots, table, lens, **k)  # noqa: E731
+    for bad in (dict(tree=_apart(tree)), dict(tree=tree, table=_apart(model.table)), dict(tree=tree, lens=_apart(args[8])), dict(tree=tree, state_lens=_apart(states)),
+                dict(table=_apart(model.table)), dict(lens=_apart(args[8])), dict(state_lens=_apart(states))):
+        with pytest.raises(ValueError):
+            call(**bad)
+    assert all(torch.equal(c, layer.cache) for c, layer in zip(before, model.layers))
+    assert LAYERS == len(model.layers)
+    call(tree=tree, state_lens=states)
+    assert not torch.equal(before[0], layer.cache)
