@@ -466,7 +466,8 @@ gpusq_status gpusq_linear_int8_tokens(const void* X, gpusq_dtype dt, const int8_
 
 /* Tokens drawn from logits [rows][vocabulary] (dt GPUSQ_F16 or GPUSQ_F32, row_stride values from row to row, aligned to a value; at most 2^18 tokens,
  * GPUSQ_ERR_SHAPE) with given random numbers, one in [0, 1) a row.  temperature, top_k, top_p, min_p: [rows] each, or NULL (1, and no cut).
- *   A token's weight is exp((x - max) / temperature), to 2^-30 of it, 0 below 2^-40; 1 where x is the greatest, also where that is infinite.  Tokens are
+ *   A token's weight is exp((x - max) / temperature), to 2^-30 of it and 2^-45 of the greatest's (one of 2^-40 is known to 2^-5 of itself, and so is its
+ *   share), 0 below 2^-40 or where x - max is beyond what 32 bits hold; 1 where x is the greatest, also where that is infinite.  Tokens are
  *   ordered by their logits, ties by their index, the lower first; -infinity and NaN are never drawn.  Kept are the first top_k (0 or less: all);
  *   of those as many as it takes for top_p of their weight, one at least (1 and more: all); of those the ones of a weight of min_p or more (of the
  *   first one's, which is 1; at most 1 is asked).

@@ -4,9 +4,10 @@
 //   first whose weights reach p of the first k's, and in front of the first whose weight is below min_p;  drawn is the first token, in the
 //   vocabulary's order, up to which the kept weights pass u of their sum.
 //
-// Where two tokens' shares meet is closer to a neighbour's than 32 bits tell apart, so weights are formed to 2^-31 of themselves and summed as whole
-// numbers of 2^-44, of which no order changes the sum.  A token's place in the order is one number, its logit's bits made monotone and its index
-// counted down: a cut is the least such number that is kept.
+// Where two tokens' shares meet is closer to a neighbour's than 32 bits tell apart, so weights are formed to 2^-31 of themselves, rounded to whole
+// numbers of 2^-44 of the greatest's (one of 2^-40 to 2^-5 of itself; in their sum that is 2^-45 a token) and summed as these, of which no order changes
+// the sum.  A token's place in the order is one number, its logit's bits made monotone and its index counted down: a cut is the least such number that
+// is kept.
 //
 // A row is read three times: for its greatest logit; for a histogram of the logits' distances from it, in 2048 bins of 28 / 2048 of the temperature, from
 // which the bin of the k-th token and the bins between which the p-th share ends are known; for the sums, and the tokens of those bins, which are sorted
