@@ -55,13 +55,16 @@ struct AttendShape {
 // Trees of drafts over the cache, of so many pairs (batch, key head), else 0, are a few tens of nodes: 33 to 256 columns leave wavefronts with columns of their own
 // one block each, or none, between two barriers a tile.  So they deal out the keys, with up to 3 blocks (4 of heads of 64: what registers hold of two
 // wavefronts a SIMD) and as many workgroups as that takes: what is spent on 32 keys, however many columns, is 190 instructions for their codes, and 45
-// a block.  16 trees of 24 behind up to 4096 tokens, 32 heads of 128 over 8: 42 us (columns of their own: 71); one of 32 behind 65536 66 (77), of 48 82
-// (84), of 63 112 (96), but 16 of 64 80 (90): up to kTreeColumns, or 256 of many pairs.
+// a block.  Keys dealt out, and columns of their own, us: 16 trees of 24 behind up to 4096 tokens, 32 heads of 128 over 8: 42, 71; one of 32 behind 65536 66, 77, of 48
+// 82, 84, of 63 112, 96.  So up to kTreeColumns.  Up to 256 where many pairs have uneven lengths (8 sequences of 52 nodes 49, 53, of 64 57, 57; 16 of 52 62 to 85, 89,
+// of 64 89 to 104, 92; 64 of 64 257, 272; but 16 of 64 of one length 104, 94), not with fewer than 64 pairs (2 and 4 sequences of 64 nodes behind 16384 and 8192:
+// 71, 58 and 69, 57); heads of 64, which have four blocks, from 16 on (the same: 38, 43 and 38, 39).
 // 8 wavefronts that fill a CU, or two workgroups of 4 where there are two for each CU: 64 trees of 24 behind 2000 tokens 81 and 66 us, 16 behind 4096 42 and 54.
 constexpr int kTreeColumns = 192;
+constexpr int tree_many_pairs(int DP) { return DP == 64 ? 16 : 64; }
 constexpr int tree_blocks(int DP) { return DP == 64 ? 4 : DP == 128 ? 3 : 1; }
 inline AttendShape attend_shape(bool kv4, int DP, int64_t cols, bool reach, int64_t tree_pairs = 0) {
-  if (tree_pairs > 0 && DP < 256 && cols <= (tree_pairs >= 16 ? 256 : kTreeColumns)) {
+  if (tree_pairs > 0 && DP < 256 && cols <= (tree_pairs >= tree_many_pairs(DP) ? 256 : kTreeColumns)) {
     const int64_t blocks = ceil_div(cols, 16), groups = ceil_div(blocks, tree_blocks(DP)), each = ceil_div(blocks, groups);
     return AttendShape{false, 16 * (int)each, each > 1 && tree_pairs * groups >= 512 ? 256 : 512};
   }
