@@ -332,8 +332,10 @@ gpusq_status launch_linear_int8_tokens(const Linear8Args& a, hipStream_t s) {
   gpusq_status st = check_launch();
   if (st != GPUSQ_OK) return st;
   // Whole rows of weights against tokens in registers, or tiles: with 32 tokens the rows are ahead up to 4096 -> 4096 (12.9 us, tiles 20.0) and level at
-  // 5120 -> 13824 (25.5, 24.7); with 64 ahead where the tiles leave CUs idle (4096 -> 4096 16.7 and 19.9, 2048 -> 8192 12.2 and 14.7), behind them
-  // from 16384 channels on (25.8 and 21.8, 28672 32.9 and 28.0).  A workgroup's registers hold 64 tokens of 4096 values.
+  // 5120 -> 13824 (25.5, 24.7).  With 64 of 4096 values they are ahead up to 8192 channels (4096 16.8 and 20.3, 8192 19.6 and 20.7, 8196 21.7 and 20.6, 12288 23.0 and
+  // 20.5, 28672 32.9 and 28.0; with 33 tokens to 12288, 20.1 and 20.5), of 2048 and less, where the tiles have fewer steps to make up for idle CUs, up to 12288
+  // (64 tokens of 2048: 8192 12.6 and 15.1, 12288 14.9 and 15.2, 14336 16.7 and 15.6; 33 of 1024: 12288 11.3 and 12.4, 14336 12.7 and 12.3).  A workgroup's registers
+  // hold 64 tokens of 4096 values.
   if (a.M <= 16)
     steps <= 64 ? launch_16<int8_t>(a, steps, s) : steps <= 96 ? launch_rows<int8_t, 1, 6, 1, false>(a, s) : steps <= 128 ? launch_rows<int8_t, 1, 8, 1, false>(a, s) : launch_rows<int8_t, 1, 8, 1, true>(a, s);
   else if (a.M <= 32)
@@ -342,7 +344,7 @@ gpusq_status launch_linear_int8_tokens(const Linear8Args& a, hipStream_t s) {
     : steps <= 64 ? launch_rows<int8_t, 2, 4, 1, false>(a, s)
     : steps <= 96 ? launch_rows<int8_t, 2, 6, 1, false>(a, s)
                   : launch_rows<int8_t, 2, 4, 1, true>(a, s);
-  else if (a.M <= 64 && steps <= 64 && a.N <= 8192)
+  else if (a.M <= 64 && steps <= 64 && a.N <= (steps <= 32 ? 12288 : 8192))
     steps <= 32 ? launch_rows<int8_t, 4, 2, 1, false>(a, s) : launch_rows<int8_t, 4, 4, 1, false>(a, s);
   else {
     const Tokens8Plan plan = tokens8_plan(a.M, a.N, a.K, num_cus());
