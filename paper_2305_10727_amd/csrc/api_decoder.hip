@@ -1,6 +1,8 @@
 // C ABI of the decoder's operators: argument validation, status codes, dispatch to the kernels.  No computation happens here.
 #include <math.h>
 
+#include <algorithm>
+
 #include "attend_plan.h"
 #include "drafts_plan.h"
 #include "linear8_plan.h"
@@ -17,6 +19,7 @@ constexpr int64_t kMostTokens8K = INT32_MAX / (127 * 128) / 64 * 64;
 // a row's weights, whole numbers up to 2^44, are together below 2^63
 constexpr int64_t kMostVocabulary = (int64_t)1 << 18;
 
+constexpr int64_t kMostCaches = 1024;  // of a call that moves tokens in them
 constexpr int64_t kMostPages = INT32_MAX / kPageTokens - 1;  // of a sequence: tokens are counted in 31 bits, a page beyond the last too
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
@@ -228,19 +231,23 @@ gpusq_status gpusq_accept_drafts(const int32_t* drafted, const int32_t* sampled,
   if (layers != 0 && (!caches || !block_table)) return GPUSQ_ERR_NULL;
   gpusq_status st = check_drafts(tokens, batch, max_q, cu_q);
   if (st != GPUSQ_OK) return st;
-  if (layers < 0 || layers > 1024 || batch * max_q > kMaxElems) return GPUSQ_ERR_SHAPE;
+  if (layers < 0 || layers > kMostCaches || batch * max_q > kMaxElems) return GPUSQ_ERR_SHAPE;
   if (layers != 0) {
     st = check_heads(kv_heads, kv_heads, head_dim);
     if (st != GPUSQ_OK) return st;
     if (!is_size(max_pages) || max_pages > kMostPages || !is_size(num_pages) || num_pages > INT32_MAX / kPageTokens || caches_of_launch(batch, kv_heads) < 1)
       return GPUSQ_ERR_SHAPE;
-    const int64_t bytes = num_pages * kv_heads * page_bytes(padded_head((int)head_dim));
+    const uint64_t bytes = (uint64_t)num_pages * kv_heads * page_bytes(padded_head((int)head_dim));
+    uintptr_t at[kMostCaches];
     for (int64_t i = 0; i < layers; ++i) {
       if (!caches[i]) return GPUSQ_ERR_NULL;
       if (!aligned16(caches[i])) return GPUSQ_ERR_ALIGN;
-      for (int64_t j = 0; j < i; ++j)  // (the same tokens moved twice)
-        if (overlap(ByteRange{caches[i], bytes}, ByteRange{caches[j], bytes})) return GPUSQ_ERR_UNSUPPORTED;
+      at[i] = (uintptr_t)caches[i];
     }
+    // (the same tokens moved twice: of caches of one size that overlap some two are neighbours in the order of their addresses)
+    std::sort(at, at + layers);
+    for (int64_t i = 1; i < layers; ++i)
+      if (at[i] - at[i - 1] < bytes) return GPUSQ_ERR_UNSUPPORTED;
   }
   if (!aligned4(drafted) || !aligned4(sampled) || !aligned4(parents) || !aligned4(kv_lens) || !aligned4(cu_q) || !aligned4(block_table) || !aligned4(path) ||
       !aligned4(accepted) || !aligned4(answers) || !aligned4(new_lens))
