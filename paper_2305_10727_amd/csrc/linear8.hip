@@ -7,7 +7,7 @@
 //   - a workgroup's wavefronts share its channels and deal out K; their sums, which are exact, meet in LDS once a tile;
 //   - a few of 32768 values in all each workgroup quantises itself, straight into the registers that are multiplied: no launch in front, no codes in memory.
 // 9 tokens, 4096 -> 131072 (542 MB): 102 us with the quantiser, weights at 5.3 TB/s, where a large copy has 5.0.  1, 16 and 32 tokens, 5120 -> 13824
-// (71 MB): 20, 23 and 26; 8, 16, 32 and 64, 4096 -> 4096: 12.4, 10.8, 12.9, 16.7; 1, 1024 -> 1024: 5.8.
+// (71 MB; 216 workgroups have four tiles each, 40 CUs none): 20, 23 and 26; 8, 16, 32 and 64, 4096 -> 4096: 12.4, 10.8, 12.9, 16.7; 1, 1024 -> 1024: 5.8.
 #include "epilogue.h"
 #include "gelu4.h"
 #include "linear8_plan.h"

@@ -15,7 +15,7 @@
 // What bounds it is the instructions of the weights, 22 a token and pass, and of the histogram's atomics in LDS; the first reading is memory's.  So few rows
 // are cut into parts, a workgroup each, in a launch for each reading and one that decides; and a thread whose greatest logit is behind the bins that are
 // asked reads nothing more.  256 rows of 131072 fp32 logits (134 MB, 27 us at a copy's rate): 60 us without a cut, 70 with top-k, 106 with top-p, 102 with
-// all; 256 of 32000 fp16 19, 30, 37, 39; one of 32000 16, 21, 31, 26, of 131072 18, 33, 40, 43; greedy ones, of one reading, 5.3.
+// all; 256 of 32000 fp16 19, 30, 37, 39; one of 32000 16, 21, 31, 26, of 131072 18, 33, 40, 43; greedy ones, of one reading, 5.3, of 131072 over several workgroups 12.7.
 #include "common.h"
 #include "sample_plan.h"
 
@@ -544,7 +544,8 @@ __device__ __forceinline__ u64 cut_of_list(Shared& sh, const Row<T>& row, const 
   return cut;
 }
 
-// By histograms of the places' digits, one after the other, over the whole row: of rows whose bins hold too many tokens to sort (ties).  The least
+// By histograms of the places' digits, one after the other, over the whole row: of rows whose bins hold too many tokens to sort (ties; nearly flat rows, which
+// take 0.5 to 1.1 ms for 64 rows of 100003 and are no model's).  The least
 // place of the smallest front part of the order from `from` on that has `target` tokens, or so much weight.
 template <typename T>
 __device__ __attribute__((noinline)) u64 cut_by_digits(Shared& sh, const Row<T>& row, const Weights& weight, bool by_mass, double target, u64 from) {
