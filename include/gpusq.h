@@ -412,7 +412,8 @@ gpusq_status gpusq_attention_kv4(const void* q, const void* cache, const int32_t
 /* The same for a tree of drafted tokens: a sequence's new tokens (its last ones in the cache) see every token in front of them, and of each other
  * those that bits of tree [tokens][tree_words] say: bit j % 32 of word j / 32 of a token's row stands for the j-th new token of its sequence (itself
  * is one of them; bits of tokens that it has not are not read).  tree_words * 32 >= max_q (GPUSQ_ERR_SHAPE), at most 2^30 tokens.  A token that sees
- * nothing gives 0.  Nodes whose keys or values are no finite numbers (by their scales) make those that see them NaN, and no others. */
+ * nothing gives 0.  Nodes whose keys or values are no finite numbers (by their scales) make those that see them NaN, and no others; of a token in front
+ * of them, which all see, every node's results have no finite numbers in the channels of that scale at least. */
 size_t gpusq_attention_tree_kv4_workspace_bytes(int64_t tokens, int64_t batch, int64_t max_q, int64_t max_pages, int64_t heads, int64_t kv_heads, int64_t head_dim);
 gpusq_status gpusq_attention_tree_kv4(const void* q, const void* cache, const int32_t* block_table, const int32_t* kv_lens, const int32_t* cu_q,
                                       const int32_t* tree, int64_t tree_words, void* out, void* workspace, int64_t tokens, int64_t batch, int64_t max_q,
